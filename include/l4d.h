@@ -341,6 +341,161 @@ int lm_head_bwd(const l4d_model* model, const l4d_parallel* par, const void* w_n
                 void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Packed documents
+ *
+ * A micro-batch may hold documents of different lengths one behind another in
+ * one row of `tokens` tokens, instead of b sequences of equal length.  Document
+ * i holds rows [starts[i], starts[i + 1]); attention does not cross documents
+ * and positions count from a document's first row.
+ *   starts: int64 [n_seqs + 1] device array, nondecreasing, 0 <= starts[0],
+ *   starts[n_seqs] <= tokens.  Documents may be empty.  Rows before starts[0] or
+ *   from starts[n_seqs] on belong to no document: their inputs are not used and
+ *   their outputs are left as they were, whatever they hold.
+ * The starts are read on the GPU only; values that break the rule give
+ * unspecified results, but no access outside the `tokens` rows.
+ * 0 <= tokens <= 2^30, 0 <= n_seqs <= 2^30.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int64_t tokens;         /* rows of every token-major array of the call */
+  int64_t n_seqs;         /* documents */
+  const int64_t* starts;  /* device, may be NULL when n_seqs == 0 */
+} l4d_packing;
+
+/* ------------------------------------------------------------------------
+ * Rotary positions
+ *
+ * Pair j (0 <= j < rot_dim/2) of every head is turned by the angle pos * f_j
+ * and multiplied by the amplitude A:
+ *   y0 = A (x0 cos - x1 sin),  y1 = A (x1 cos + x0 sin),
+ * the elements rot_dim .. head_dim - 1 of a head are copied.  rope_bwd applies
+ * the transposed map (angle -pos f_j), which takes the gradient of y to that of x.
+ *   layout   L4D_ROPE_HALF: pair j is (j, j + rot_dim/2), the layer's own layout;
+ *            L4D_ROPE_INTERLEAVED: pair j is (2j, 2j + 1).
+ *   scaling  f_j = base^(-2j/rot_dim) ((1 - g_j)/factor + g_j), where
+ *            L4D_ROPE_PLAIN   g_j = 1;
+ *            L4D_ROPE_LINEAR  g_j = 0 (positions divided by factor);
+ *            L4D_ROPE_BANDS   g_j = clamp((r_j - low)/(high - low), 0, 1) with
+ *                             r_j = original base^(-2j/rot_dim) / 2 pi the turns of
+ *                             pair j over the original context;
+ *            L4D_ROPE_RAMP    g_j = 1 - clamp((j - j0)/(j1 - j0), 0, 1), j0 and j1 the
+ *                             pair indices, rounded down and up, at which a pair makes
+ *                             high and low turns over the original context, kept
+ *                             within 0 and rot_dim - 1; 0.001 stands for j1 - j0 = 0.
+ * Angles are formed and reduced in double precision, the rotation is fp32,
+ * and the result is rounded once.
+ *   dtype: L4D_BF16 or L4D_F32, of every tensor of the call;
+ *   positions: int64 [tokens] device array of any sign, or NULL: the distance from
+ *   the document's first row (from row 0 without a packing);
+ *   packing: NULL = every row is rotated, else packing->tokens == tokens;
+ *   q, k: up to two tensors [tokens][heads][head_dim] rotated in one launch (k may be
+ *   NULL).  Row i starts at x + i x_ld, heads are contiguous within a row, so the
+ *   columns of a fused [tokens][(a_t + 2 k_t) d_h] array are addressed in place.
+ *   y == x with y_ld == x_ld rotates in place; other overlaps of a tensor's input
+ *   and output ranges are refused.
+ * L4D_EINVAL: head_dim outside 2 .. 512, rot_dim odd or outside 2 .. head_dim, an
+ * unknown enum value, base <= 1, factor <= 0, amplitude <= 0, original <= 0 or not
+ * 0 < low < high where the scaling uses them, ld < heads head_dim, NULL or
+ * misaligned tensors (element size).  tokens == 0 launches nothing.
+ * ---------------------------------------------------------------------- */
+enum { L4D_BF16 = 0, L4D_F32 = 1 };
+enum { L4D_ROPE_HALF = 0, L4D_ROPE_INTERLEAVED = 1 };
+enum { L4D_ROPE_PLAIN = 0, L4D_ROPE_LINEAR = 1, L4D_ROPE_BANDS = 2, L4D_ROPE_RAMP = 3 };
+
+typedef struct {
+  int64_t head_dim, rot_dim;
+  int32_t layout, scaling;
+  double base;
+  double factor;        /* LINEAR, BANDS, RAMP */
+  double low, high;     /* turns over the original context: BANDS, RAMP */
+  double original;      /* original context length: BANDS, RAMP */
+  double amplitude;     /* A, 1 = a pure rotation */
+} l4d_rope;
+
+typedef struct {
+  const void* x;
+  void* y;
+  int64_t heads;
+  int64_t x_ld, y_ld;   /* elements between consecutive rows */
+} l4d_rope_heads;
+
+int rope_fwd(const l4d_rope* rope, int dtype, int64_t tokens, const l4d_packing* packing, const int64_t* positions,
+             const l4d_rope_heads* q, const l4d_rope_heads* k, void* hip_stream);
+int rope_bwd(const l4d_rope* rope, int dtype, int64_t tokens, const l4d_packing* packing, const int64_t* positions,
+             const l4d_rope_heads* dq, const l4d_rope_heads* dk, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Causal attention over packed documents, grouped query heads
+ *
+ *   o_i = sum_j p_ij v_j,  p_i. = softmax of scale q_i . k_j over the rows j <= i of
+ *   row i's document;  lse_i = log sum_j exp(scale q_i . k_j).
+ * Query head h uses key/value head h / (n_heads/n_kv_heads).
+ *   q, o, d_o, dq: bf16 [tokens][n_heads][head_dim];  k, v, dk, dv: bf16
+ *   [tokens][n_kv_heads][head_dim]; row i of each starts at its pointer + i ld
+ *   (elements), heads contiguous within a row (columns of a fused array are fine);
+ *   lse: f32 [n_heads][tokens], natural logarithm, written by the forward, read by
+ *   the backward.  Outputs must not overlap inputs or each other.
+ * The backward overwrites dq, dk, dv with the gradients for d_o (dk and dv summed
+ * over the query heads of their head); its sums have a fixed order.  A value that
+ * is not finite in one document reaches no other document.
+ * L4D_EINVAL: head_dim not 64 or 128, n_heads % n_kv_heads != 0, more than 2^16
+ * heads, a scale that is negative or not finite, an ld that is smaller than the
+ * heads' columns, no multiple of 8 or above 2^22, a NULL tensor or one not 16-byte
+ * aligned (lse: 4), more blocks than a launch holds (2^24 blocks of rows and heads).  tokens == 0 or n_seqs == 0 launches nothing.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int64_t n_heads, n_kv_heads, head_dim;
+  float scale;          /* 0 = 1/sqrt(head_dim) */
+} l4d_attn;
+
+int attn_packed_fwd(const l4d_attn* attn, const l4d_packing* packing, const void* q, int64_t q_ld, const void* k,
+                    int64_t k_ld, const void* v, int64_t v_ld, void* o, int64_t o_ld, float* lse, void* hip_stream);
+/* Arena room of the backward (rowsum(d_o * o) per row and head, and fp32 partial
+ * sums of dk and dv where the query heads of a key head are split). */
+int l4d_attn_packed_workspace_bytes(const l4d_attn* attn, int64_t tokens, uint64_t* bytes);
+int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void* q, int64_t q_ld, const void* k,
+                    int64_t k_ld, const void* v, int64_t v_ld, const void* o, int64_t o_ld, const float* lse,
+                    const void* d_o, int64_t do_ld, void* dq, int64_t dq_ld, void* dk, int64_t dk_ld, void* dv,
+                    int64_t dv_ld, l4d_arena* arena, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * LM-head cross-entropy without stored logits
+ *
+ * Forward and backward of the loss of lm_head_xent for any number of tokens and
+ * any vocabulary, in workspace that does not grow with n x v: the forward keeps
+ * one (maximum, sum) pair per token and block of columns, the backward forms the
+ * logits again, a piece of the vocabulary at a time.
+ *   z = hidden W_lm^T (fp32);  lse_i = log sum_j exp z_ij, combined with
+ *   peer_lse_i when given;  loss_i = lse_i - z_i[target], 0 where target < 0
+ *   (an ignored token: a document's last one, padding).
+ *   G_ij = w_i (exp(z_ij - lse_i) - [j = target]), w_i = d_loss[i] (1 without a
+ *   d_loss) x grad_scale, 0 for ignored tokens;
+ *   d_hidden = G W_lm (bf16, overwritten);  d_w_lm += G^T hidden (f32).
+ *   hidden: bf16 [N][h];  w_lm: bf16 [v_t][h], rows [vocab_start, +v_t) of the head;
+ *   targets: int64 [N] device array, any negative value = ignored;
+ *   peer_lse, peer_target_logit: f32 [N], NULL iff t == 1, as in lm_head_xent;
+ *   loss, lse: f32 [N];  target_logit: f32 [N] or NULL: this shard's z_i[target],
+ *   -infinity where the target lies in no row of the shard.  Without peers lse and
+ *   target_logit are what the other ranks of a vocabulary-parallel head need;
+ *   lse of the backward: f32 [N], over the whole vocabulary.
+ * With peers NULL, a target >= vocab_start + v_t or below vocab_start counts as
+ * logit -infinity (loss +infinity).
+ * In G the fp32 value is kept as two bf16 parts for d_w_lm (relative error 2^-17)
+ * and rounded to one for d_hidden.
+ * Requirements: h % 8 == 0, h <= 8192, hidden, w_lm and d_hidden 16-byte aligned;
+ * finite hidden rows also
+ * of ignored tokens (their zero weights multiply them); any N from 0 to 2^29 and v_t from 1 to 2^30 with N x v_t <= 2^40.  N == 0 launches
+ * nothing.
+ * ---------------------------------------------------------------------- */
+int l4d_lm_loss_workspace_bytes(int64_t n_tokens, int64_t hidden, int64_t vocab_shard, uint64_t* fwd_bytes,
+                                uint64_t* bwd_bytes);
+int lm_loss_fwd(int64_t n_tokens, int64_t hidden, int64_t vocab_shard, int64_t vocab_start, const void* hidden_states,
+                const void* w_lm, const int64_t* targets, const float* peer_lse, const float* peer_target_logit,
+                float* loss, float* lse, float* target_logit, l4d_arena* arena, void* hip_stream);
+int lm_loss_bwd(int64_t n_tokens, int64_t hidden, int64_t vocab_shard, int64_t vocab_start, const void* hidden_states,
+                const void* w_lm, const int64_t* targets, const float* lse, const float* d_loss, float grad_scale,
+                void* d_hidden, float* d_w_lm, l4d_arena* arena, void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * Optimizer step over one shard of the model states (Sec. 3.1, Eqs. 4-5, 10)
  *
  * Each GPU holds 2 bytes (bf16 weight) and 4 bytes (fp32 gradient) per

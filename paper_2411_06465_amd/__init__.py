@@ -67,6 +67,23 @@ class Adam(C.Structure):
                 ("step", C.c_int64), ("zero_grad", C.c_int32)]
 
 
+class PackingC(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("n_seqs", C.c_int64), ("starts", C.c_void_p)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("head_dim", C.c_int64), ("rot_dim", C.c_int64), ("layout", C.c_int32), ("scaling", C.c_int32)] + \
+               [(n, C.c_double) for n in ("base", "factor", "low", "high", "original", "amplitude")]
+
+
+class RopeHeads(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("heads", C.c_int64), ("x_ld", C.c_int64), ("y_ld", C.c_int64)]
+
+
+class Attn(C.Structure):
+    _fields_ = [("n_heads", C.c_int64), ("n_kv_heads", C.c_int64), ("head_dim", C.c_int64), ("scale", C.c_float)]
+
+
 _lib = None
 
 
@@ -105,6 +122,17 @@ def lib():
                             C.c_int),
             "lm_head_bwd": ([C.POINTER(Model), C.POINTER(Parallel), P, P, P, P, P, P, f32, P, P, P, P, P, P],
                             C.c_int),
+            "rope_fwd": ([C.POINTER(Rope), C.c_int, i64, C.POINTER(PackingC), P, C.POINTER(RopeHeads),
+                          C.POINTER(RopeHeads), P], C.c_int),
+            "rope_bwd": ([C.POINTER(Rope), C.c_int, i64, C.POINTER(PackingC), P, C.POINTER(RopeHeads),
+                          C.POINTER(RopeHeads), P], C.c_int),
+            "attn_packed_fwd": ([C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64, P, P], C.c_int),
+            "attn_packed_bwd": ([C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64, P, P, i64,
+                                 P, i64, P, i64, P, i64, P, P], C.c_int),
+            "l4d_attn_packed_workspace_bytes": ([C.POINTER(Attn), i64, C.POINTER(u64)], C.c_int),
+            "l4d_lm_loss_workspace_bytes": ([i64, i64, i64, C.POINTER(u64), C.POINTER(u64)], C.c_int),
+            "lm_loss_fwd": ([i64, i64, i64, i64, P, P, P, P, P, P, P, P, P, P], C.c_int),
+            "lm_loss_bwd": ([i64, i64, i64, i64, P, P, P, P, P, f32, P, P, P, P], C.c_int),
             "l4d_profile_enable": ([C.c_int], C.c_int),
             "l4d_profile_only": ([C.c_char_p], C.c_int),
             "l4d_profile_read": ([C.c_char_p, C.POINTER(i64), C.POINTER(C.c_double)], C.c_int),
@@ -317,6 +345,206 @@ def lm_head_bwd(model, par, w_norm, w_lm, targets, stash, dx, d_w_norm, d_w_lm, 
                              _ptr(peer_dxn), _ptr(dxn_send), grad_scale, stash.h, _ptr(dx), _ptr(d_w_norm),
                              _ptr(d_w_lm), arena.h, _stream(stream)))
     stash.h = None
+
+
+# ------------------------------------------------------------------ packed documents
+
+def _on(tensor, stream):
+    """The stream to launch on (default: the current one of the tensor's GPU) and that GPU as the current one."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(tensor.device)
+    if stream.device != tensor.device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {tensor.device}")
+    return torch.cuda.device(tensor.device), C.c_void_p(stream.cuda_stream)
+
+
+def _want(name, t, dtype, shape=None, like=None):
+    """Refuse a tensor that the C entry point would read as something else."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    return t
+
+
+def _flat(name, t, dtype, shape, like):
+    _want(name, t, dtype, shape, like)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _rows(name, t, dtype, like, shape=None):
+    """Row stride of a [tokens][heads][head_dim] tensor whose heads are contiguous within a row."""
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens][heads][head_dim]")
+    _want(name, t, dtype, shape, like)
+    n, heads, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"the heads of {name} must be contiguous within a row")
+    if n > 1 and t.stride(0) < heads * d:
+        raise ValueError(f"the rows of {name} overlap")
+    return t.stride(0) if n > 1 else heads * d
+
+
+class Packing:
+    """Documents one behind another in `tokens` rows: document i holds rows
+    [starts[i], starts[i + 1]); starts is an int64 tensor on the GPU, kept alive here."""
+
+    def __init__(self, starts, tokens):
+        import torch
+        if starts.dim() != 1 or starts.numel() < 1 or not starts.is_contiguous():
+            raise ValueError("starts must be a contiguous vector of n_seqs + 1 rows")
+        self.starts = _want("starts", starts, torch.int64)
+        self.tokens = tokens
+        self.c = PackingC(tokens, starts.numel() - 1, starts.data_ptr())
+
+
+def make_packing(starts, tokens):
+    return Packing(starts, tokens)
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "bands": 2, "ramp": 3}
+
+
+def make_rope(head_dim, rot_dim=None, layout="half", base=1e4, scaling="none", factor=1.0, low=1.0, high=4.0,
+              original=8192, amplitude=1.0):
+    """Rotary positions of heads of head_dim whose first rot_dim elements (default: all) turn."""
+    return Rope(head_dim, head_dim if rot_dim is None else rot_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], base,
+                factor, low, high, original, amplitude)
+
+
+def _rope(entry, rope, q, q_out, k, k_out, positions, packing, stream):
+    import torch
+    dtype = {torch.bfloat16: 0, torch.float32: 1}.get(q.dtype)
+    if dtype is None:
+        raise TypeError(f"q must be bfloat16 or float32, not {q.dtype}")
+    tokens, io = q.shape[0], []
+    for name, x, y in (("q", q, q_out), ("k", k, k_out)):
+        if x is None:
+            io.append(None)
+            continue
+        y = x if y is None else y
+        x_ld, y_ld = _rows(name, x, q.dtype, q), _rows(name + "_out", y, q.dtype, q, x.shape)
+        if x.shape[0] != tokens or x.shape[2] != rope.head_dim:
+            raise ValueError(f"{name} must be [{tokens}][heads][{rope.head_dim}]")
+        io.append(RopeHeads(x.data_ptr(), y.data_ptr(), x.shape[1], x_ld, y_ld))
+    if positions is not None:
+        _flat("positions", positions, torch.int64, (tokens,), q)
+    if packing is not None:
+        _want("starts", packing.starts, torch.int64, like=q)
+    device, s = _on(q, stream)
+    with device:
+        _check(entry(C.byref(rope), dtype, tokens, None if packing is None else C.byref(packing.c), _ptr(positions),
+                     C.byref(io[0]), None if io[1] is None else C.byref(io[1]), s))
+
+
+def rope_fwd(rope, q, q_out=None, k=None, k_out=None, positions=None, packing=None, stream=None):
+    """Rotate q (and k), [tokens][heads][head_dim], into q_out (k_out); in place without an output."""
+    _rope(lib().rope_fwd, rope, q, q_out, k, k_out, positions, packing, stream)
+
+
+def rope_bwd(rope, dq, dq_out=None, dk=None, dk_out=None, positions=None, packing=None, stream=None):
+    """The gradient with respect to rope_fwd's inputs from that of its outputs."""
+    _rope(lib().rope_bwd, rope, dq, dq_out, dk, dk_out, positions, packing, stream)
+
+
+def _attn_args(packing, q, tensors):
+    """Checks of a call's tensors [(name, tensor, shape)] -> [pointer, row stride, ..]."""
+    import torch
+    args = []
+    for name, t, shape in tensors:
+        args += [_ptr(t), _rows(name, t, torch.bfloat16, q, shape)]
+    _want("starts", packing.starts, torch.int64, like=q)
+    return args
+
+
+def attn_packed_fwd(q, k, v, o, lse, packing, scale=0.0, stream=None):
+    """Causal attention within the packing's documents.  q, o [tokens][heads][d], k, v
+    [tokens][kv_heads][d] bf16; lse f32 [heads][tokens].  scale 0 = 1/sqrt(d)."""
+    import torch
+    n, (a, d), g = packing.tokens, q.shape[1:], k.shape[1]
+    args = _attn_args(packing, q, [("q", q, (n, a, d)), ("k", k, (n, g, d)), ("v", v, (n, g, d)),
+                                      ("o", o, (n, a, d))])
+    _flat("lse", lse, torch.float32, (a, n), q)
+    device, s = _on(q, stream)
+    with device:
+        _check(lib().attn_packed_fwd(C.byref(Attn(a, g, d, scale)), C.byref(packing.c), *args, _ptr(lse), s))
+
+
+def l4d_attn_packed_workspace_bytes(tokens, n_heads, n_kv_heads, head_dim):
+    b = C.c_uint64()
+    _check(lib().l4d_attn_packed_workspace_bytes(C.byref(Attn(n_heads, n_kv_heads, head_dim, 0.0)), tokens, C.byref(b)))
+    return b.value
+
+
+def attn_packed_bwd(q, k, v, o, lse, d_o, dq, dk, dv, packing, arena, scale=0.0, stream=None):
+    """Gradients of attn_packed_fwd, overwriting dq, dk and dv."""
+    import torch
+    n, (a, d), g = packing.tokens, q.shape[1:], k.shape[1]
+    qs, ks = (n, a, d), (n, g, d)
+    args = _attn_args(packing, q, [("q", q, qs), ("k", k, ks), ("v", v, ks), ("o", o, qs), ("d_o", d_o, qs),
+                                      ("dq", dq, qs), ("dk", dk, ks), ("dv", dv, ks)])
+    _flat("lse", lse, torch.float32, (a, n), q)
+    device, s = _on(q, stream)
+    with device:
+        _check(lib().attn_packed_bwd(C.byref(Attn(a, g, d, scale)), C.byref(packing.c), *args[:8], _ptr(lse), *args[8:],
+                                     arena.h, s))
+
+
+# ------------------------------------------------------------------ loss without stored logits
+
+def l4d_lm_loss_workspace_bytes(n, h, v_t):
+    """(forward, backward) arena bytes."""
+    f, b = C.c_uint64(), C.c_uint64()
+    _check(lib().l4d_lm_loss_workspace_bytes(n, h, v_t, C.byref(f), C.byref(b)))
+    return f.value, b.value
+
+
+def _loss_args(hidden, w_lm, targets):
+    import torch
+    if hidden.dim() != 2 or w_lm.dim() != 2:
+        raise ValueError("hidden must be [tokens][h], w_lm [vocab][h]")
+    (n, h), v_t = hidden.shape, w_lm.shape[0]
+    _flat("hidden", hidden, torch.bfloat16, (n, h), hidden)
+    _flat("w_lm", w_lm, torch.bfloat16, (v_t, h), hidden)
+    _flat("targets", targets, torch.int64, (n,), hidden)
+    return n, h, v_t
+
+
+def lm_loss_fwd(hidden, w_lm, targets, loss, lse, arena, vocab_start=0, peer_lse=None, peer_target_logit=None,
+                target_logit=None, stream=None):
+    """Cross-entropy of every token (0 where the target is negative) and its log-sum-exp, without stored logits."""
+    import torch
+    n, h, v_t = _loss_args(hidden, w_lm, targets)
+    for name, t in (("loss", loss), ("lse", lse), ("peer_lse", peer_lse), ("peer_target_logit", peer_target_logit),
+                    ("target_logit", target_logit)):
+        if t is not None:
+            _flat(name, t, torch.float32, (n,), hidden)
+    device, s = _on(hidden, stream)
+    with device:
+        _check(lib().lm_loss_fwd(n, h, v_t, vocab_start, _ptr(hidden), _ptr(w_lm), _ptr(targets), _ptr(peer_lse),
+                                 _ptr(peer_target_logit), _ptr(loss), _ptr(lse), _ptr(target_logit), arena.h, s))
+
+
+def lm_loss_bwd(hidden, w_lm, targets, lse, d_hidden, d_w_lm, arena, d_loss=None, grad_scale=1.0, vocab_start=0,
+                stream=None):
+    """Gradients of lm_loss_fwd's losses weighted by d_loss * grad_scale: d_hidden overwritten, d_w_lm added to."""
+    import torch
+    n, h, v_t = _loss_args(hidden, w_lm, targets)
+    _flat("lse", lse, torch.float32, (n,), hidden)
+    _flat("d_hidden", d_hidden, torch.bfloat16, (n, h), hidden)
+    _flat("d_w_lm", d_w_lm, torch.float32, (v_t, h), hidden)
+    if d_loss is not None:
+        _flat("d_loss", d_loss, torch.float32, (n,), hidden)
+    device, s = _on(hidden, stream)
+    with device:
+        _check(lib().lm_loss_bwd(n, h, v_t, vocab_start, _ptr(hidden), _ptr(w_lm), _ptr(targets), _ptr(lse),
+                                 _ptr(d_loss), grad_scale, _ptr(d_hidden), _ptr(d_w_lm), arena.h, s))
 
 
 # ------------------------------------------------------------------ optimizer step

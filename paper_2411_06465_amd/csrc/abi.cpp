@@ -8,6 +8,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <set>
@@ -1297,6 +1298,366 @@ extern "C" int lm_head_bwd(const l4d_model* m, const l4d_parallel* p, const void
                      op(gathered(sptr(st, L4D_HEAD_XN), peer_xn, x), x.h), Layout::MN, epi_acc(d_w_lm, x.h))))
     return rc;
   return l4d_stash_release(A, st);
+}
+
+// ============================================================== packed documents
+
+namespace {
+int check_packing(const l4d_packing* pk) {
+  if (!pk) return fail(L4D_EINVAL, "packing is required");
+  if (pk->tokens < 0 || pk->tokens > (int64_t)1 << 30 || pk->n_seqs < 0 || pk->n_seqs > (int64_t)1 << 30)
+    return fail(L4D_EINVAL, "packing: tokens and n_seqs must lie in 0 .. 2^30");
+  if (pk->n_seqs > 0 && !pk->starts) return fail(L4D_EINVAL, "packing: starts is required");
+  if (reinterpret_cast<uintptr_t>(pk->starts) % 8) return fail(L4D_EINVAL, "packing: starts must be 8-byte aligned");
+  return L4D_OK;
+}
+Packing device_packing(const l4d_packing* pk) {
+  return Packing{pk->starts, (int32_t)pk->n_seqs, (int32_t)pk->tokens};
+}
+
+// ------------------------------------------------------------ rotary positions
+
+// f_j / 2 pi of every pair, in double.
+int rope_turns(const l4d_rope* r, double* turns) {
+  constexpr double kTwoPi = 6.283185307179586476925286766559;
+  if (r->head_dim < 2 || r->head_dim > 2 * kMaxRopePairs) return fail(L4D_EINVAL, "rope: head_dim must lie in 2 .. 512");
+  if (r->rot_dim < 2 || r->rot_dim > r->head_dim || r->rot_dim % 2)
+    return fail(L4D_EINVAL, "rope: rot_dim must be even and lie in 2 .. head_dim");
+  if (r->layout != L4D_ROPE_HALF && r->layout != L4D_ROPE_INTERLEAVED) return fail(L4D_EINVAL, "rope: unknown layout");
+  if (r->scaling < L4D_ROPE_PLAIN || r->scaling > L4D_ROPE_RAMP) return fail(L4D_EINVAL, "rope: unknown scaling");
+  if (!(r->base > 1.0) || !std::isfinite(r->base)) return fail(L4D_EINVAL, "rope: base must be finite and above 1");
+  if (!(r->amplitude > 0.0) || !std::isfinite((float)r->amplitude))
+    return fail(L4D_EINVAL, "rope: the amplitude must be finite and positive");
+  const bool scaled = r->scaling != L4D_ROPE_PLAIN, bands = r->scaling == L4D_ROPE_BANDS || r->scaling == L4D_ROPE_RAMP;
+  if (scaled && (!(r->factor > 0.0) || !std::isfinite(r->factor)))
+    return fail(L4D_EINVAL, "rope: factor must be finite and positive");
+  if (bands && (!(r->original > 0.0) || !std::isfinite(r->original) || !(r->low > 0.0) || !(r->high > r->low) ||
+                !std::isfinite(r->high)))
+    return fail(L4D_EINVAL, "rope: need original > 0 and 0 < low < high");
+  const double rot = (double)r->rot_dim, log_base = std::log(r->base);
+  double j0 = 0.0, j1 = 0.0;
+  if (r->scaling == L4D_ROPE_RAMP) {
+    // the pair that makes `t` turns over the original context: base^(-2j/rot) original = 2 pi t
+    const auto pair_of = [&](double t) { return rot * std::log(r->original / (kTwoPi * t)) / (2.0 * log_base); };
+    j0 = std::max(std::floor(pair_of(r->high)), 0.0);
+    j1 = std::min(std::ceil(pair_of(r->low)), rot - 1.0);
+  }
+  for (int64_t j = 0; j < r->rot_dim / 2; ++j) {
+    const double f = std::exp(-2.0 * (double)j / rot * log_base);
+    double keep = 1.0;                       // g_j
+    if (r->scaling == L4D_ROPE_LINEAR) keep = 0.0;
+    else if (r->scaling == L4D_ROPE_BANDS) keep = (r->original * f / kTwoPi - r->low) / (r->high - r->low);
+    else if (r->scaling == L4D_ROPE_RAMP) keep = 1.0 - std::min(std::max(((double)j - j0) / (j1 > j0 ? j1 - j0 : 0.001), 0.0), 1.0);
+    keep = std::min(std::max(keep, 0.0), 1.0);
+    turns[j] = (scaled ? f * ((1.0 - keep) / r->factor + keep) : f) / kTwoPi;
+  }
+  return L4D_OK;
+}
+
+int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk,
+              const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, int inverse, void* stream_ptr) {
+  if (!r || !q) return fail(L4D_EINVAL, "rope and q are required");
+  if (dtype != L4D_BF16 && dtype != L4D_F32) return fail(L4D_EINVAL, "rope: unknown dtype");
+  if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "rope: tokens must lie in 0 .. 2^30");
+  int rc;
+  if (pk && (rc = check_packing(pk))) return rc;
+  if (pk && pk->tokens != tokens) return fail(L4D_EINVAL, "rope: the packing is of another number of tokens");
+  if (reinterpret_cast<uintptr_t>(positions) % 8) return fail(L4D_EINVAL, "rope: positions must be 8-byte aligned");
+  RopeRotate a{};
+  if ((rc = rope_turns(r, a.turns))) return rc;
+  const int64_t size = dtype == L4D_F32 ? 4 : 2;
+  const l4d_rope_heads* in[2] = {q, k};
+  for (const l4d_rope_heads* t : in) {
+    if (!t) continue;
+    if (!t->x || !t->y) return fail(L4D_EINVAL, "rope: a tensor is NULL");
+    if (t->heads < 1 || t->heads > (int64_t)1 << 16) return fail(L4D_EINVAL, "rope: heads must lie in 1 .. 2^16");
+    const int64_t cols = t->heads * r->head_dim;
+    if (t->x_ld < cols || t->y_ld < cols || t->x_ld > (int64_t)1 << 31 || t->y_ld > (int64_t)1 << 31)
+      return fail(L4D_EINVAL, "rope: a row stride is shorter than the heads, or above 2^31");
+    const uintptr_t x = reinterpret_cast<uintptr_t>(t->x), y = reinterpret_cast<uintptr_t>(t->y);
+    if (x % size || y % size) return fail(L4D_EINVAL, "rope: a tensor is misaligned");
+    const uint64_t nx = tokens ? ((uint64_t)(tokens - 1) * t->x_ld + cols) * size : 0;
+    const uint64_t ny = tokens ? ((uint64_t)(tokens - 1) * t->y_ld + cols) * size : 0;
+    if (!(x == y && t->x_ld == t->y_ld) && x < y + ny && y < x + nx)
+      return fail(L4D_EINVAL, "rope: input and output overlap");
+    a.t[a.n_tensors++] = RopeHeads{t->x, t->y, t->x_ld, t->y_ld, (int32_t)t->heads};
+  }
+  if (tokens == 0 || (pk && pk->n_seqs == 0)) return L4D_OK;
+  a.pk = pk ? device_packing(pk) : Packing{nullptr, -1, (int32_t)tokens};
+  a.positions = positions;
+  a.tokens = (int32_t)tokens;
+  a.d_h = (int32_t)r->head_dim;
+  a.rot = (int32_t)r->rot_dim;
+  a.f32 = dtype == L4D_F32;
+  a.interleaved = r->layout == L4D_ROPE_INTERLEAVED;
+  a.inverse = inverse;
+  a.amplitude = (float)r->amplitude;
+  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
+  return launch(name, s, [&] { return rope_rotate(a, s); });
+}
+}  // namespace
+
+extern "C" int rope_fwd(const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk, const int64_t* positions,
+                        const l4d_rope_heads* q, const l4d_rope_heads* k, void* stream_ptr) {
+  return rope_call("rope_fwd", r, dtype, tokens, pk, positions, q, k, 0, stream_ptr);
+}
+
+extern "C" int rope_bwd(const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk, const int64_t* positions,
+                        const l4d_rope_heads* q, const l4d_rope_heads* k, void* stream_ptr) {
+  return rope_call("rope_bwd", r, dtype, tokens, pk, positions, q, k, 1, stream_ptr);
+}
+
+// ------------------------------------------------------------ packed attention
+
+namespace {
+struct AttnRows {        // one tensor of a call
+  const char* name;
+  const void* p;
+  int64_t ld, heads;
+};
+int attn_shape(const l4d_attn* at, int64_t tokens, PackedAttn* p) {
+  if (!at) return fail(L4D_EINVAL, "attn is required");
+  if (at->head_dim != 64 && at->head_dim != 128)
+    return fail(L4D_EINVAL, "head dim %lld unsupported (64 or 128)", (long long)at->head_dim);
+  if (at->n_heads < 1 || at->n_heads > (int64_t)1 << 16 || at->n_kv_heads < 1 || at->n_heads % at->n_kv_heads)
+    return fail(L4D_EINVAL, "n_heads must lie in 1 .. 2^16 and be a multiple of n_kv_heads");
+  if (!(at->scale >= 0.f) || !std::isfinite(at->scale)) return fail(L4D_EINVAL, "the scale must be finite and >= 0");
+  p->heads = (int32_t)at->n_heads;
+  p->kv_heads = (int32_t)at->n_kv_heads;
+  p->d_h = (int32_t)at->head_dim;
+  p->scale = at->scale > 0.f ? at->scale : 1.0f / std::sqrt((float)at->head_dim);
+  p->n_split = attn_packed_splits(tokens, at->n_heads, at->n_kv_heads);
+  return L4D_OK;
+}
+int attn_rows(const AttnRows* t, int n, int64_t d) {
+  for (int i = 0; i < n; ++i) {
+    if (!t[i].p) return fail(L4D_EINVAL, "%s is required", t[i].name);
+    if (reinterpret_cast<uintptr_t>(t[i].p) % 16) return fail(L4D_EINVAL, "%s must be 16-byte aligned", t[i].name);
+    if (t[i].ld < t[i].heads * d || t[i].ld % 8 || t[i].ld > (int64_t)1 << 22)
+      return fail(L4D_EINVAL, "the row stride of %s must cover its heads, be a multiple of 8 and at most 2^22", t[i].name);
+  }
+  return L4D_OK;
+}
+// No output may start where another tensor does.
+int attn_distinct(const AttnRows* t, int n, int first_out) {
+  for (int i = first_out; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if (t[i].p == t[j].p) return fail(L4D_EINVAL, "%s and %s are the same array", t[i].name, t[j].name);
+  return L4D_OK;
+}
+struct PackedWs {
+  uint64_t delta, partial, total;
+};
+PackedWs plan_packed(const PackedAttn& p, int64_t tokens) {
+  Carver cv;
+  PackedWs w{};
+  w.delta = cv.take((uint64_t)p.heads * tokens * 4);
+  w.partial = p.n_split > 1 ? cv.take(2ull * p.n_split * tokens * p.kv_heads * p.d_h * 4) : 0;
+  w.total = cv.used;
+  return w;
+}
+}  // namespace
+
+extern "C" int l4d_attn_packed_workspace_bytes(const l4d_attn* at, int64_t tokens, uint64_t* bytes) {
+  if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "tokens must lie in 0 .. 2^30");
+  PackedAttn p{};
+  int rc = attn_shape(at, tokens, &p);
+  if (rc) return rc;
+  if (bytes) *bytes = align_up(plan_packed(p, tokens).total);
+  return L4D_OK;
+}
+
+extern "C" int attn_packed_fwd(const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld, const void* k,
+                               int64_t k_ld, const void* v, int64_t v_ld, void* o, int64_t o_ld, float* lse,
+                               void* stream_ptr) {
+  int rc = check_packing(pk);
+  if (rc) return rc;
+  PackedAttn p{};
+  if ((rc = attn_shape(at, pk->tokens, &p))) return rc;
+  const AttnRows t[4] = {{"q", q, q_ld, at->n_heads}, {"k", k, k_ld, at->n_kv_heads}, {"v", v, v_ld, at->n_kv_heads},
+                         {"o", o, o_ld, at->n_heads}};
+  if ((rc = attn_rows(t, 4, at->head_dim)) || (rc = attn_distinct(t, 4, 3))) return rc;
+  if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return fail(L4D_EINVAL, "lse is required, 4-byte aligned");
+  p.pk = device_packing(pk);
+  if (!attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
+  if (pk->tokens == 0 || pk->n_seqs == 0) return L4D_OK;
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.o = static_cast<uint16_t*>(o);
+  p.q_ld = q_ld, p.k_ld = k_ld, p.v_ld = v_ld, p.o_ld = o_ld;
+  p.lse = lse;
+  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
+  return launch("attn_packed_fwd", s, [&] { return attn_packed_fwd(p, s); });
+}
+
+extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld, const void* k,
+                               int64_t k_ld, const void* v, int64_t v_ld, const void* o, int64_t o_ld, const float* lse,
+                               const void* d_o, int64_t do_ld, void* dq, int64_t dq_ld, void* dk, int64_t dk_ld, void* dv,
+                               int64_t dv_ld, l4d_arena* A, void* stream_ptr) {
+  int rc = check_packing(pk);
+  if (rc) return rc;
+  PackedAttn p{};
+  if ((rc = attn_shape(at, pk->tokens, &p))) return rc;
+  const int64_t a = at->n_heads, g = at->n_kv_heads;
+  const AttnRows t[8] = {{"q", q, q_ld, a}, {"k", k, k_ld, g}, {"v", v, v_ld, g}, {"o", o, o_ld, a},
+                         {"d_o", d_o, do_ld, a}, {"dq", dq, dq_ld, a}, {"dk", dk, dk_ld, g}, {"dv", dv, dv_ld, g}};
+  if ((rc = attn_rows(t, 8, at->head_dim)) || (rc = attn_distinct(t, 8, 5))) return rc;
+  if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return fail(L4D_EINVAL, "lse is required, 4-byte aligned");
+  if (!A) return fail(L4D_EINVAL, "arena is required");
+  p.pk = device_packing(pk);
+  if (!attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
+  if (pk->tokens == 0 || pk->n_seqs == 0) return L4D_OK;
+  const PackedWs plan = plan_packed(p, pk->tokens);
+  Workspace ws;
+  if ((rc = take_ws(A, plan.total, ws))) return rc;
+  uint8_t* wsb = reinterpret_cast<uint8_t*>(A->base + ws.off);
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.o = static_cast<uint16_t*>(const_cast<void*>(o));
+  p.lse = const_cast<float*>(lse);
+  p.dout = static_cast<const uint16_t*>(d_o);
+  p.dq = static_cast<uint16_t*>(dq);
+  p.dk = static_cast<uint16_t*>(dk);
+  p.dv = static_cast<uint16_t*>(dv);
+  p.q_ld = q_ld, p.k_ld = k_ld, p.v_ld = v_ld, p.o_ld = o_ld, p.do_ld = do_ld;
+  p.dq_ld = dq_ld, p.dk_ld = dk_ld, p.dv_ld = dv_ld;
+  p.delta = reinterpret_cast<float*>(wsb + plan.delta);
+  p.dkv_partial = reinterpret_cast<float*>(wsb + plan.partial);
+  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
+  // dQ first: it also writes delta, which dK/dV reads
+  if ((rc = launch("attn_packed_dq", s, [&] { return attn_packed_bwd(p, 2, s); }))) return rc;
+  if ((rc = launch("attn_packed_dkdv", s, [&] { return attn_packed_bwd(p, 1, s); }))) return rc;
+  if (p.n_split > 1) return launch("attn_packed_reduce", s, [&] { return attn_packed_bwd(p, 3, s); });
+  return L4D_OK;
+}
+
+// ============================================================== loss without stored logits
+
+namespace {
+// Columns of a piece of the vocabulary.
+int64_t loss_piece_cols(int64_t n, int64_t v_t) {
+  const int64_t cols = std::max<int64_t>(4096, (((int64_t)1 << 26) / std::max<int64_t>(n, 1)) / 256 * 256);
+  return std::min(cols, (v_t + 7) / 8 * 8);
+}
+struct LossWs {
+  int64_t piece;                                     // columns, the row length of the piece's arrays
+  uint64_t stats, zt, z, g_hi, dh, fwd, bwd;
+};
+LossWs plan_loss(int64_t n, int64_t h, int64_t v_t) {
+  LossWs w{};
+  w.piece = loss_piece_cols(n, v_t);
+  Carver f, b;
+  w.z = f.take((uint64_t)n * w.piece * 4);
+  w.stats = f.take((uint64_t)n * 8);
+  w.zt = f.take((uint64_t)n * 4);
+  w.fwd = f.used;
+  b.take((uint64_t)n * w.piece * 4);
+  w.g_hi = b.take((uint64_t)n * w.piece * 4);        // the high parts [n][piece], then the low ones
+  w.dh = b.take((uint64_t)n * h * 4);
+  w.bwd = b.used;
+  return w;
+}
+// rows: arrays of bf16 rows; words: the others, which need no more than their element's alignment (4 or 8 bytes)
+int loss_check(int64_t n, int64_t h, int64_t v_t, int64_t v0, std::initializer_list<const void*> rows,
+               std::initializer_list<const void*> words, const int64_t* targets) {
+  if (n < 0 || h <= 0 || v_t <= 0 || v0 < 0) return fail(L4D_EINVAL, "bad LM-head sizes");
+  if (h % 8 || h > 8192) return fail(L4D_EINVAL, "hidden must be a multiple of 8 and at most 8192");
+  if (n > (int64_t)1 << 29 || v_t > (int64_t)1 << 30 || n * v_t > (int64_t)1 << 40) return fail(L4D_EINVAL, "problem too large");
+  for (const void* p : rows)
+    if (!p || reinterpret_cast<uintptr_t>(p) % 16)
+      return fail(L4D_EINVAL, "hidden, w_lm and d_hidden are required, 16-byte aligned");
+  for (const void* p : words)
+    if (!p || reinterpret_cast<uintptr_t>(p) % 4) return fail(L4D_EINVAL, "loss, lse and d_w_lm are required, 4-byte aligned");
+  if (words.size() && (!targets || reinterpret_cast<uintptr_t>(targets) % 8))
+    return fail(L4D_EINVAL, "targets is required, 8-byte aligned");
+  return L4D_OK;
+}
+// z (f32 [n][ld]) = the logits of columns [c0, c0 + cols) of the shard
+int loss_logits(const char* name, int64_t n, int64_t h, const void* hidden, const void* w_lm, int64_t c0, int64_t cols,
+                float* z, int64_t ld, hipStream_t s) {
+  EpiParams e{};
+  e.kind = EpiKind::StoreF32;
+  e.c = z;
+  e.ldc = ld;
+  return run_gemm(name, s, n, cols, h, op(RowSrc::plain(hidden, h), n), Layout::KC,
+                  op(RowSrc::plain(static_cast<const uint16_t*>(w_lm) + c0 * h, h), cols), Layout::KC, e);
+}
+}  // namespace
+
+extern "C" int l4d_lm_loss_workspace_bytes(int64_t n, int64_t h, int64_t v_t, uint64_t* fwd, uint64_t* bwd) {
+  int rc = loss_check(n, h, v_t, 0, {}, {}, nullptr);
+  if (rc) return rc;
+  const LossWs w = plan_loss(n, h, v_t);
+  if (fwd) *fwd = align_up(w.fwd);
+  if (bwd) *bwd = align_up(w.bwd);
+  return L4D_OK;
+}
+
+extern "C" int lm_loss_fwd(int64_t n, int64_t h, int64_t v_t, int64_t v0, const void* hidden, const void* w_lm,
+                           const int64_t* targets, const float* peer_lse, const float* peer_z, float* loss, float* lse,
+                           float* target_logit, l4d_arena* A, void* stream_ptr) {
+  int rc = loss_check(n, h, v_t, v0, {hidden, w_lm}, {loss, lse}, targets);
+  if (rc) return rc;
+  if ((peer_lse == nullptr) != (peer_z == nullptr)) return fail(L4D_EINVAL, "peer_lse and peer_target_logit go together");
+  if (!A) return fail(L4D_EINVAL, "arena is required");
+  if (n == 0) return L4D_OK;
+  const LossWs plan = plan_loss(n, h, v_t);
+  Workspace ws;
+  if ((rc = take_ws(A, plan.fwd, ws))) return rc;
+  uint8_t* wsb = reinterpret_cast<uint8_t*>(A->base + ws.off);
+  float *z = reinterpret_cast<float*>(wsb + plan.z), *zt = reinterpret_cast<float*>(wsb + plan.zt);
+  float2* stats = reinterpret_cast<float2*>(wsb + plan.stats);
+  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
+  for (int64_t c0 = 0; c0 < v_t; c0 += plan.piece) {
+    const int64_t cols = std::min(plan.piece, v_t - c0);
+    if ((rc = loss_logits("gemm_loss_logits", n, h, hidden, w_lm, c0, cols, z, plan.piece, s))) return rc;
+    if ((rc = launch("loss_piece", s, [&] {
+           return loss_piece(z, plan.piece, n, (int32_t)cols, v0 + c0, targets, stats, zt, c0 == 0, s);
+         })))
+      return rc;
+  }
+  return launch("loss_finish", s, [&] {
+    return loss_finish(stats, zt, n, targets, peer_lse, peer_z, loss, lse, target_logit, s);
+  });
+}
+
+extern "C" int lm_loss_bwd(int64_t n, int64_t h, int64_t v_t, int64_t v0, const void* hidden, const void* w_lm,
+                           const int64_t* targets, const float* lse, const float* d_loss, float grad_scale,
+                           void* d_hidden, float* d_w, l4d_arena* A, void* stream_ptr) {
+  int rc = loss_check(n, h, v_t, v0, {hidden, w_lm, d_hidden}, {lse, d_w}, targets);
+  if (rc) return rc;
+  if (!std::isfinite(grad_scale)) return fail(L4D_EINVAL, "grad_scale must be finite");
+  if (!A) return fail(L4D_EINVAL, "arena is required");
+  if (n == 0) return L4D_OK;
+  const LossWs plan = plan_loss(n, h, v_t);
+  Workspace ws;
+  if ((rc = take_ws(A, plan.bwd, ws))) return rc;
+  uint8_t* wsb = reinterpret_cast<uint8_t*>(A->base + ws.off);
+  float *z = reinterpret_cast<float*>(wsb + plan.z), *dh = reinterpret_cast<float*>(wsb + plan.dh);
+  uint16_t *g_hi = reinterpret_cast<uint16_t*>(wsb + plan.g_hi), *g_lo = g_hi + n * plan.piece;
+  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
+  // the products of G^T hidden run over 2 n rows: the high parts of G, then the low ones, against hidden twice
+  const RowSrc twice{static_cast<const uint16_t*>(hidden), static_cast<const uint16_t*>(hidden), h, (int32_t)(2 * n),
+                     (int32_t)n, 0, 2};
+  if ((rc = launch("zero_dh", s, [&] { return zero_f32(dh, n * h, s); }))) return rc;
+  for (int64_t c0 = 0; c0 < v_t; c0 += plan.piece) {
+    const int64_t cols = std::min(plan.piece, v_t - c0), ld = plan.piece;
+    const uint16_t* w = static_cast<const uint16_t*>(w_lm) + c0 * h;
+    if ((rc = loss_logits("gemm_loss_logits", n, h, hidden, w_lm, c0, cols, z, ld, s))) return rc;
+    if ((rc = launch("loss_grad", s, [&] {
+           return loss_grad(z, ld, n, (int32_t)cols, v0 + c0, targets, lse, d_loss, grad_scale, g_hi, g_lo, s);
+         })))
+      return rc;
+    if ((rc = run_gemm("gemm_loss_dx", s, n, h, cols, op(RowSrc::plain(g_hi, ld), n), Layout::KC,
+                       op(RowSrc::plain(w, h), h), Layout::MN, epi_acc(dh, h))))
+      return rc;
+    if ((rc = run_gemm("gemm_loss_dw", s, cols, h, 2 * n, op(RowSrc::plain(g_hi, ld), ld), Layout::MN, op(twice, h),
+                       Layout::MN, epi_acc(d_w + c0 * h, h))))
+      return rc;
+  }
+  return launch("round_dh", s, [&] { return round_bf16(dh, static_cast<uint16_t*>(d_hidden), n * h, s); });
 }
 
 // ============================================================== optimizer

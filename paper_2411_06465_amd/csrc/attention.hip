@@ -34,6 +34,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "packing.h"
 
 namespace l4d {
 namespace {
@@ -1093,6 +1094,8 @@ hipError_t bwd_impl(const AttnParams& p, int part, hipStream_t stream) {
   return hipGetLastError();
 }
 
+#include "attention_packed.h"
+
 }  // namespace
 
 int attn_bwd_splits(const AttnParams& p) {
@@ -1121,6 +1124,29 @@ hipError_t attn_bwd(const AttnParams& p, int part, hipStream_t stream) {
   if (p.d_h == 128) return bwd_impl<128>(p, part, stream);
   if (p.d_h == 64) return bwd_impl<64>(p, part, stream);
   return hipErrorInvalidValue;
+}
+
+// The rule of attn_bwd_splits, with the blocks that full documents would give.
+int attn_packed_splits(int64_t tokens, int64_t heads, int64_t kv_heads) {
+  const int64_t group = heads / kv_heads, base = (tokens + 127) / 128 * kv_heads;
+  int n = 1;
+  while (base * n < 512 && n < group && group % (2 * n) == 0) n *= 2;
+  return n;
+}
+
+bool attn_packed_fits(const PackedAttn& p) {
+  // a grid holds less than 2^32 threads; slots of the smallest query blocks (32 rows) and of the key blocks
+  const int64_t q = packed_slots(p, 32) * p.heads, k = packed_slots(p, 128) * p.heads;
+  const int64_t r = static_cast<int64_t>(p.pk.tokens) * p.kv_heads * (p.d_h / 8);
+  return q < (int64_t{1} << 24) && k < (int64_t{1} << 23) && r < (int64_t{1} << 32);
+}
+
+hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream) {
+  return p.d_h == 128 ? packed_launch<128>(p, 0, stream) : packed_launch<64>(p, 0, stream);
+}
+
+hipError_t attn_packed_bwd(PackedAttn p, int part, hipStream_t stream) {
+  return p.d_h == 128 ? packed_launch<128>(p, part, stream) : packed_launch<64>(p, part, stream);
 }
 
 }  // namespace l4d

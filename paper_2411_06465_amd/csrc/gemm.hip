@@ -1300,6 +1300,7 @@ hipError_t gemm(const GemmParams& params, Layout la, Layout lb, hipStream_t stre
     if (k == E::SwiGLUBwd) return launch<L::KC, L::MN, E::SwiGLUBwd, 128>(p, stream);
     if (k == E::ResidualSP) return launch<L::KC, L::MN, E::ResidualSP, 128>(p, stream);
     if (k == E::StoreBF16) return launch<L::KC, L::MN, E::StoreBF16, 128>(p, stream);
+    if (k == E::AccF32) return launch<L::KC, L::MN, E::AccF32, 128>(p, stream);
   } else if (la == L::MN && lb == L::MN) {
     if (k == E::AccF32) return launch<L::MN, L::MN, E::AccF32, 128>(p, stream);
   }

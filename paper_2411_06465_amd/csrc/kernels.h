@@ -227,6 +227,65 @@ hipError_t attn_fwd(const AttnParams& p, hipStream_t stream);
 // 3: the sum of the query-head slices of dK, dV when n_split > 1 (nothing otherwise).
 hipError_t attn_bwd(const AttnParams& p, int part, hipStream_t stream);
 
+// ---------------------------------------------------------------- packed documents
+
+// Document i holds rows [starts[i], starts[i + 1]) of `tokens` rows (device array,
+// clamped where it is read).
+struct Packing {
+  const int64_t* starts;
+  int32_t n_seqs;     // -1: no packing, every row counts
+  int32_t tokens;
+};
+
+// Causal attention within the documents.  Row i of a tensor starts at its
+// pointer + i ld, head h at column h d_h; 16-byte aligned, ld a multiple of 8.
+struct PackedAttn {
+  Packing pk;
+  int32_t heads, kv_heads, d_h;
+  int32_t hpb;              // query heads of one kv head that a query block takes together (1, 2, 4): 128/hpb rows
+  int32_t n_slots;          // blocks of rows per head: see seq_block
+  float scale;
+  const uint16_t *q, *k, *v;
+  int64_t q_ld, k_ld, v_ld;
+  uint16_t* o;              // forward: output, backward: input
+  int64_t o_ld;
+  float* lse;               // [heads][tokens], natural log
+  // backward
+  const uint16_t* dout;
+  int64_t do_ld;
+  uint16_t *dq, *dk, *dv;
+  int64_t dq_ld, dk_ld, dv_ld;
+  float* delta;             // [heads][tokens]: rowsum(dO * O)
+  int32_t n_split;          // slices of a kv head's query heads in the dK/dV pass
+  float* dkv_partial;       // n_split > 1: dK [n_split][tokens][kv_heads][d_h], then dV
+};
+int attn_packed_splits(int64_t tokens, int64_t heads, int64_t kv_heads);
+bool attn_packed_fits(const PackedAttn& p);      // every launch within the grid limits
+hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream);
+// part 2: dQ and delta; 1: dK, dV (after part 2); 3: the sum of the slices (n_split > 1).
+hipError_t attn_packed_bwd(PackedAttn p, int part, hipStream_t stream);
+
+// ---------------------------------------------------------------- rotary positions
+
+constexpr int kMaxRopePairs = 256;
+struct RopeHeads {          // one tensor [tokens][heads][d_h] (element strides)
+  const void* x;
+  void* y;
+  int64_t x_ld, y_ld;
+  int32_t heads;
+};
+struct RopeRotate {
+  Packing pk;
+  const int64_t* positions; // null: the distance from the document's first row
+  RopeHeads t[2];
+  int32_t n_tensors, tokens;
+  int32_t d_h, rot;
+  int32_t f32, interleaved, inverse;
+  float amplitude;
+  double turns[kMaxRopePairs];   // f_j / 2 pi
+};
+hipError_t rope_rotate(const RopeRotate& p, hipStream_t stream);
+
 // ---------------------------------------------------------------- cross-entropy
 
 hipError_t xent_rows(const uint16_t* logits, int64_t n, int32_t v_t, int64_t v0,
@@ -240,6 +299,22 @@ hipError_t xent_probs(float* logits, int64_t n, int32_t v_t, int64_t v0, const i
 // dlogits (bf16 [n][v_t]) = (softmax - onehot(target)) * grad_scale.
 hipError_t xent_grad(const float* probs, int64_t n, int32_t v_t, int64_t v0, const int64_t* targets,
                      float grad_scale, uint16_t* dlogits, hipStream_t stream);
+
+// Loss without stored logits, one piece of n_cols columns (rows of the vocabulary,
+// from v0 on) at a time; z: fp32 logits [n][ld] of the piece.
+// stats[i] = (m, s), the running maximum of row i and the sum of exp(z - m) (first:
+// the row's first piece); zt[i] = the target's logit, -infinity until met.
+hipError_t loss_piece(const float* z, int64_t ld, int64_t n, int32_t n_cols, int64_t v0, const int64_t* targets,
+                      float2* stats, float* zt, bool first, hipStream_t stream);
+hipError_t loss_finish(const float2* stats, const float* zt, int64_t n, const int64_t* targets, const float* peer_lse,
+                       const float* peer_z, float* loss, float* lse, float* target_logit, hipStream_t stream);
+// G = w_i (exp(z - lse) - [target]) as two bf16 parts [n][ld] each, zero in the columns n_cols .. ld - 1.
+hipError_t loss_grad(const float* z, int64_t ld, int64_t n, int32_t n_cols, int64_t v0, const int64_t* targets,
+                     const float* lse, const float* d_loss, float grad_scale, uint16_t* g_hi, uint16_t* g_lo,
+                     hipStream_t stream);
+hipError_t zero_f32(float* x, int64_t n, hipStream_t stream);      // n a multiple of 4
+// y (bf16) = x, n elements (a multiple of 8).
+hipError_t round_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t stream);
 
 // ---------------------------------------------------------------- embedding
 

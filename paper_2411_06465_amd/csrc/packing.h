@@ -1,0 +1,58 @@
+// Packed documents on the device: which document a row, or a block of rows,
+// belongs to.  starts[0 .. n_seqs] is read as it is on every call; values outside
+// [0, tokens] are clamped, so that no access leaves the arrays whatever it holds.
+#pragma once
+#include "kernels.h"
+
+namespace l4d {
+
+__device__ __forceinline__ int seq_start(const Packing& p, int i) {
+  const int64_t v = p.starts[i];
+  return static_cast<int>(v < 0 ? 0 : v > p.tokens ? p.tokens : v);
+}
+
+// The last i in [0, n_seqs) with key(i) <= x, or -1; key is nondecreasing.  The
+// lanes of a wave probe 64 places at once: one load latency up to 64 documents,
+// two up to 4096.  Every lane must call it; the result is the same in all.
+template <class Key>
+__device__ __forceinline__ int last_not_above(int n_seqs, int x, int lane, Key key) {
+  int base = 0, len = n_seqs, found = -1;
+  while (len > 0) {
+    const int step = (len + 63) / 64, i = base + lane * step;
+    const bool le = lane * step < len && key(i) <= x;
+    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(le));
+    if (c == 0) break;
+    found = base + (c - 1) * step;          // key(found) <= x: the rest of its stride is left to search
+    len = min(step, len - (c - 1) * step) - 1;
+    base = found + 1;
+  }
+  return __builtin_amdgcn_readfirstlane(found);
+}
+
+struct SeqRows {
+  int lo, hi;      // the document's rows; lo == hi: none
+};
+__device__ __forceinline__ SeqRows seq_rows(const Packing& p, int i) {
+  const int lo = seq_start(p, i);
+  return SeqRows{__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(max(lo, seq_start(p, i + 1)))};
+}
+
+// Blocks of `rows` rows that never cross a document: document i owns the slots
+// from starts[i]/rows + i on.  It has ceil(len/rows) blocks and the next one's
+// first slot is floor((start + len)/rows) - floor(start/rows) + 1 >= ceil(len/rows)
+// further, so slots never meet, and a block finds its place without a table:
+// tokens/rows + n_seqs slots cover every packing, the unused ones return at once.
+struct SeqBlock {
+  int lo, hi;      // the document's rows
+  int row0;        // the block's first row; hi <= row0: no block in this slot
+};
+__device__ __forceinline__ SeqBlock seq_block(const Packing& p, int slot, int rows, int lane) {
+  const int i = last_not_above(p.n_seqs, slot, lane, [&](int j) { return seq_start(p, j) / rows + j; });
+  if (i < 0) return SeqBlock{0, 0, 0};
+  const SeqRows s = seq_rows(p, i);
+  const int t = slot - (s.lo / rows + i);
+  if (t >= (s.hi - s.lo + rows - 1) / rows) return SeqBlock{0, 0, 0};
+  return SeqBlock{s.lo, s.hi, s.lo + t * rows};
+}
+
+}  // namespace l4d

@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include "kernels.h"
+#include "packing.h"
 
 namespace l4d {
 namespace {
@@ -59,6 +60,70 @@ __device__ __forceinline__ void rope_entry(const RopeTable& r, int64_t idx) {
 }
 unsigned rope_blocks(const RopeTable* r, int threads) {
   return r ? static_cast<unsigned>((static_cast<int64_t>(r->rows) * (r->d_h / 2) + threads - 1) / threads) : 0u;
+}
+
+// ------------------------------------------------------------------ rotary positions
+// y = A R(pos) x per pair of a head; see RopeRotate.  One wave per row: a lane
+// forms the angle of pair `lane` (and lane + 64, ..) once for all heads, pos * f in
+// double reduced to a fraction of a turn, its fp32 sine and cosine through LDS,
+// and the row's heads follow in groups of V pairs.
+template <typename T>
+__device__ __forceinline__ float to_f32(T v);
+template <>
+__device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_f32<uint16_t>(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ uint16_t from_f32<uint16_t>(float v) { return f2bf(v); }
+
+template <typename T>
+__global__ void __launch_bounds__(256) rope_rotate_kernel(RopeRotate p) {
+  __shared__ float2 table[4][kMaxRopePairs];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = static_cast<int>(blockIdx.x) * 4 + wave;
+  if (row >= p.tokens) return;
+  int64_t pos = row;
+  if (p.pk.n_seqs >= 0) {
+    const int i = last_not_above(p.pk.n_seqs, row, lane, [&](int j) { return seq_start(p.pk, j); });
+    if (i < 0) return;
+    const SeqRows s = seq_rows(p.pk, i);
+    if (row >= s.hi) return;
+    pos = row - s.lo;
+  }
+  if (p.positions) pos = p.positions[row];
+  const int pairs = p.rot / 2;
+  float2* tab = table[wave];
+  for (int j = lane; j < pairs; j += 64) {
+    double turn = static_cast<double>(pos) * p.turns[j];
+    turn -= rint(turn);
+    float s, c;
+    sincospif(static_cast<float>(2.0 * turn), &s, &c);
+    tab[j] = make_float2(p.amplitude * c, p.amplitude * (p.inverse ? -s : s));
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  for (int t = 0; t < p.n_tensors; ++t) {
+    const RopeHeads& h = p.t[t];
+    const T* x = static_cast<const T*>(h.x) + row * h.x_ld;
+    T* y = static_cast<T*>(h.y) + row * h.y_ld;
+    const int rest = x == y ? 0 : p.d_h - p.rot, units = pairs + rest;   // in place the rest of a head stays
+    for (int u = lane; u < h.heads * units; u += 64) {
+      const int head = u / units, j = u - head * units, base = head * p.d_h;
+      if (j < pairs) {
+        const int a = base + (p.interleaved ? 2 * j : j), b = base + (p.interleaved ? 2 * j + 1 : j + pairs);
+        const float x0 = to_f32<T>(x[a]), x1 = to_f32<T>(x[b]);
+        const float2 cs = tab[j];
+        y[a] = from_f32<T>(x0 * cs.x - x1 * cs.y);
+        y[b] = from_f32<T>(x1 * cs.x + x0 * cs.y);
+      } else {
+        const int a = base + p.rot + j - pairs;
+        y[a] = x[a];
+      }
+    }
+  }
 }
 
 // ------------------------------------------------------------------ RMSNorm
@@ -553,6 +618,86 @@ __global__ void __launch_bounds__(256) xent_grad_kernel(const float* __restrict_
   reinterpret_cast<u32x4*>(dl)[i] = pack8(f);
 }
 
+// ------------------------------------------------------------------ loss without stored logits
+// One wave per row of a piece of fp32 logits.
+
+// The row's running (maximum, sum) and target logit after one more piece.
+__global__ void __launch_bounds__(256) loss_piece_kernel(const float* __restrict__ z, int64_t ld, int64_t n, int32_t n_cols,
+                                                        int64_t v0, const int64_t* __restrict__ targets,
+                                                        float2* __restrict__ stats, float* __restrict__ zt, int first) {
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (row >= n) return;
+  const float* zr = z + row * ld;
+  float m = -INFINITY;
+  for (int j = lane; j < n_cols; j += 64) m = fmaxf(m, zr[j]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  float s = 0.f;
+  for (int j = lane; j < n_cols; j += 64) s += __expf(zr[j] - m);
+  s = wave_sum(s);
+  if (lane != 0) return;
+  if (!first) {
+    const float2 old = stats[row];
+    const float big = fmaxf(m, old.x);
+    s = s * __expf(m - big) + old.y * __expf(old.x - big);
+    m = big;
+  }
+  stats[row] = make_float2(m, s);
+  const int64_t t = targets[row] - v0;
+  const bool here = t >= 0 && t < n_cols && targets[row] >= 0;
+  if (here) zt[row] = zr[t];
+  else if (first) zt[row] = -INFINITY;
+}
+
+__global__ void __launch_bounds__(256) loss_finish_kernel(const float2* __restrict__ stats, const float* __restrict__ zt,
+                                                         int64_t n, const int64_t* __restrict__ targets,
+                                                         const float* __restrict__ peer_lse, const float* __restrict__ peer_z,
+                                                         float* __restrict__ loss, float* __restrict__ lse_out,
+                                                         float* __restrict__ z_out) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= n) return;
+  const float2 st = stats[i];
+  float lse = st.x + logf(st.y), z = zt[i];
+  if (z_out) z_out[i] = z;
+  if (peer_lse) {
+    const float p = peer_lse[i], big = fmaxf(lse, p), small = fminf(lse, p);
+    lse = big + log1pf(expf(small - big));
+    if (z == -INFINITY) z = peer_z[i];
+  }
+  lse_out[i] = lse;
+  loss[i] = targets[i] >= 0 ? lse - z : 0.f;
+}
+
+__global__ void __launch_bounds__(256) loss_grad_kernel(const float* __restrict__ z, int64_t ld, int64_t n, int32_t n_cols,
+                                                       int64_t v0, const int64_t* __restrict__ targets,
+                                                       const float* __restrict__ lse, const float* __restrict__ d_loss,
+                                                       float grad_scale, uint16_t* __restrict__ g_hi,
+                                                       uint16_t* __restrict__ g_lo) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= n * ld) return;
+  const int64_t row = i / ld, j = i - row * ld, t = targets[row];
+  const float w = t < 0 ? 0.f : grad_scale * (d_loss ? d_loss[row] : 1.f);
+  float g = 0.f;
+  if (j < n_cols && t >= 0) g = w * (__expf(z[i] - lse[row]) - (t - v0 == j ? 1.f : 0.f));
+  const uint16_t hi = f2bf(g);
+  g_hi[i] = hi;
+  g_lo[i] = f2bf(g - __uint_as_float(static_cast<uint32_t>(hi) << 16));
+}
+
+__global__ void __launch_bounds__(256) zero_f32_kernel(float* __restrict__ x, int64_t n4) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i < n4) reinterpret_cast<float4*>(x)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+__global__ void __launch_bounds__(256) round_bf16_kernel(const float* __restrict__ x, uint16_t* __restrict__ y, int64_t n8) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= n8) return;
+  const float4 a = reinterpret_cast<const float4*>(x)[2 * i], b = reinterpret_cast<const float4*>(x)[2 * i + 1];
+  const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  reinterpret_cast<u32x4*>(y)[i] = pack8(v);
+}
+
 // ------------------------------------------------------------------ embedding
 // Rows of the gathered [b][s_c] token view are split between this rank's own
 // sequence-parallel rows and the peers' rows as in the layer (SpRows below).
@@ -845,6 +990,41 @@ hipError_t embed_bwd(const int64_t* ids, uint64_t* keys, RowSrc dy, int64_t v0, 
                      dim3(kEmbChunk / 2), 0, stream, ids, keys, v0, v_t, rows);
   hipLaunchKernelGGL(embed_bwd_kernel<true>, grid, dim3(256), 0, stream, reinterpret_cast<const int64_t*>(keys), dy,
                      v0, v_t, h, rows, dw);
+  return hipGetLastError();
+}
+
+hipError_t rope_rotate(const RopeRotate& p, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>((p.tokens + 3) / 4));
+  if (p.f32) hipLaunchKernelGGL(rope_rotate_kernel<float>, grid, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL(rope_rotate_kernel<uint16_t>, grid, dim3(256), 0, stream, p);
+  return hipGetLastError();
+}
+
+hipError_t loss_piece(const float* z, int64_t ld, int64_t n, int32_t n_cols, int64_t v0, const int64_t* targets,
+                      float2* stats, float* zt, bool first, hipStream_t stream) {
+  hipLaunchKernelGGL(loss_piece_kernel, dim3(static_cast<unsigned>((n + 3) / 4)), dim3(256), 0, stream, z, ld, n, n_cols, v0,
+                     targets, stats, zt, first ? 1 : 0);
+  return hipGetLastError();
+}
+hipError_t loss_finish(const float2* stats, const float* zt, int64_t n, const int64_t* targets, const float* peer_lse,
+                       const float* peer_z, float* loss, float* lse, float* target_logit, hipStream_t stream) {
+  hipLaunchKernelGGL(loss_finish_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, stream, stats, zt, n,
+                     targets, peer_lse, peer_z, loss, lse, target_logit);
+  return hipGetLastError();
+}
+hipError_t loss_grad(const float* z, int64_t ld, int64_t n, int32_t n_cols, int64_t v0, const int64_t* targets,
+                     const float* lse, const float* d_loss, float grad_scale, uint16_t* g_hi, uint16_t* g_lo,
+                     hipStream_t stream) {
+  hipLaunchKernelGGL(loss_grad_kernel, dim3(static_cast<unsigned>((n * ld + 255) / 256)), dim3(256), 0, stream, z, ld, n,
+                     n_cols, v0, targets, lse, d_loss, grad_scale, g_hi, g_lo);
+  return hipGetLastError();
+}
+hipError_t zero_f32(float* x, int64_t n, hipStream_t stream) {
+  hipLaunchKernelGGL(zero_f32_kernel, dim3(static_cast<unsigned>((n / 4 + 255) / 256)), dim3(256), 0, stream, x, n / 4);
+  return hipGetLastError();
+}
+hipError_t round_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t stream) {
+  hipLaunchKernelGGL(round_bf16_kernel, dim3(static_cast<unsigned>((n / 8 + 255) / 256)), dim3(256), 0, stream, x, y, n / 8);
   return hipGetLastError();
 }
 
