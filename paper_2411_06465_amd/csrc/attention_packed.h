@@ -207,115 +207,235 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 }
 
 // ------------------------------------------------------------------ backward: dK, dV
-// One workgroup per (block of 128 keys, kv head, slice of its query heads): 4
-// waves x 32 keys, each lane one key.  Per query tile and head: S = Q K^T and
-// dP = dO V^T, then dV^T += dO^T P and dK^T += Q^T dS with P, dS from registers.
+// One workgroup per (block of 128 keys, kv head, slice of its query heads), 8 waves.
+// The 128 keys form four groups of 32, each with two waves on the same SIMD
+// (wave w runs on SIMD w % 4):
+//  * role 0 holds K, computes S = Q K^T and P = exp(S - lse), hands P (fp32) to
+//    its partner through LDS and accumulates dV^T += dO^T P;
+//  * role 1 holds V, computes dP = dO V^T, takes P, forms dS = P (dP - delta) and
+//    accumulates dK^T += Q^T dS.
+// Each then needs one operand and one accumulator block, which fits 256 registers
+// (two waves per SIMD), and the softmax of one wave runs under the products of
+// the other.  One wave per group doing both (one wave per SIMD) took 4064 us where
+// this takes 1580 (32768 tokens in 6 documents, 8/1 heads of 128), 441 and 200 (8192
+// tokens in 23, 32/8 heads).
+//
+// Tiles of 32 queries, from the block's own first row to the document's end, of
+// each head in turn, stream through a ring of four stages.
 template <int D>
-__global__ void __launch_bounds__(256) attn_packed_dkdv_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) attn_packed_dkdv_kernel(PackedAttn p) {
   constexpr int TB = QT * D * 2;
-  __shared__ __attribute__((aligned(16))) uint8_t qbuf[2][TB], gbuf[2][TB];
-  __shared__ __attribute__((aligned(16))) float st[2][2][QT];    // lse, delta
+  __shared__ __attribute__((aligned(16))) uint8_t qg[kDkvStages][2][TB];   // per stage: Q tile, then dO tile
+  __shared__ __attribute__((aligned(16))) float st[kDkvStages][2][QT];     // lse, delta
+  __shared__ __attribute__((aligned(16))) float4 xp[2][4][QT / 16][2][64]; // P handover: [buffer][group][16 queries][half][lane]
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = wave & 3, role = wave >> 2;
   const int group = p.heads / p.kv_heads, hps = group / p.n_split;
   const int nyz = p.kv_heads * p.n_split;
   const int slot = static_cast<int>(blockIdx.x) / nyz, yz = static_cast<int>(blockIdx.x) % nyz;
   const int hk = yz / p.n_split, split = yz % p.n_split, head0 = hk * group + split * hps;
   const SeqBlock blk = seq_block(p.pk, slot, 128, lane);
   if (blk.row0 >= blk.hi) return;
-  const int wave_k0 = blk.row0 + wave * 32;
-  const int my_key = wave_k0 + (lane & 31);
+  const int grp_k0 = blk.row0 + grp * 32;
+  const int my_key = grp_k0 + (lane & 31);
   const bool key_ok = my_key < blk.hi;
   const int rbase = 4 * (lane >> 5);
   const LaneAddr la = lane_addr<D>(lane);
+  // offsets into a stage's [Q | dO] pair: the first product reads Q (role 0) or dO, the second the other
+  const LaneAddr la1{la.rows + role * TB, la.cols};
+  const LaneAddr la2{la.rows, la.cols + (1 - role) * TB};
+  // the role's member by arithmetic: a select of two members' addresses would put the kernel argument on the stack
+  const uint64_t role_mask = 0ull - static_cast<uint64_t>(role);
+  const auto pick = [&](uint64_t a, uint64_t b) { return a + ((b - a) & role_mask); };
+  const auto addr = [](const void* x) { return reinterpret_cast<uint64_t>(x); };
 
-  bf16x8 kf[D / 16], vf[D / 16];
+  bf16x8 kv[D / 16];                     // role 0: K rows, role 1: V rows of the group's keys
   {
-    const int64_t row = min(my_key, blk.hi - 1);
+    const uint16_t* src = reinterpret_cast<const uint16_t*>(pick(addr(p.k), addr(p.v))) +
+                          static_cast<int64_t>(pick(p.k_ld, p.v_ld)) * min(my_key, blk.hi - 1) + hk * D;
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) {
-      const int dcol = hk * D + (2 * kk + (lane >> 5)) * 8;
-      kf[kk] = *reinterpret_cast<const bf16x8*>(p.k + row * p.k_ld + dcol);
-      vf[kk] = *reinterpret_cast<const bf16x8*>(p.v + row * p.v_ld + dcol);
-    }
+    for (int kk = 0; kk < D / 16; ++kk) kv[kk] = *reinterpret_cast<const bf16x8*>(src + (2 * kk + (lane >> 5)) * 8);
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) {
-      settle(kf[kk]);
-      settle(vf[kk]);
-    }
+    for (int kk = 0; kk < D / 16; ++kk) settle(kv[kk]);
   }
-  f32x16 dk[D / 32], dv[D / 32];
+  f32x16 acc[D / 32];                    // role 0: dV^T, role 1: dK^T (d rows, the lane's key)
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = f32x16{};
+  for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
   const float c = p.scale * kLog2e;
-  const TileCopy<D, QT> copy_q(p.q_ld, wave, lane), copy_g(p.do_ld, wave, lane);
-  const int n_qt = (blk.hi - blk.row0 + QT - 1) / QT, n_tiles = n_qt * hps;    // query tiles from the block's own rows on
-  // lse or delta by arithmetic: a select of the members' addresses would put the kernel argument on the stack
-  const uint64_t stat0 = reinterpret_cast<uint64_t>(p.lse) +
-                         ((reinterpret_cast<uint64_t>(p.delta) - reinterpret_cast<uint64_t>(p.lse)) & (0ull - (wave & 1)));
-  const auto issue = [&](int t, int b) __attribute__((always_inline)) {
-    const int h = head0 + t / n_qt;
-    const int64_t r0 = blk.row0 + t % n_qt * QT;
-    const int valid = blk.hi - static_cast<int>(r0);
-    copy_q(lds_addr(qbuf[b]), p.q + r0 * p.q_ld + h * D, valid);
-    copy_g(lds_addr(gbuf[b]), p.dout + r0 * p.do_ld + h * D, valid);
-    // waves 0 and 1 fetch the rows' lse and delta
-    const float* stat = reinterpret_cast<const float*>(stat0) + static_cast<int64_t>(h) * p.pk.tokens + r0;
-    if (wave < 2 && lane < QT) dma4(stat, static_cast<uint32_t>(min(lane, valid - 1)) * 4u, lds_addr(st[b][wave & 1]));
+  const int n_rows = blk.hi - blk.row0, n_qt = (n_rows + QT - 1) / QT;
+  // waves 0-3 copy the Q tiles and their lse, waves 4-7 the dO tiles and delta
+  const int64_t ld = pick(p.q_ld, p.do_ld);
+  const TileCopy<D, QT> copy(ld, grp, lane);
+  const uint32_t qg_addr = lds_addr(qg) + role * TB, st_addr = lds_addr(st) + (role * QT + grp * (QT / 4)) * 4;
+  // the next tile to copy: its first row, its head's statistics from the block's first row on, its query tile, tiles left after it
+  uint64_t src = pick(addr(p.q), addr(p.dout)) + (blk.row0 * ld + head0 * D) * 2;
+  uint64_t row = pick(addr(p.lse), addr(p.delta)) + (static_cast<int64_t>(head0) * p.pk.tokens + blk.row0) * 4;
+  const int64_t tile_step = QT * ld * 2, head_step = D * 2 - (n_qt - 1) * tile_step;
+  int copy_qt = 0, copy_left = hps * n_qt - 1;
+  // Copies that tile into stage b, kCopies per wave, and moves on; past the last
+  // tile it repeats it, so that the waits count exactly.
+  constexpr int kCopies = TileCopy<D, QT>::NKB / 4 + 1;
+  auto issue = [&](int b) __attribute__((always_inline)) {
+    const int q0 = copy_qt * QT;
+    if (lane < QT / 4)
+      dma4(reinterpret_cast<const float*>(row), static_cast<uint32_t>(min(q0 + grp * (QT / 4) + lane, n_rows - 1)) * 4u,
+           st_addr + b * (2 * QT * 4));
+    copy(qg_addr + b * (2 * TB), reinterpret_cast<const uint16_t*>(src), n_rows - q0);
+    const bool more = copy_left > 0, wrap = copy_qt + 1 == n_qt;
+    src += more ? (wrap ? head_step : tile_step) : 0;
+    row += more && wrap ? static_cast<int64_t>(p.pk.tokens) * 4 : 0;
+    copy_qt = more ? (wrap ? 0 : copy_qt + 1) : copy_qt;
+    copy_left -= more;
   };
-  issue(0, 0);
-  for (int t = 0; t < n_tiles; ++t) {
-    const int b = t & 1;
-    wait_copies<0>();
-    ring_barrier();
-    if (t + 1 < n_tiles) issue(t + 1, b ^ 1);
-    __builtin_amdgcn_sched_barrier(0);
-    const int q0 = blk.row0 + t % n_qt * QT;
-    f32x16 s = f32x16{}, dp = f32x16{};
-    scores2<D, kLookDq>(qbuf[b], 0, kf, s, gbuf[b], 0, vf, dp, la);
-    // visible query rows r (relative to the lane's first row): lo <= r <= hi
-    const int lo = my_key - q0 - rbase, hi = blk.hi - 1 - q0 - rbase;
+  f32x16 s;                  // role 0: S -> P of a tile, role 1: its dP - delta
+  bf16x8 x[2];               // role 0: P, role 1: dS (bf16)
+  // role 0: P = exp(S - lse) of tile qt from its scores in s; bf16 into x, fp32 into handover hb
+  auto probs = [&](int qt, const float4 (&ls4)[4], float4 (*hb)[2][64]) __attribute__((always_inline)) {
+    const int q0 = blk.row0 + qt * QT;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int r = 8 * (i >> 2) + (i & 3);
-      const float pr = fast_exp2(fmaf(s[i], c, -st[b][0][r + rbase] * kLog2e));
-      s[i] = r < lo || r > hi ? 0.f : pr;
-      dp[i] = r < lo || r > hi ? 0.f : pr * (dp[i] - st[b][1][r + rbase]);
+    for (int jj = 0; jj < 4; ++jj) {
+      const float4 ls = ls4[jj];
+      const float lsv[4] = {ls.x * kLog2e, ls.y * kLog2e, ls.z * kLog2e, ls.w * kLog2e};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s[4 * jj + u] = fast_exp2(fmaf(s[4 * jj + u], c, -lsv[u]));
     }
-    const bf16x8 x[2] = {frag_acc(s, 0), frag_acc(s, 8)}, y[2] = {frag_acc(dp, 0), frag_acc(dp, 8)};
-    accum_t<D, 2, kLookDq>(gbuf[b], x, dv, la);
-    accum_t<D, 2, kLookDq>(qbuf[b], y, dk, la);
-  }
-  if (!key_ok) return;
+    if (q0 < grp_k0 + 31 || q0 + QT > blk.hi) {      // the tile straddles the diagonal, or the document ends in it
+      // visible query rows r (relative to the lane's first row): lo <= r <= hi
+      const int lo = (key_ok ? my_key - q0 : QT) - rbase, hi = blk.hi - 1 - q0 - rbase;
 #pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt) dk[dt] *= p.scale;
+      for (int i = 0; i < 16; ++i) {
+        const int r = 8 * (i >> 2) + (i & 3);
+        if (r < lo || r > hi) s[i] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int i0 = 8 * g;
+      x[g] = frag_acc(s, i0);
+      hb[g][0][lane] = make_float4(s[i0], s[i0 + 1], s[i0 + 2], s[i0 + 3]);
+      hb[g][1][lane] = make_float4(s[i0 + 4], s[i0 + 5], s[i0 + 6], s[i0 + 7]);
+    }
+  };
+  // role 1: dS = P (dP - delta) of the tile whose dP - delta is in s, into x
+  auto grads = [&](const float4 (*hb)[2][64]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const float4 p0 = hb[g][0][lane], p1 = hb[g][1][lane];
+      const float pv[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+      float ds[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) ds[j] = pv[j] * s[8 * g + j];
+      x[g] = __builtin_bit_cast(
+          bf16x8, u32x4{pack2(ds[0], ds[1]), pack2(ds[2], ds[3]), pack2(ds[4], ds[5]), pack2(ds[6], ds[7])});
+    }
+  };
+  auto minus = [&](const float4 (&d4)[4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) {
+      s[4 * jj] -= d4[jj].x;
+      s[4 * jj + 1] -= d4[jj].y;
+      s[4 * jj + 2] -= d4[jj].z;
+      s[4 * jj + 3] -= d4[jj].w;
+    }
+  };
+  // Both roles run one stream of products over role-selected tiles: the next
+  // tile's scores (stage bn) alternating with this tile's accumulation (stage b) of x.
+  auto products = [&](int b, int bn, bool accumulate) __attribute__((always_inline)) {
+    s = f32x16{};
+    const uint8_t* tb = qg[b][0];
+    const uint8_t* tn = qg[bn][0];
+    constexpr int NS = D / 16, NA = 2 * (D / 32);     // products of either kind (equal)
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      s = mfma(frag_rows<D>(tn, 0, i, la1), kv[i], s);
+      if (accumulate) {
+        const int g = i / (D / 32), dt = i % (D / 32);
+        acc[dt] = mfma(frag_cols<D>(tb, dt, g, la2), x[g], acc[dt]);
+      }
+    }
+    static_assert(NS == NA, "scores and accumulation alternate");
+  };
+
+  // One barrier per tile.  Interval j, after the barrier that publishes tile
+  // j + 1 and the handover of P_j: role 1 forms dS_j; both roles run tile j's
+  // accumulation and tile j + 1's scores; role 0 forms and hands over P_(j+1).
+  // The copies of tile j + 3 go out behind the products; past the last tile its
+  // scores are computed once more, unused.
+  float4 stat[4];            // the lane's rows of the next tile's lse (role 0) or delta (role 1)
+  const auto read_stat = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) stat[jj] = *reinterpret_cast<const float4*>(&st[b][role][8 * jj + rbase]);
+  };
+#pragma unroll
+  for (int b = 0; b < kDkvStages - 1; ++b) issue(b);
+  wait_copies<(kDkvStages - 2) * kCopies>();
+  ring_barrier();
+  read_stat(0);
+  products(0, 0, false);
+  if (role == 0) probs(0, stat, xp[0][grp]);
+  else minus(stat);
+  int left = hps * n_qt, qt = 0;
+  const auto interval = [&](auto stage) __attribute__((always_inline)) {
+    constexpr int b = decltype(stage)::value, bn = (b + 1) % kDkvStages;
+    wait_copies<(kDkvStages - 3) * kCopies>();
+    ring_barrier();
+    if (role == 1) grads(xp[b & 1][grp]);
+    __builtin_amdgcn_sched_barrier(0);
+    products(b, bn, true);
+    __builtin_amdgcn_sched_group_barrier(0x100, 3 * 2, 0);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    read_stat(bn);
+    issue((b + kDkvStages - 1) % kDkvStages);     // under the last products
+    if (++qt == n_qt) qt = 0;
+    if (role == 0) probs(qt, stat, xp[bn & 1][grp]);
+    else minus(stat);
+  };
+  while (true) {
+    interval(std::integral_constant<int, 0>{});
+    if (--left == 0) break;
+    interval(std::integral_constant<int, 1>{});
+    if (--left == 0) break;
+    interval(std::integral_constant<int, 2>{});
+    if (--left == 0) break;
+    interval(std::integral_constant<int, 3>{});
+    if (--left == 0) break;
+  }
+  wait_copies<0>();      // no copy may land after the end
+
+  if (!key_ok) return;
+  // lane owns key my_key; register i of tile dt is d = 32 dt + acc_row(i)
+  if (role == 1) {
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) acc[dt] *= p.scale;
+  }
   if (p.n_split > 1) {
     const int64_t half = static_cast<int64_t>(p.n_split) * p.pk.tokens * p.kv_heads * D;
-    float* pk = p.dkv_partial + ((static_cast<int64_t>(split) * p.pk.tokens + my_key) * p.kv_heads + hk) * D;
+    float* out = p.dkv_partial + (role == 1 ? 0 : half) +
+                 ((static_cast<int64_t>(split) * p.pk.tokens + my_key) * p.kv_heads + hk) * D;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj) {
-        const int d = dt * 32 + 8 * jj + rbase;
-        *reinterpret_cast<float4*>(pk + d) =
-            make_float4(dk[dt][4 * jj], dk[dt][4 * jj + 1], dk[dt][4 * jj + 2], dk[dt][4 * jj + 3]);
-        *reinterpret_cast<float4*>(pk + half + d) =
-            make_float4(dv[dt][4 * jj], dv[dt][4 * jj + 1], dv[dt][4 * jj + 2], dv[dt][4 * jj + 3]);
-      }
+      for (int jj = 0; jj < 4; ++jj)
+        *reinterpret_cast<float4*>(out + dt * 32 + 8 * jj + rbase) =
+            make_float4(acc[dt][4 * jj], acc[dt][4 * jj + 1], acc[dt][4 * jj + 2], acc[dt][4 * jj + 3]);
     return;
   }
-  uint16_t* ok = p.dk + static_cast<int64_t>(my_key) * p.dk_ld + hk * D;
-  uint16_t* ov = p.dv + static_cast<int64_t>(my_key) * p.dv_ld + hk * D;
+  uint16_t* out = reinterpret_cast<uint16_t*>(pick(addr(p.dv), addr(p.dk))) +
+                  static_cast<int64_t>(pick(p.dv_ld, p.dk_ld)) * my_key + hk * D;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int jj = 0; jj < 4; ++jj) {
-      const int d = dt * 32 + 8 * jj + rbase;
-      *reinterpret_cast<u32x2*>(ok + d) =
-          u32x2{pack2(dk[dt][4 * jj], dk[dt][4 * jj + 1]), pack2(dk[dt][4 * jj + 2], dk[dt][4 * jj + 3])};
-      *reinterpret_cast<u32x2*>(ov + d) =
-          u32x2{pack2(dv[dt][4 * jj], dv[dt][4 * jj + 1]), pack2(dv[dt][4 * jj + 2], dv[dt][4 * jj + 3])};
-    }
+    for (int jj = 0; jj < 4; ++jj)
+      *reinterpret_cast<u32x2*>(out + dt * 32 + 8 * jj + rbase) =
+          u32x2{pack2(acc[dt][4 * jj], acc[dt][4 * jj + 1]), pack2(acc[dt][4 * jj + 2], acc[dt][4 * jj + 3])};
 }
 
 // dK, dV = the sum of the slices' fp32 parts in order, for the rows that belong to
@@ -363,7 +483,7 @@ hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
   } else if (part == 1) {
     p.n_slots = static_cast<int32_t>(packed_slots(p, 128));
     const dim3 grid(static_cast<unsigned>(p.n_slots) * p.kv_heads * p.n_split);
-    hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, grid, dim3(256), 0, stream, p);
+    hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, grid, dim3(512), 0, stream, p);
   } else {
     if (p.n_split == 1) return hipSuccess;
     const int64_t n = static_cast<int64_t>(p.pk.tokens) * p.kv_heads * (D / 8);
