@@ -13,10 +13,16 @@
 // One workgroup per block of query rows and hpb query heads of one kv head: 4
 // waves x 32 rows, wave w on head w % hpb.  Each lane holds one query's scores
 // (S^T = K Q^T), so the softmax statistics are per-lane scalars.
+//
+// Key tiles of 64; while tile j's softmax runs, the products of tile j + 1's scores
+// are issued between its exponentials, and then tile j's P V products.  Two
+// buffers each for K and V; 64 KB of LDS and at most 256 registers, two workgroups
+// per CU.  The output and the row sum are rescaled only on tiles where some row's
+// maximum grew (a wave-wide vote).
 template <int D>
-__global__ void __launch_bounds__(256) attn_packed_fwd_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) attn_packed_fwd_kernel(PackedAttn p) {
   constexpr int TB = KT * D * 2;
-  __shared__ __attribute__((aligned(16))) uint8_t kbuf[2][TB], vbuf[2][TB];
+  __shared__ __attribute__((aligned(16))) uint8_t k0[TB], v0[TB], k1[TB], v1[TB];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_hg = p.heads / p.hpb, rows = 128 / p.hpb;
@@ -24,7 +30,8 @@ __global__ void __launch_bounds__(256) attn_packed_fwd_kernel(PackedAttn p) {
   const SeqBlock blk = seq_block(p.pk, slot, rows, lane);
   if (blk.row0 >= blk.hi) return;
   const int hq = h0 + wave % p.hpb, hk = h0 / (p.heads / p.kv_heads);
-  const int my_q = blk.row0 + wave / p.hpb * 32 + (lane & 31);
+  const int wave_q0 = blk.row0 + wave / p.hpb * 32;
+  const int my_q = wave_q0 + (lane & 31);
   const bool q_ok = my_q < blk.hi;
   const int n_keys = min(blk.row0 + rows, blk.hi) - blk.lo;      // keys the block's last row sees
   const int rbase = 4 * (lane >> 5);
@@ -45,50 +52,121 @@ __global__ void __launch_bounds__(256) attn_packed_fwd_kernel(PackedAttn p) {
   for (int i = 0; i < D / 32; ++i) o[i] = f32x16{};
 
   const TileCopy<D, KT> copy_k(p.k_ld, wave, lane), copy_v(p.v_ld, wave, lane);
+  const uint32_t ka0 = lds_addr(k0), ka1 = lds_addr(k1), va0 = lds_addr(v0), va1 = lds_addr(v1);
   const int n_tiles = (n_keys + KT - 1) / KT;
-  const auto issue = [&](int t, int b) __attribute__((always_inline)) {
-    const int64_t row = blk.lo + t * KT;
-    const int valid = blk.hi - static_cast<int>(row);
-    copy_k(lds_addr(kbuf[b]), p.k + row * p.k_ld + hk * D, valid);
-    copy_v(lds_addr(vbuf[b]), p.v + row * p.v_ld + hk * D, valid);
+  const auto row_max = [](const f32x16 (&s)[2]) __attribute__((always_inline)) {
+    float m = __builtin_fmaxf(s[0][0], s[0][1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) m = __builtin_fmaxf(__builtin_fmaxf(m, s[0][i]), s[0][i + 1]);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) m = __builtin_fmaxf(__builtin_fmaxf(m, s[1][i]), s[1][i + 1]);
+    return m;
   };
-  issue(0, 0);
-  for (int t = 0; t < n_tiles; ++t) {
-    const int b = t & 1;
-    wait_copies<0>();
-    ring_barrier();                     // tile t is visible; the other buffers are free
-    if (t + 1 < n_tiles) issue(t + 1, b ^ 1);
-    __builtin_amdgcn_sched_barrier(0);
-    f32x16 s[2] = {f32x16{}, f32x16{}};
-    scores2<D, kLookFwd>(kbuf[b], 0, qf, s[0], kbuf[b], 32, qf, s[1], la);
-    const int lim = my_q - (blk.lo + t * KT) - rbase;      // last visible key, relative to the lane's first
-    float mx = -INFINITY;
+  // Key tile t, its scores already in s (their maximum in mx): the softmax and
+  // O += V^T P, with the next tile's scores (into sn, mxn) computed under the
+  // exponentials.  After the last tile sn comes from stale LDS and is never used.
+  const auto step = [&](int t, const uint8_t* vt, const uint8_t* kt_next, f32x16 (&s)[2], float mx, f32x16 (&sn)[2],
+                        float& mxn) __attribute__((always_inline)) {
+    const int kpos0 = blk.lo + t * KT;
+    if (kpos0 + KT - 1 > wave_q0) {                   // the tile reaches past the wave's first row
+      const int lim = my_q - kpos0 - rbase;           // last visible key, relative to the lane's first
 #pragma unroll
-    for (int t2 = 0; t2 < 2; ++t2)
+      for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (t2 * 32 + 8 * (i >> 2) + (i & 3) > lim) s[t2][i] = -INFINITY;
-        mx = fmaxf(mx, s[t2][i]);
-      }
+        for (int i = 0; i < 16; ++i)
+          if (t2 * 32 + 8 * (i >> 2) + (i & 3) > lim) s[t2][i] = -INFINITY;
+      mx = row_max(s);
+    }
     mx = half_max(mx) * c;
-    const float m_new = fmaxf(m_run, mx);
-    const float alpha = m_new == -INFINITY ? 1.f : fast_exp2(m_run - m_new);
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;
-    m_run = m_new;
-    l_run *= alpha;
+    if (__builtin_amdgcn_ballot_w64(mx > m_run)) {
+      const float m_new = fmaxf(m_run, mx);
+      const float alpha = fast_exp2(m_run - m_new);   // 0 on the first tile, whose own key every row sees
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
+      for (int dt = 0; dt < D / 32; ++dt) o[dt] *= alpha;
+      l_run *= alpha;
+      m_run = m_new;
+    }
+    sn[0] = f32x16{};
+    sn[1] = f32x16{};
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      sn[0] = mfma(frag_rows<D>(kt_next, 0, kk, la), qf[kk], sn[0]);
+      sn[1] = mfma(frag_rows<D>(kt_next, 32, kk, la), qf[kk], sn[1]);
+    }
+    float rs[2] = {0.f, 0.f};
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[t2][i] = fast_exp2(fmaf(s[t2][i], c, -m_use));
-        l_run += s[t2][i];
+        const float pr = fast_exp2(fmaf(s[t2][i], c, -m_run));
+        s[t2][i] = pr;
+        rs[i & 1] += pr;
       }
-    // P as bf16 for the product: half a step, 2^-9 of each probability, of the size
+    l_run += rs[0] + rs[1];
+    // the score products: an LDS read (kLookFwd ahead), exponentials and their sums between every two
+    constexpr int NS = D / 8, NV = D / 32;
+    __builtin_amdgcn_sched_group_barrier(0x100, kLookFwd, 0);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);            // MFMA
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);            // LDS read
+      __builtin_amdgcn_sched_group_barrier(0x400, 32 / NS, 0);      // exponentials
+      __builtin_amdgcn_sched_group_barrier(0x002, 96 / NS, 0);      // other VALU
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // P enters the product as bf16, off by at most 2^-8 of each probability: the size
     // of the output's own rounding
-    const bf16x8 x[4] = {frag_acc(s[0], 0), frag_acc(s[0], 8), frag_acc(s[1], 0), frag_acc(s[1], 8)};
-    accum_t<D, 4, kLookDq>(vbuf[b], x, o, la);
+    bf16x8 x[2], f[2][NV];
+    const auto group = [&](int g) __attribute__((always_inline)) {
+      x[g & 1] = frag_acc(s[g >> 1], 8 * (g & 1));
+#pragma unroll
+      for (int dt = 0; dt < NV; ++dt) f[g & 1][dt] = frag_cols<D>(vt, dt, g, la);
+    };
+    group(0);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (g < 3) group(g + 1);
+      else mxn = row_max(sn);
+#pragma unroll
+      for (int dt = 0; dt < NV; ++dt) o[dt] = mfma(f[g & 1][dt], x[g & 1], o[dt]);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 16 / NV, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // While tile j is in step, V_j and K_(j+1) are in use, V_(j+1) and K_(j+2) land in
+  // the buffers that V_(j-1) and K_j held.
+  const auto copy_tile = [&](const TileCopy<D, KT>& copy, const uint16_t* base, int64_t ld, int t, uint32_t lds)
+      __attribute__((always_inline)) {
+    const int64_t row = blk.lo + t * KT;
+    if (t < n_tiles) copy(lds, base + row * ld + hk * D, blk.hi - static_cast<int>(row));
+  };
+  copy_tile(copy_k, p.k, p.k_ld, 0, ka0);
+  copy_tile(copy_v, p.v, p.v_ld, 0, va0);
+  copy_tile(copy_k, p.k, p.k_ld, 1, ka1);
+  wait_copies<0>();
+  ring_barrier();
+  f32x16 sa[2] = {f32x16{}, f32x16{}}, sb[2];
+  scores2<D, kLookFwd>(k0, 0, qf, sa[0], k0, 32, qf, sa[1], la);
+  float ma = row_max(sa), mb = -INFINITY;
+  const auto turn = [&](int t, const uint8_t* vt, uint32_t va_next, uint32_t ka, const uint8_t* kt_next, f32x16 (&s)[2],
+                        float mx, f32x16 (&sn)[2], float& mxn) __attribute__((always_inline)) {
+    wait_copies<0>();
+    ring_barrier();                      // every wave's copies are visible and the two old buffers are free
+    copy_tile(copy_v, p.v, p.v_ld, t + 1, va_next);
+    copy_tile(copy_k, p.k, p.k_ld, t + 2, ka);
+    __builtin_amdgcn_sched_barrier(0);   // the copies go out now, not next to the wait for them
+    step(t, vt, kt_next, s, mx, sn, mxn);
+  };
+  for (int t = 0; t < n_tiles; t += 2) {
+    turn(t, v0, va1, ka0, k1, sa, ma, sb, mb);
+    if (t + 1 >= n_tiles) break;
+    turn(t + 1, v1, va0, ka1, k0, sb, mb, sa, ma);
   }
 
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
