@@ -461,9 +461,9 @@ int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void
  * LM-head cross-entropy without stored logits
  *
  * Forward and backward of the loss of lm_head_xent for any number of tokens and
- * any vocabulary, in workspace that does not grow with n x v: the forward keeps
- * one (maximum, sum) pair per token and block of columns, the backward forms the
- * logits again, a piece of the vocabulary at a time.
+ * any vocabulary, in bounded pieces of the vocabulary: the forward keeps one
+ * (maximum, sum) pair per token and block of columns, the backward forms the logits
+ * again and the gradient G of one piece at a time.
  *   z = hidden W_lm^T (fp32);  lse_i = log sum_j exp z_ij, combined with
  *   peer_lse_i when given;  loss_i = lse_i - z_i[target], 0 where target < 0
  *   (an ignored token: a document's last one, padding).
@@ -479,12 +479,16 @@ int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void
  *   lse of the backward: f32 [N], over the whole vocabulary.
  * With peers NULL, a target >= vocab_start + v_t or below vocab_start counts as
  * logit -infinity (loss +infinity).
- * In G the fp32 value is kept as two bf16 parts for d_w_lm (relative error 2^-17)
- * and rounded to one for d_hidden.
- * Requirements: h % 8 == 0, h <= 8192, hidden, w_lm and d_hidden 16-byte aligned;
- * finite hidden rows also
- * of ignored tokens (their zero weights multiply them); any N from 0 to 2^29 and v_t from 1 to 2^30 with N x v_t <= 2^40.  N == 0 launches
- * nothing.
+ * The products take G in bf16: one part for d_hidden, two for d_w_lm (they leave
+ * 2^-18 of an element); what the parts leave at the target, where G is largest, is
+ * added in fp32.
+ * The workspace holds 8 bytes per token and 64 columns in the forward, 4 per token
+ * and column in the backward, of a piece of the vocabulary: what 2^25 tokens x
+ * columns take (268 MB) or, for many tokens, 65536 and 4096 columns; and the fp32
+ * d_hidden.
+ * Requirements: h % 8 == 0, h <= 8192; hidden, w_lm and d_hidden 16-byte aligned;
+ * N <= 2^20, v_t <= 2^24; finite hidden rows also of ignored tokens (their zero
+ * weights multiply them in d_w_lm).  N == 0 launches nothing.
  * ---------------------------------------------------------------------- */
 int l4d_lm_loss_workspace_bytes(int64_t n_tokens, int64_t hidden, int64_t vocab_shard, uint64_t* fwd_bytes,
                                 uint64_t* bwd_bytes);

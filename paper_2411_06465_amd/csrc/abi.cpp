@@ -1536,26 +1536,41 @@ extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const 
 // ============================================================== loss without stored logits
 
 namespace {
-// Columns of a piece of the vocabulary.
-int64_t loss_piece_cols(int64_t n, int64_t v_t) {
-  const int64_t cols = std::max<int64_t>(4096, (((int64_t)1 << 26) / std::max<int64_t>(n, 1)) / 256 * 256);
+// Columns of a piece of the vocabulary: forward (its statistics: 8 bytes for 64
+// columns) and backward (its gradient: 4 bytes a column).
+int64_t loss_piece_cols(int64_t n, int64_t v_t, int64_t least, int64_t elements) {
+  const int64_t cols = std::max(least, elements / std::max<int64_t>(n, 1) / 256 * 256);
   return std::min(cols, (v_t + 7) / 8 * 8);
 }
 struct LossWs {
-  int64_t piece;                                     // columns, the row length of the piece's arrays
-  uint64_t stats, zt, z, g_hi, dh, fwd, bwd;
+  int64_t fwd_piece, bwd_piece;                      // columns
+  uint64_t stats, zt, run, fwd;                      // forward: offsets and total
+  uint64_t g, dh, gt, rep, part, bwd;                // backward: g [parts][n][bwd_piece], rep = hidden once per part
+  int parts, dx_splits;                              // bf16 parts of G; parts of the K range of G W
 };
+// Bf16 parts of G in the product with hidden: two leave 2.4e-6 (rms) of an element and,
+// with the targets' elements completed, 1e-7 to 1e-6 of d_w.  A shard that holds
+// no token's target has only the small elements; with few tokens that happens, and
+// there the product is bound by d_w's own traffic: the third part costs nothing.
+constexpr int64_t kThreeParts = 256;
+constexpr int kDxSplits = 8;
 LossWs plan_loss(int64_t n, int64_t h, int64_t v_t) {
   LossWs w{};
-  w.piece = loss_piece_cols(n, v_t);
+  w.fwd_piece = loss_piece_cols(n, v_t, 65536, (int64_t)1 << 31);
+  w.bwd_piece = loss_piece_cols(n, v_t, 4096, (int64_t)1 << 26);
+  w.parts = n <= kThreeParts ? 3 : 2;
+  const GemmPlan dx = gemm_plan(n, h, std::min(w.bwd_piece, v_t), EpiKind::AccF32, kDxSplits);
+  w.dx_splits = dx.splits;
   Carver f, b;
-  w.z = f.take((uint64_t)n * w.piece * 4);
-  w.stats = f.take((uint64_t)n * 8);
+  w.stats = f.take((uint64_t)n * ((w.fwd_piece + 255) / 256 * 4) * 8);
   w.zt = f.take((uint64_t)n * 4);
+  w.run = f.take((uint64_t)n * 8);
   w.fwd = f.used;
-  b.take((uint64_t)n * w.piece * 4);
-  w.g_hi = b.take((uint64_t)n * w.piece * 4);        // the high parts [n][piece], then the low ones
+  w.g = b.take((uint64_t)n * w.bwd_piece * 2 * w.parts);
   w.dh = b.take((uint64_t)n * h * 4);
+  w.gt = b.take((uint64_t)n * 4);
+  w.rep = b.take((uint64_t)n * h * 2 * w.parts);
+  w.part = b.take((uint64_t)n * h * 4 * (w.dx_splits - 1));
   w.bwd = b.used;
   return w;
 }
@@ -1564,7 +1579,7 @@ int loss_check(int64_t n, int64_t h, int64_t v_t, int64_t v0, std::initializer_l
                std::initializer_list<const void*> words, const int64_t* targets) {
   if (n < 0 || h <= 0 || v_t <= 0 || v0 < 0) return fail(L4D_EINVAL, "bad LM-head sizes");
   if (h % 8 || h > 8192) return fail(L4D_EINVAL, "hidden must be a multiple of 8 and at most 8192");
-  if (n > (int64_t)1 << 29 || v_t > (int64_t)1 << 30 || n * v_t > (int64_t)1 << 40) return fail(L4D_EINVAL, "problem too large");
+  if (n > (int64_t)1 << 20 || v_t > (int64_t)1 << 24) return fail(L4D_EINVAL, "problem too large");   // grid sizes
   for (const void* p : rows)
     if (!p || reinterpret_cast<uintptr_t>(p) % 16)
       return fail(L4D_EINVAL, "hidden, w_lm and d_hidden are required, 16-byte aligned");
@@ -1574,15 +1589,10 @@ int loss_check(int64_t n, int64_t h, int64_t v_t, int64_t v0, std::initializer_l
     return fail(L4D_EINVAL, "targets is required, 8-byte aligned");
   return L4D_OK;
 }
-// z (f32 [n][ld]) = the logits of columns [c0, c0 + cols) of the shard
-int loss_logits(const char* name, int64_t n, int64_t h, const void* hidden, const void* w_lm, int64_t c0, int64_t cols,
-                float* z, int64_t ld, hipStream_t s) {
-  EpiParams e{};
-  e.kind = EpiKind::StoreF32;
-  e.c = z;
-  e.ldc = ld;
-  return run_gemm(name, s, n, cols, h, op(RowSrc::plain(hidden, h), n), Layout::KC,
-                  op(RowSrc::plain(static_cast<const uint16_t*>(w_lm) + c0 * h, h), cols), Layout::KC, e);
+// The product of the logits of `cols` columns from row w of the head, with epilogue e.
+int loss_logits(int64_t n, int64_t h, const void* hidden, const uint16_t* w, int64_t cols, const EpiParams& e, hipStream_t s) {
+  return run_gemm(e.kind == EpiKind::LossStats ? "gemm_loss_stats" : "gemm_loss_grad", s, n, cols, h,
+                  op(RowSrc::plain(hidden, h), n), Layout::KC, op(RowSrc::plain(w, h), cols), Layout::KC, e);
 }
 }  // namespace
 
@@ -1607,20 +1617,30 @@ extern "C" int lm_loss_fwd(int64_t n, int64_t h, int64_t v_t, int64_t v0, const 
   Workspace ws;
   if ((rc = take_ws(A, plan.fwd, ws))) return rc;
   uint8_t* wsb = reinterpret_cast<uint8_t*>(A->base + ws.off);
-  float *z = reinterpret_cast<float*>(wsb + plan.z), *zt = reinterpret_cast<float*>(wsb + plan.zt);
-  float2* stats = reinterpret_cast<float2*>(wsb + plan.stats);
   hipStream_t s = static_cast<hipStream_t>(stream_ptr);
-  for (int64_t c0 = 0; c0 < v_t; c0 += plan.piece) {
-    const int64_t cols = std::min(plan.piece, v_t - c0);
-    if ((rc = loss_logits("gemm_loss_logits", n, h, hidden, w_lm, c0, cols, z, plan.piece, s))) return rc;
-    if ((rc = launch("loss_piece", s, [&] {
-           return loss_piece(z, plan.piece, n, (int32_t)cols, v0 + c0, targets, stats, zt, c0 == 0, s);
-         })))
-      return rc;
+  LossJoin j{};
+  j.stats = reinterpret_cast<float2*>(wsb + plan.stats);
+  j.run = reinterpret_cast<float2*>(wsb + plan.run);
+  j.zt = reinterpret_cast<float*>(wsb + plan.zt);
+  j.n = n, j.v0 = v0, j.v_t = v_t;
+  j.targets = targets;
+  j.peer_lse = peer_lse, j.peer_z = peer_z;
+  j.loss = loss, j.lse = lse, j.target_logit = target_logit;
+  EpiParams e{};
+  e.kind = EpiKind::LossStats;
+  e.targets = targets;
+  e.stats = reinterpret_cast<float2*>(wsb + plan.stats);
+  e.zt = reinterpret_cast<float*>(wsb + plan.zt);
+  for (int64_t c0 = 0; c0 < v_t; c0 += plan.fwd_piece) {
+    const int64_t cols = std::min(plan.fwd_piece, v_t - c0);
+    e.v0 = v0 + c0;
+    if ((rc = loss_logits(n, h, hidden, static_cast<const uint16_t*>(w_lm) + c0 * h, cols, e, s))) return rc;
+    j.n_blocks = (int32_t)loss_stat_blocks(cols, gemm_plan(n, cols, h, e.kind, 1).tile);
+    j.first = c0 == 0;
+    j.last = c0 + cols == v_t;
+    if ((rc = launch("loss_join", s, [&] { return loss_join(j, s); }))) return rc;
   }
-  return launch("loss_finish", s, [&] {
-    return loss_finish(stats, zt, n, targets, peer_lse, peer_z, loss, lse, target_logit, s);
-  });
+  return L4D_OK;
 }
 
 extern "C" int lm_loss_bwd(int64_t n, int64_t h, int64_t v_t, int64_t v0, const void* hidden, const void* w_lm,
@@ -1635,29 +1655,51 @@ extern "C" int lm_loss_bwd(int64_t n, int64_t h, int64_t v_t, int64_t v0, const 
   Workspace ws;
   if ((rc = take_ws(A, plan.bwd, ws))) return rc;
   uint8_t* wsb = reinterpret_cast<uint8_t*>(A->base + ws.off);
-  float *z = reinterpret_cast<float*>(wsb + plan.z), *dh = reinterpret_cast<float*>(wsb + plan.dh);
-  uint16_t *g_hi = reinterpret_cast<uint16_t*>(wsb + plan.g_hi), *g_lo = g_hi + n * plan.piece;
+  const int64_t ld = plan.bwd_piece;
+  float *dh = reinterpret_cast<float*>(wsb + plan.dh), *gt = reinterpret_cast<float*>(wsb + plan.gt);
+  uint16_t* g = reinterpret_cast<uint16_t*>(wsb + plan.g);
   hipStream_t s = static_cast<hipStream_t>(stream_ptr);
-  // the products of G^T hidden run over 2 n rows: the high parts of G, then the low ones, against hidden twice
-  const RowSrc twice{static_cast<const uint16_t*>(hidden), static_cast<const uint16_t*>(hidden), h, (int32_t)(2 * n),
-                     (int32_t)n, 0, 2};
-  if ((rc = launch("zero_dh", s, [&] { return zero_f32(dh, n * h, s); }))) return rc;
-  for (int64_t c0 = 0; c0 < v_t; c0 += plan.piece) {
-    const int64_t cols = std::min(plan.piece, v_t - c0), ld = plan.piece;
+  EpiParams e{};
+  e.kind = EpiKind::LossGrad;
+  e.targets = targets;
+  e.lse = lse;
+  e.d_loss = d_loss;
+  e.grad_scale = grad_scale;
+  e.zt = gt;
+  e.g = g;
+  e.g_parts = plan.parts;
+  e.ldc = ld;
+  EpiParams store{};           // dh of the first piece: an fp32 store, unless its K range is cut
+  store.kind = EpiKind::ResidualSP;
+  store.ldc = h;
+  store.own_out_f32 = dh;
+  store.t = 1;
+  uint16_t* rep = reinterpret_cast<uint16_t*>(wsb + plan.rep);
+  float* part = reinterpret_cast<float*>(wsb + plan.part);
+  const bool split = plan.dx_splits > 1;
+  if (split && (rc = launch("loss_zero_dh", s, [&] { return zero_f32(dh, n * h, s); }))) return rc;
+  // G^T hidden runs over parts x n rows: one part of G after another, hidden again for each
+  if ((rc = launch("loss_repeat", s, [&] {
+         return repeat_bf16(static_cast<const uint16_t*>(hidden), rep, n * h, plan.parts, s);
+       })))
+    return rc;
+  for (int64_t c0 = 0; c0 < v_t; c0 += ld) {
+    const int64_t cols = std::min(ld, v_t - c0);
     const uint16_t* w = static_cast<const uint16_t*>(w_lm) + c0 * h;
-    if ((rc = loss_logits("gemm_loss_logits", n, h, hidden, w_lm, c0, cols, z, ld, s))) return rc;
-    if ((rc = launch("loss_grad", s, [&] {
-           return loss_grad(z, ld, n, (int32_t)cols, v0 + c0, targets, lse, d_loss, grad_scale, g_hi, g_lo, s);
-         })))
+    e.v0 = v0 + c0;
+    if ((rc = loss_logits(n, h, hidden, w, cols, e, s))) return rc;
+    if ((rc = run_gemm("gemm_loss_dx", s, n, h, cols, op(RowSrc::plain(g, ld), n), Layout::KC, op(RowSrc::plain(w, h), h),
+                       Layout::MN, c0 == 0 && !split ? store : epi_acc(dh, h), split ? part : nullptr,
+                       split ? plan.dx_splits : 0)))
       return rc;
-    if ((rc = run_gemm("gemm_loss_dx", s, n, h, cols, op(RowSrc::plain(g_hi, ld), n), Layout::KC,
-                       op(RowSrc::plain(w, h), h), Layout::MN, epi_acc(dh, h))))
-      return rc;
-    if ((rc = run_gemm("gemm_loss_dw", s, cols, h, 2 * n, op(RowSrc::plain(g_hi, ld), ld), Layout::MN, op(twice, h),
-                       Layout::MN, epi_acc(d_w + c0 * h, h))))
+    if ((rc = run_gemm("gemm_loss_dw", s, cols, h, plan.parts * n, op(RowSrc::plain(g, ld), (cols + 7) / 8 * 8), Layout::MN,
+                       op(RowSrc::plain(rep, h), h), Layout::MN, epi_acc(d_w + c0 * h, h))))
       return rc;
   }
-  return launch("round_dh", s, [&] { return round_bf16(dh, static_cast<uint16_t*>(d_hidden), n * h, s); });
+  const LossTargets t{n, v0, v_t, (int32_t)h, targets, gt, plan.parts, dh, static_cast<const uint16_t*>(hidden),
+                      static_cast<const uint16_t*>(w_lm), static_cast<uint16_t*>(d_hidden), d_w};
+  if ((rc = launch("loss_finish_dh", s, [&] { return loss_finish_dh(t, s); }))) return rc;
+  return launch("loss_finish_dw", s, [&] { return loss_finish_dw(t, s); });
 }
 
 // ============================================================== optimizer

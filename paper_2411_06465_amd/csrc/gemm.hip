@@ -177,6 +177,17 @@ struct EpiIn<EpiKind::AccF32> {
   f32x4 c[4];             // the accumulator: low and high half
 };
 
+template <>
+struct EpiIn<EpiKind::LossStats> {
+  int32_t t;              // the target's column, -1 = none of the product's
+};
+template <>
+struct EpiIn<EpiKind::LossGrad> {
+  int32_t t;
+  float lse, w;           // w: the row's weight, 0 for an ignored token
+};
+constexpr float kLog2e = 1.4426950408889634f;
+
 // Output row of logical row m for ResidualSP: own rows map into own_out,
 // the others into the send buffer.
 __device__ __forceinline__ int64_t resid_row(const EpiParams& e, int64_t m, bool& own) {
@@ -237,6 +248,13 @@ __device__ __forceinline__ void epi_load(const GemmParams& p, int64_t m, int n_l
     const float4* tab = reinterpret_cast<const float4*>(e.rope + static_cast<int64_t>(i) * (e.d_h / 2) + (n % e.d_h));
 #pragma unroll
     for (int j = 0; j < 4; ++j) in.cs[j] = tab[j];
+  } else if constexpr (KIND == EpiKind::LossStats || KIND == EpiKind::LossGrad) {
+    const int64_t id = e.targets[m], t = id - e.v0;
+    in.t = id >= 0 && t >= 0 && t < p.N ? static_cast<int32_t>(t) : -1;
+    if constexpr (KIND == EpiKind::LossGrad) {
+      in.lse = e.lse[m];
+      in.w = id < 0 ? 0.f : e.grad_scale * (e.d_loss ? e.d_loss[m] : 1.f);
+    }
   }
 }
 
@@ -388,6 +406,64 @@ __device__ __forceinline__ void epilogue(const GemmParams& p, int64_t m, int n_l
           uint16_t* out = e.dgu + m * (2 * static_cast<int64_t>(e.f));
           *reinterpret_cast<u32x4*>(out + n) = pack8(dg);
           *reinterpret_cast<u32x4*>(out + e.f + n) = pack8(du);
+        }
+      }
+      break;
+    }
+    case EpiKind::LossStats: {
+      // The 16 columns of this call, then the row's other lanes of the block: 4 in a
+      // wave of the 256-row kernel (64 columns of the tile), T/16 in a T-column tile.
+      if constexpr (KIND == EpiKind::LossStats) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (n_lo + j >= p.N) lo[j] = -INFINITY;
+          if (n_lo + pair + j >= p.N) hi[j] = -INFINITY;
+          mx = fmaxf(mx, fmaxf(lo[j], hi[j]));
+          if (n_lo + j == in.t) e.zt[m] = lo[j];
+          if (n_lo + pair + j == in.t) e.zt[m] = hi[j];
+        }
+        const int lanes = pair == 32 || pair == 128 ? 4 : 8;
+        mx = fmaxf(mx, __shfl_xor(mx, 1, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 2, 64));
+        if (lanes == 8) mx = fmaxf(mx, __shfl_xor(mx, 4, 64));
+        const float top = mx == -INFINITY ? 0.f : mx;
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          s += __builtin_amdgcn_exp2f((lo[j] - top) * kLog2e) + __builtin_amdgcn_exp2f((hi[j] - top) * kLog2e);
+        s += __shfl_xor(s, 1, 64);
+        s += __shfl_xor(s, 2, 64);
+        if (lanes == 8) s += __shfl_xor(s, 4, 64);
+        const int blk = pair == 128 ? (n_lo >> 8) * 4 + ((n_lo >> 5) & 3) : n_lo / (2 * pair);
+        if ((n_lo & (pair == 128 ? 31 : 2 * pair - 1)) == 0) e.stats[static_cast<int64_t>(blk) * p.M + m] = make_float2(mx, s);
+      }
+      break;
+    }
+    case EpiKind::LossGrad: {
+      if constexpr (KIND == EpiKind::LossGrad) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int n = n_lo + h * pair;
+          if (n >= p.N) continue;
+          const float* z = h ? hi : lo;
+          float g[8], r[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            // a difference first: where the probability is large it is exact or nearly so
+            const float pr = __builtin_amdgcn_exp2f((z[j] - in.lse) * kLog2e);
+            g[j] = in.w * (n + j == in.t ? pr - 1.f : pr);
+            if (n + j >= p.N || in.w == 0.f) g[j] = 0.f;
+            if (n + j == in.t) e.zt[m] = g[j];
+          }
+          uint16_t* out = e.g + m * e.ldc + n;
+          for (int part = 0; part < e.g_parts; ++part) {     // each part the bf16 nearest to what the ones before leave
+            const u32x4 b = pack8(g);
+            *reinterpret_cast<u32x4*>(out + part * (p.M * e.ldc)) = b;
+            unpack8(b, r);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] -= r[j];
+          }
         }
       }
       break;
@@ -1296,6 +1372,8 @@ hipError_t gemm(const GemmParams& params, Layout la, Layout lb, hipStream_t stre
     if (k == E::SwiGLUFwd) return launch<L::KC, L::KC, E::SwiGLUFwd, 128>(p, stream);
     if (k == E::StoreBF16) return launch<L::KC, L::KC, E::StoreBF16, 128>(p, stream);
     if (k == E::StoreF32) return launch<L::KC, L::KC, E::StoreF32, 128>(p, stream);
+    if (k == E::LossStats) return launch<L::KC, L::KC, E::LossStats, 128>(p, stream);
+    if (k == E::LossGrad) return launch<L::KC, L::KC, E::LossGrad, 128>(p, stream);
   } else if (la == L::KC && lb == L::MN) {
     if (k == E::SwiGLUBwd) return launch<L::KC, L::MN, E::SwiGLUBwd, 128>(p, stream);
     if (k == E::ResidualSP) return launch<L::KC, L::MN, E::ResidualSP, 128>(p, stream);
@@ -1472,6 +1550,8 @@ GemmPlan gemm_plan(int64_t M, int64_t N, int64_t K, EpiKind kind, int max_splits
   }
   return best;
 }
+
+int64_t loss_stat_blocks(int64_t N, int32_t tile) { return tile == 256 ? (N + 255) / 256 * 4 : (N + tile - 1) / tile; }
 
 hipError_t gemm_split_reduce(float* c, int64_t ldc, const float* partial, int64_t M, int64_t N, int32_t splits,
                              hipStream_t stream) {

@@ -66,7 +66,9 @@ enum class EpiKind {
   QkvRope,      // split [Q|K|V] columns, RoPE on Q and K, bf16
   ResidualSP,   // own rows: bf16 or fp32 (acc + resid + receipt); peer rows: bf16(acc) -> send buffer
   SwiGLUFwd,    // gate/up tile pairs -> G, U, act, prod (bf16)
-  SwiGLUBwd     // acc = d(prod) -> dG, dU from the stashed G, U, act
+  SwiGLUBwd,    // acc = d(prod) -> dG, dU from the stashed G, U, act
+  LossStats,    // acc = logits -> (maximum, sum of exponentials) per row and block of columns, the target's logit
+  LossGrad      // acc = logits -> the loss gradient G, as a sum of bf16 parts
 };
 
 struct EpiParams {
@@ -90,6 +92,15 @@ struct EpiParams {
   const uint16_t *g_in, *u_in, *act_in;
   uint16_t* dgu;        // [tokens][2f] : dG columns [0,f), dU columns [f,2f)
   int32_t f;
+  // LossStats / LossGrad: column 0 of the product is vocabulary id v0
+  const int64_t* targets;   // [M]
+  int64_t v0;
+  float2* stats;            // LossStats: [loss_stat_blocks()][M]
+  float* zt;                // [M], where the target is a column: LossStats its logit, LossGrad its G
+  const float *lse, *d_loss;   // LossGrad: [M]; d_loss may be null (1)
+  float grad_scale;
+  uint16_t* g;              // LossGrad: [g_parts][M][ldc], whole groups of 8 columns (zeros past N)
+  int32_t g_parts;
 };
 
 struct GemmParams {
@@ -300,21 +311,41 @@ hipError_t xent_probs(float* logits, int64_t n, int32_t v_t, int64_t v0, const i
 hipError_t xent_grad(const float* probs, int64_t n, int32_t v_t, int64_t v0, const int64_t* targets,
                      float grad_scale, uint16_t* dlogits, hipStream_t stream);
 
-// Loss without stored logits, one piece of n_cols columns (rows of the vocabulary,
-// from v0 on) at a time; z: fp32 logits [n][ld] of the piece.
-// stats[i] = (m, s), the running maximum of row i and the sum of exp(z - m) (first:
-// the row's first piece); zt[i] = the target's logit, -infinity until met.
-hipError_t loss_piece(const float* z, int64_t ld, int64_t n, int32_t n_cols, int64_t v0, const int64_t* targets,
-                      float2* stats, float* zt, bool first, hipStream_t stream);
-hipError_t loss_finish(const float2* stats, const float* zt, int64_t n, const int64_t* targets, const float* peer_lse,
-                       const float* peer_z, float* loss, float* lse, float* target_logit, hipStream_t stream);
-// G = w_i (exp(z - lse) - [target]) as two bf16 parts [n][ld] each, zero in the columns n_cols .. ld - 1.
-hipError_t loss_grad(const float* z, int64_t ld, int64_t n, int32_t n_cols, int64_t v0, const int64_t* targets,
-                     const float* lse, const float* d_loss, float grad_scale, uint16_t* g_hi, uint16_t* g_lo,
-                     hipStream_t stream);
+// Blocks of columns of a LossStats product on tiles of `tile` rows.
+int64_t loss_stat_blocks(int64_t N, int32_t tile);
+// Joins the blocks' statistics of one piece of the vocabulary with `run` (f32 pairs
+// [n], unless it is the first piece), into run or, for the last piece, into the
+// losses: see lm_loss_fwd.  zt holds the logits of the targets in [v0, v0 + v_t).
+struct LossJoin {
+  const float2* stats;
+  int32_t n_blocks;
+  float2* run;
+  bool first, last;
+  int64_t n, v0, v_t;
+  const int64_t* targets;
+  const float *zt, *peer_lse, *peer_z;
+  float *loss, *lse, *target_logit;   // target_logit may be null
+};
+hipError_t loss_join(const LossJoin& p, hipStream_t stream);
+// What the bf16 parts of G leave out at the targets, where G is largest:
+// d_hidden (bf16) = dh + (g - 1 part) W[target], d_w[target] += (g - g_parts parts) hidden,
+// g = gt[i] for the targets in [v0, v0 + v_t); rows of one target are added in order.
+struct LossTargets {
+  int64_t n, v0, v_t;
+  int32_t h;
+  const int64_t* targets;
+  const float* gt;
+  int32_t g_parts;
+  const float* dh;
+  const uint16_t *hidden, *w;
+  uint16_t* d_hidden;
+  float* d_w;
+};
+hipError_t loss_finish_dh(const LossTargets& p, hipStream_t stream);
+hipError_t loss_finish_dw(const LossTargets& p, hipStream_t stream);
+// y = the n elements (a multiple of 8) of x, `times` times one behind another (bf16).
+hipError_t repeat_bf16(const uint16_t* x, uint16_t* y, int64_t n, int32_t times, hipStream_t stream);
 hipError_t zero_f32(float* x, int64_t n, hipStream_t stream);      // n a multiple of 4
-// y (bf16) = x, n elements (a multiple of 8).
-hipError_t round_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t stream);
 
 // ---------------------------------------------------------------- embedding
 

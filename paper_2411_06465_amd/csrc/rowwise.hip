@@ -619,83 +619,146 @@ __global__ void __launch_bounds__(256) xent_grad_kernel(const float* __restrict_
 }
 
 // ------------------------------------------------------------------ loss without stored logits
-// One wave per row of a piece of fp32 logits.
+// The logits' product (gemm.hip) leaves a (maximum, sum) pair per row and block of
+// columns, [block][row].  A workgroup joins 64 rows: lane = row, so that loads are
+// whole lines, 16 waves share the blocks.
+constexpr int kJoinWaves = 16;
+__device__ __forceinline__ void join_stats(float& m, float& s, float2 b) {
+  const float top = fmaxf(m, b.x), ref = top == -INFINITY ? 0.f : top;
+  s = s * __expf(m - ref) + b.y * __expf(b.x - ref);
+  m = top;
+}
+__global__ void __launch_bounds__(kJoinWaves * 64) loss_join_kernel(LossJoin p) {
+  __shared__ float2 part[kJoinWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+  const bool ok = row < p.n;
+  float m = -INFINITY, s = 0.f;
+  if (ok) {
+    constexpr int U = 8;                       // loads in flight
+    int b = wave;
+    for (; b + (U - 1) * kJoinWaves < p.n_blocks; b += U * kJoinWaves) {
+      float2 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = p.stats[static_cast<int64_t>(b + u * kJoinWaves) * p.n + row];
+#pragma unroll
+      for (int u = 0; u < U; ++u) join_stats(m, s, v[u]);
+    }
+    for (; b < p.n_blocks; b += kJoinWaves) join_stats(m, s, p.stats[static_cast<int64_t>(b) * p.n + row]);
+  }
+  part[wave][lane] = make_float2(m, s);
+  __syncthreads();
+  if (wave != 0 || !ok) return;
+  for (int w = 1; w < kJoinWaves; ++w) join_stats(m, s, part[w][lane]);
+  if (!p.first) join_stats(m, s, p.run[row]);
+  if (!p.last) {
+    p.run[row] = make_float2(m, s);
+    return;
+  }
+  const int64_t id = p.targets[row];
+  const bool here = id >= p.v0 && id - p.v0 < p.v_t;         // v0 >= 0: an ignored token is nowhere
+  float lse = m + logf(s), z = here ? p.zt[row] : -INFINITY;
+  if (p.target_logit) p.target_logit[row] = z;
+  if (p.peer_lse) {
+    const float q = p.peer_lse[row], big = fmaxf(lse, q), small = fminf(lse, q);
+    lse = big + log1pf(expf(small - big));
+    if (!here) z = p.peer_z[row];
+  }
+  p.lse[row] = lse;
+  p.loss[row] = id >= 0 ? lse - z : 0.f;
+}
 
-// The row's running (maximum, sum) and target logit after one more piece.
-__global__ void __launch_bounds__(256) loss_piece_kernel(const float* __restrict__ z, int64_t ld, int64_t n, int32_t n_cols,
-                                                        int64_t v0, const int64_t* __restrict__ targets,
-                                                        float2* __restrict__ stats, float* __restrict__ zt, int first) {
+// One wave per row: d_hidden = dh + (g - hi) W[target].
+__global__ void __launch_bounds__(256) loss_finish_dh_kernel(LossTargets p) {
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (row >= n) return;
-  const float* zr = z + row * ld;
-  float m = -INFINITY;
-  for (int j = lane; j < n_cols; j += 64) m = fmaxf(m, zr[j]);
+  if (row >= p.n) return;
+  const int64_t id = p.targets[row], t = id - p.v0;
+  const bool here = id >= 0 && t >= 0 && t < p.v_t;
+  float r = 0.f;
+  if (here) {
+    const float g = p.gt[row];
+    r = g - __uint_as_float(static_cast<uint32_t>(f2bf(g)) << 16);
+  }
+  const float* x = p.dh + row * p.h;
+  const uint16_t* w = p.w + (here ? t : 0) * p.h;
+  for (int c = lane * 8; c < p.h; c += 512) {
+    const float4 a = *reinterpret_cast<const float4*>(x + c), b = *reinterpret_cast<const float4*>(x + c + 4);
+    float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (r != 0.f) {
+      float q[8];
+      unpack8(*reinterpret_cast<const u32x4*>(w + c), q);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  float s = 0.f;
-  for (int j = lane; j < n_cols; j += 64) s += __expf(zr[j] - m);
-  s = wave_sum(s);
-  if (lane != 0) return;
-  if (!first) {
-    const float2 old = stats[row];
-    const float big = fmaxf(m, old.x);
-    s = s * __expf(m - big) + old.y * __expf(old.x - big);
-    m = big;
+      for (int j = 0; j < 8; ++j) v[j] = fmaf(r, q[j], v[j]);
+    }
+    *reinterpret_cast<u32x4*>(p.d_hidden + row * p.h + c) = pack8(v);
   }
-  stats[row] = make_float2(m, s);
-  const int64_t t = targets[row] - v0;
-  const bool here = t >= 0 && t < n_cols && targets[row] >= 0;
-  if (here) zt[row] = zr[t];
-  else if (first) zt[row] = -INFINITY;
 }
 
-__global__ void __launch_bounds__(256) loss_finish_kernel(const float2* __restrict__ stats, const float* __restrict__ zt,
-                                                         int64_t n, const int64_t* __restrict__ targets,
-                                                         const float* __restrict__ peer_lse, const float* __restrict__ peer_z,
-                                                         float* __restrict__ loss, float* __restrict__ lse_out,
-                                                         float* __restrict__ z_out) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= n) return;
-  const float2 st = stats[i];
-  float lse = st.x + logf(st.y), z = zt[i];
-  if (z_out) z_out[i] = z;
-  if (peer_lse) {
-    const float p = peer_lse[i], big = fmaxf(lse, p), small = fminf(lse, p);
-    lse = big + log1pf(expf(small - big));
-    if (z == -INFINITY) z = peer_z[i];
+// d_w[target] += what the parts of g leave x hidden.  A workgroup per token (and 2048
+// columns): the first token of a target adds the rows of all of them, in order, so
+// that the sum does not depend on timing.
+constexpr int kScan = 1024;          // tokens compared between two barriers
+__global__ void __launch_bounds__(256) loss_finish_dw_kernel(LossTargets p) {
+  __shared__ float rest[kScan];
+  __shared__ uint64_t hits[kScan / 64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t i = blockIdx.x, id = p.targets[i], t = id - p.v0;
+  if (id < 0 || t < 0 || t >= p.v_t) return;
+  for (int64_t j0 = 0; j0 < i; j0 += kScan) {
+    bool seen = false;
+#pragma unroll
+    for (int u = 0; u < kScan / 256; ++u) {
+      const int64_t j = j0 + u * 256 + tid;
+      seen |= j < i && p.targets[j] == id;
+    }
+    if (__syncthreads_or(seen)) return;
   }
-  lse_out[i] = lse;
-  loss[i] = targets[i] >= 0 ? lse - z : 0.f;
+  const int c = static_cast<int>(blockIdx.y) * 2048 + tid * 8;
+  const bool mine = c < p.h;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int64_t j0 = i; j0 < p.n; j0 += kScan) {
+#pragma unroll
+    for (int u = 0; u < kScan / 256; ++u) {
+      const int k = u * 256 + tid;
+      const bool hit = j0 + k < p.n && p.targets[j0 + k] == id;
+      if (hit) {
+        float g = p.gt[j0 + k];
+        for (int part = 0; part < p.g_parts; ++part) g -= __uint_as_float(static_cast<uint32_t>(f2bf(g)) << 16);
+        rest[k] = g;
+      }
+      const uint64_t mask = __builtin_amdgcn_ballot_w64(hit);
+      if (lane == 0) hits[k >> 6] = mask;
+    }
+    __syncthreads();
+    if (mine)
+      for (int q = 0; q < kScan / 64; ++q)
+        for (uint64_t left = hits[q]; left; left &= left - 1) {       // the same for the whole workgroup
+          const int k = q * 64 + __builtin_ctzll(left);
+          const float s = rest[k];
+          float v[8];
+          unpack8(*reinterpret_cast<const u32x4*>(p.hidden + (j0 + k) * p.h + c), v);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) acc[u] = fmaf(s, v[u], acc[u]);
+        }
+    __syncthreads();
+  }
+  if (!mine) return;
+  float* d = p.d_w + t * p.h + c;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) d[u] += acc[u];
 }
 
-__global__ void __launch_bounds__(256) loss_grad_kernel(const float* __restrict__ z, int64_t ld, int64_t n, int32_t n_cols,
-                                                       int64_t v0, const int64_t* __restrict__ targets,
-                                                       const float* __restrict__ lse, const float* __restrict__ d_loss,
-                                                       float grad_scale, uint16_t* __restrict__ g_hi,
-                                                       uint16_t* __restrict__ g_lo) {
+__global__ void __launch_bounds__(256) repeat_bf16_kernel(const uint16_t* __restrict__ x, uint16_t* __restrict__ y, int64_t n8,
+                                                         int32_t times) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= n * ld) return;
-  const int64_t row = i / ld, j = i - row * ld, t = targets[row];
-  const float w = t < 0 ? 0.f : grad_scale * (d_loss ? d_loss[row] : 1.f);
-  float g = 0.f;
-  if (j < n_cols && t >= 0) g = w * (__expf(z[i] - lse[row]) - (t - v0 == j ? 1.f : 0.f));
-  const uint16_t hi = f2bf(g);
-  g_hi[i] = hi;
-  g_lo[i] = f2bf(g - __uint_as_float(static_cast<uint32_t>(hi) << 16));
+  if (i >= n8) return;
+  const u32x4 v = reinterpret_cast<const u32x4*>(x)[i];
+  for (int k = 0; k < times; ++k) reinterpret_cast<u32x4*>(y)[i + k * n8] = v;
 }
-
 __global__ void __launch_bounds__(256) zero_f32_kernel(float* __restrict__ x, int64_t n4) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (i < n4) reinterpret_cast<float4*>(x)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-}
-
-__global__ void __launch_bounds__(256) round_bf16_kernel(const float* __restrict__ x, uint16_t* __restrict__ y, int64_t n8) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= n8) return;
-  const float4 a = reinterpret_cast<const float4*>(x)[2 * i], b = reinterpret_cast<const float4*>(x)[2 * i + 1];
-  const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  reinterpret_cast<u32x4*>(y)[i] = pack8(v);
 }
 
 // ------------------------------------------------------------------ embedding
@@ -1000,31 +1063,25 @@ hipError_t rope_rotate(const RopeRotate& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t loss_piece(const float* z, int64_t ld, int64_t n, int32_t n_cols, int64_t v0, const int64_t* targets,
-                      float2* stats, float* zt, bool first, hipStream_t stream) {
-  hipLaunchKernelGGL(loss_piece_kernel, dim3(static_cast<unsigned>((n + 3) / 4)), dim3(256), 0, stream, z, ld, n, n_cols, v0,
-                     targets, stats, zt, first ? 1 : 0);
+hipError_t loss_join(const LossJoin& p, hipStream_t stream) {
+  hipLaunchKernelGGL(loss_join_kernel, dim3(static_cast<unsigned>((p.n + 63) / 64)), dim3(kJoinWaves * 64), 0, stream, p);
   return hipGetLastError();
 }
-hipError_t loss_finish(const float2* stats, const float* zt, int64_t n, const int64_t* targets, const float* peer_lse,
-                       const float* peer_z, float* loss, float* lse, float* target_logit, hipStream_t stream) {
-  hipLaunchKernelGGL(loss_finish_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, stream, stats, zt, n,
-                     targets, peer_lse, peer_z, loss, lse, target_logit);
+hipError_t loss_finish_dh(const LossTargets& p, hipStream_t stream) {
+  hipLaunchKernelGGL(loss_finish_dh_kernel, dim3(static_cast<unsigned>((p.n + 3) / 4)), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
-hipError_t loss_grad(const float* z, int64_t ld, int64_t n, int32_t n_cols, int64_t v0, const int64_t* targets,
-                     const float* lse, const float* d_loss, float grad_scale, uint16_t* g_hi, uint16_t* g_lo,
-                     hipStream_t stream) {
-  hipLaunchKernelGGL(loss_grad_kernel, dim3(static_cast<unsigned>((n * ld + 255) / 256)), dim3(256), 0, stream, z, ld, n,
-                     n_cols, v0, targets, lse, d_loss, grad_scale, g_hi, g_lo);
+hipError_t repeat_bf16(const uint16_t* x, uint16_t* y, int64_t n, int32_t times, hipStream_t stream) {
+  hipLaunchKernelGGL(repeat_bf16_kernel, dim3(static_cast<unsigned>((n / 8 + 255) / 256)), dim3(256), 0, stream, x, y, n / 8,
+                     times);
   return hipGetLastError();
 }
 hipError_t zero_f32(float* x, int64_t n, hipStream_t stream) {
   hipLaunchKernelGGL(zero_f32_kernel, dim3(static_cast<unsigned>((n / 4 + 255) / 256)), dim3(256), 0, stream, x, n / 4);
   return hipGetLastError();
 }
-hipError_t round_bf16(const float* x, uint16_t* y, int64_t n, hipStream_t stream) {
-  hipLaunchKernelGGL(round_bf16_kernel, dim3(static_cast<unsigned>((n / 8 + 255) / 256)), dim3(256), 0, stream, x, y, n / 8);
+hipError_t loss_finish_dw(const LossTargets& p, hipStream_t stream) {
+  hipLaunchKernelGGL(loss_finish_dw_kernel, dim3(static_cast<unsigned>(p.n), (p.h + 2047) / 2048), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
