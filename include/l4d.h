@@ -483,9 +483,9 @@ int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void
  * 2^-18 of an element); what the parts leave at the target, where G is largest, is
  * added in fp32.
  * The workspace holds 8 bytes per token and 64 columns in the forward, 4 per token
- * and column in the backward, of a piece of the vocabulary: what 2^25 tokens x
- * columns take (268 MB) or, for many tokens, 65536 and 4096 columns; and the fp32
- * d_hidden.
+ * and column in the backward (6 with at most 256 tokens), of a piece of the
+ * vocabulary: 2^31 and 2^26 tokens x columns (268 MB) or, for many tokens, 65536 and
+ * 8192 columns.  The backward adds fp32 d_hidden and two or three copies of hidden.
  * Requirements: h % 8 == 0, h <= 8192; hidden, w_lm and d_hidden 16-byte aligned;
  * N <= 2^20, v_t <= 2^24; finite hidden rows also of ignored tokens (their zero
  * weights multiply them in d_w_lm).  N == 0 launches nothing.

@@ -1537,7 +1537,11 @@ extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const 
 
 namespace {
 // Columns of a piece of the vocabulary: forward (its statistics: 8 bytes for 64
-// columns) and backward (its gradient: 4 bytes a column).
+// columns) and backward (its gradient: 4 bytes a column).  More tokens take fewer
+// columns, down to 8192: narrower pieces leave d_w's product too few tiles and add
+// fp32 d_hidden once more each (forward and backward with pieces of 4096, 8192, 32768
+// columns: 8192 tokens, hidden 4096, 32064 columns 9.09, 8.92, 9.00 ms; 32768 tokens,
+// hidden 2048, 32000 columns 21.8, 19.2, 19.1; 2048 tokens, 128256 columns 11.0, 10.2, 9.5).
 int64_t loss_piece_cols(int64_t n, int64_t v_t, int64_t least, int64_t elements) {
   const int64_t cols = std::max(least, elements / std::max<int64_t>(n, 1) / 256 * 256);
   return std::min(cols, (v_t + 7) / 8 * 8);
@@ -1557,7 +1561,7 @@ constexpr int kDxSplits = 8;
 LossWs plan_loss(int64_t n, int64_t h, int64_t v_t) {
   LossWs w{};
   w.fwd_piece = loss_piece_cols(n, v_t, 65536, (int64_t)1 << 31);
-  w.bwd_piece = loss_piece_cols(n, v_t, 4096, (int64_t)1 << 26);
+  w.bwd_piece = loss_piece_cols(n, v_t, 8192, (int64_t)1 << 26);
   w.parts = n <= kThreeParts ? 3 : 2;
   const GemmPlan dx = gemm_plan(n, h, std::min(w.bwd_piece, v_t), EpiKind::AccF32, kDxSplits);
   w.dx_splits = dx.splits;

@@ -293,6 +293,10 @@ struct RopeRotate {
   int32_t d_h, rot;
   int32_t f32, interleaved, inverse;
   float amplitude;
+  // set by rope_rotate
+  int32_t parts;                 // waves that share a row
+  int32_t units[2], first_rest[2];   // units per head of each tensor; those from first_rest on are copied
+  uint32_t magic[2];             // ceil(2^32 / units)
   double turns[kMaxRopePairs];   // f_j / 2 pi
 };
 hipError_t rope_rotate(const RopeRotate& p, hipStream_t stream);
