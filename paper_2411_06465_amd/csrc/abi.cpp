@@ -1415,7 +1415,7 @@ struct AttnRows {        // one tensor of a call
   const void* p;
   int64_t ld, heads;
 };
-int attn_shape(const l4d_attn* at, int64_t tokens, PackedAttn* p) {
+int attn_shape(const l4d_attn* at, int64_t tokens, int64_t n_seqs, PackedAttn* p) {
   if (!at) return fail(L4D_EINVAL, "attn is required");
   if (at->head_dim != 64 && at->head_dim != 128)
     return fail(L4D_EINVAL, "head dim %lld unsupported (64 or 128)", (long long)at->head_dim);
@@ -1426,7 +1426,7 @@ int attn_shape(const l4d_attn* at, int64_t tokens, PackedAttn* p) {
   p->kv_heads = (int32_t)at->n_kv_heads;
   p->d_h = (int32_t)at->head_dim;
   p->scale = at->scale > 0.f ? at->scale : 1.0f / std::sqrt((float)at->head_dim);
-  p->n_split = attn_packed_splits(tokens, at->n_heads, at->n_kv_heads);
+  p->n_split = attn_packed_splits(tokens, n_seqs, at->n_heads, at->n_kv_heads);
   return L4D_OK;
 }
 int attn_rows(const AttnRows* t, int n, int64_t d) {
@@ -1461,7 +1461,7 @@ PackedWs plan_packed(const PackedAttn& p, int64_t tokens) {
 extern "C" int l4d_attn_packed_workspace_bytes(const l4d_attn* at, int64_t tokens, uint64_t* bytes) {
   if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "tokens must lie in 0 .. 2^30");
   PackedAttn p{};
-  int rc = attn_shape(at, tokens, &p);
+  int rc = attn_shape(at, tokens, 1, &p);     // one document: the most slices
   if (rc) return rc;
   if (bytes) *bytes = align_up(plan_packed(p, tokens).total);
   return L4D_OK;
@@ -1473,7 +1473,7 @@ extern "C" int attn_packed_fwd(const l4d_attn* at, const l4d_packing* pk, const 
   int rc = check_packing(pk);
   if (rc) return rc;
   PackedAttn p{};
-  if ((rc = attn_shape(at, pk->tokens, &p))) return rc;
+  if ((rc = attn_shape(at, pk->tokens, pk->n_seqs, &p))) return rc;
   const AttnRows t[4] = {{"q", q, q_ld, at->n_heads}, {"k", k, k_ld, at->n_kv_heads}, {"v", v, v_ld, at->n_kv_heads},
                          {"o", o, o_ld, at->n_heads}};
   if ((rc = attn_rows(t, 4, at->head_dim)) || (rc = attn_distinct(t, 4, 3))) return rc;
@@ -1498,7 +1498,7 @@ extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const 
   int rc = check_packing(pk);
   if (rc) return rc;
   PackedAttn p{};
-  if ((rc = attn_shape(at, pk->tokens, &p))) return rc;
+  if ((rc = attn_shape(at, pk->tokens, pk->n_seqs, &p))) return rc;
   const int64_t a = at->n_heads, g = at->n_kv_heads;
   const AttnRows t[8] = {{"q", q, q_ld, a}, {"k", k, k_ld, g}, {"v", v, v_ld, g}, {"o", o, o_ld, a},
                          {"d_o", d_o, do_ld, a}, {"dq", dq, dq_ld, a}, {"dk", dk, dk_ld, g}, {"dv", dv, dv_ld, g}};

@@ -1126,19 +1126,28 @@ hipError_t attn_bwd(const AttnParams& p, int part, hipStream_t stream) {
   return hipErrorInvalidValue;
 }
 
-// The rule of attn_bwd_splits, with the blocks that full documents would give.
-int attn_packed_splits(int64_t tokens, int64_t heads, int64_t kv_heads) {
-  const int64_t group = heads / kv_heads, base = (tokens + 127) / 128 * kv_heads;
+// Slices of a kv head's query heads in the dK/dV pass: one workgroup runs on a CU at
+// a time, and the longest document's first keys make the longest one, so the heads
+// are cut (by 2, by 4) until there are two workgroups a CU, at the price of fp32
+// partial sums, which also push the next kernels' inputs out of the caches.  Four a
+// CU pay where documents are long (the sums grow with the rows, the work with the
+// pairs).  Forward and backward in 1, 2, 4 slices: 32768 tokens in 6 documents, 8/1
+// heads of 128: 4.71, 3.32, 3.05 ms; 8192 tokens in 23, 32/8 heads: 441, 456, 510 us;
+// 16384 tokens in 160, 16/4 heads of 64: 216, 215, 255.  Cutting only the blocks that
+// turn out long on the GPU was slower: the empty workgroups of the other slices
+// upset the order and the spread over the XCDs.
+int attn_packed_splits(int64_t tokens, int64_t n_seqs, int64_t heads, int64_t kv_heads) {
+  const int64_t base = (tokens + 127) / 128 * kv_heads, want = tokens >= 2048 * n_seqs ? 1024 : 512;
+  const int most = packed_hpb(static_cast<int>(heads), static_cast<int>(kv_heads));
   int n = 1;
-  while (base * n < 512 && n < group && group % (2 * n) == 0) n *= 2;
+  while (base * n < want && n < most) n *= 2;
   return n;
 }
 
 bool attn_packed_fits(const PackedAttn& p) {
   // a grid holds less than 2^32 threads; slots of the smallest query blocks (32 rows) and of the key blocks
   const int64_t q = packed_slots(p, 32) * p.heads, k = packed_slots(p, 128) * p.heads;
-  const int64_t r = static_cast<int64_t>(p.pk.tokens) * p.kv_heads * (p.d_h / 8);
-  return q < (int64_t{1} << 24) && k < (int64_t{1} << 23) && r < (int64_t{1} << 32);
+  return q < (int64_t{1} << 24) && k < (int64_t{1} << 23);
 }
 
 hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream) {

@@ -37,14 +37,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int rbase = 4 * (lane >> 5);
   const LaneAddr la = lane_addr<D>(lane);
 
-  bf16x8 qf[D / 16];
-  {
-    const uint16_t* qb = p.q + static_cast<int64_t>(min(my_q, blk.hi - 1)) * p.q_ld + hq * D;
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qb + (2 * kk + (lane >> 5)) * 8);
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) settle(qf[kk]);
-  }
   const float c = p.scale * kLog2e;
   float m_run = -INFINITY, l_run = 0.f;
   f32x16 o[D / 32];
@@ -54,6 +46,23 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   const TileCopy<D, KT> copy_k(p.k_ld, wave, lane), copy_v(p.v_ld, wave, lane);
   const uint32_t ka0 = lds_addr(k0), ka1 = lds_addr(k1), va0 = lds_addr(v0), va1 = lds_addr(v1);
   const int n_tiles = (n_keys + KT - 1) / KT;
+  const auto copy_tile = [&](const TileCopy<D, KT>& copy, const uint16_t* base, int64_t ld, int t, uint32_t lds)
+      __attribute__((always_inline)) {
+    const int64_t row = blk.lo + t * KT;
+    if (t < n_tiles) copy(lds, base + row * ld + hk * D, blk.hi - static_cast<int>(row));
+  };
+  // the first tiles' copies, and under them the queries
+  copy_tile(copy_k, p.k, p.k_ld, 0, ka0);
+  copy_tile(copy_v, p.v, p.v_ld, 0, va0);
+  copy_tile(copy_k, p.k, p.k_ld, 1, ka1);
+  bf16x8 qf[D / 16];
+  {
+    const uint16_t* qb = p.q + static_cast<int64_t>(min(my_q, blk.hi - 1)) * p.q_ld + hq * D;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qb + (2 * kk + (lane >> 5)) * 8);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) settle(qf[kk]);
+  }
   const auto row_max = [](const f32x16 (&s)[2]) __attribute__((always_inline)) {
     float m = __builtin_fmaxf(s[0][0], s[0][1]);
 #pragma unroll
@@ -141,14 +150,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 
   // While tile j is in step, V_j and K_(j+1) are in use, V_(j+1) and K_(j+2) land in
   // the buffers that V_(j-1) and K_j held.
-  const auto copy_tile = [&](const TileCopy<D, KT>& copy, const uint16_t* base, int64_t ld, int t, uint32_t lds)
-      __attribute__((always_inline)) {
-    const int64_t row = blk.lo + t * KT;
-    if (t < n_tiles) copy(lds, base + row * ld + hk * D, blk.hi - static_cast<int>(row));
-  };
-  copy_tile(copy_k, p.k, p.k_ld, 0, ka0);
-  copy_tile(copy_v, p.v, p.v_ld, 0, va0);
-  copy_tile(copy_k, p.k, p.k_ld, 1, ka1);
   wait_copies<0>();
   ring_barrier();
   f32x16 sa[2] = {f32x16{}, f32x16{}}, sb[2];
@@ -217,7 +218,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int rbase = 4 * (lane >> 5);
   const LaneAddr la = lane_addr<D>(lane);
 
-  bf16x8 qf[D / 16], dof[D / 16];
+  const TileCopy<D, KQ> copy_k(p.k_ld, wave, lane), copy_v(p.v_ld, wave, lane);
+  const int n_tiles = (n_keys + KQ - 1) / KQ;
+  const auto issue = [&](int t, int b) __attribute__((always_inline)) {
+    const int64_t r0 = blk.lo + t * KQ;
+    const int valid = blk.hi - static_cast<int>(r0);
+    copy_k(lds_addr(kbuf[b]), p.k + r0 * p.k_ld + hk * D, valid);
+    copy_v(lds_addr(vbuf[b]), p.v + r0 * p.v_ld + hk * D, valid);
+  };
+  issue(0, 0);
+  bf16x8 qf[D / 16], dof[D / 16];      // under the first tile's copies
   float my_delta = 0.f;
   const int row = min(my_q, blk.hi - 1);
   {
@@ -253,15 +263,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dq[i] = f32x16{};
 
-  const TileCopy<D, KQ> copy_k(p.k_ld, wave, lane), copy_v(p.v_ld, wave, lane);
-  const int n_tiles = (n_keys + KQ - 1) / KQ;
-  const auto issue = [&](int t, int b) __attribute__((always_inline)) {
-    const int64_t r0 = blk.lo + t * KQ;
-    const int valid = blk.hi - static_cast<int>(r0);
-    copy_k(lds_addr(kbuf[b]), p.k + r0 * p.k_ld + hk * D, valid);
-    copy_v(lds_addr(vbuf[b]), p.v + r0 * p.v_ld + hk * D, valid);
-  };
-  issue(0, 0);
   for (int t = 0; t < n_tiles; ++t) {
     const int b = t & 1;
     wait_copies<0>();
@@ -343,12 +344,13 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = wave & 3, role = wave >> 2;
-  const int group = p.heads / p.kv_heads, hps = group / p.n_split;
+  const int group = p.heads / p.kv_heads;
   const int nyz = p.kv_heads * p.n_split;
   const int slot = static_cast<int>(blockIdx.x) / nyz, yz = static_cast<int>(blockIdx.x) % nyz;
-  const int hk = yz / p.n_split, split = yz % p.n_split, head0 = hk * group + split * hps;
+  const int hk = yz / p.n_split, split = yz % p.n_split, hps = group / p.n_split, head0 = hk * group + split * hps;
   const SeqBlock blk = seq_block(p.pk, slot, 128, lane);
   if (blk.row0 >= blk.hi) return;
+  const int n_rows = blk.hi - blk.row0, n_qt = (n_rows + QT - 1) / QT;
   const int grp_k0 = blk.row0 + grp * 32;
   const int my_key = grp_k0 + (lane & 31);
   const bool key_ok = my_key < blk.hi;
@@ -362,20 +364,10 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   const auto pick = [&](uint64_t a, uint64_t b) { return a + ((b - a) & role_mask); };
   const auto addr = [](const void* x) { return reinterpret_cast<uint64_t>(x); };
 
-  bf16x8 kv[D / 16];                     // role 0: K rows, role 1: V rows of the group's keys
-  {
-    const uint16_t* src = reinterpret_cast<const uint16_t*>(pick(addr(p.k), addr(p.v))) +
-                          static_cast<int64_t>(pick(p.k_ld, p.v_ld)) * min(my_key, blk.hi - 1) + hk * D;
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) kv[kk] = *reinterpret_cast<const bf16x8*>(src + (2 * kk + (lane >> 5)) * 8);
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) settle(kv[kk]);
-  }
   f32x16 acc[D / 32];                    // role 0: dV^T, role 1: dK^T (d rows, the lane's key)
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
   const float c = p.scale * kLog2e;
-  const int n_rows = blk.hi - blk.row0, n_qt = (n_rows + QT - 1) / QT;
   // waves 0-3 copy the Q tiles and their lse, waves 4-7 the dO tiles and delta
   const int64_t ld = pick(p.q_ld, p.do_ld);
   const TileCopy<D, QT> copy(ld, grp, lane);
@@ -400,6 +392,15 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
     copy_qt = more ? (wrap ? 0 : copy_qt + 1) : copy_qt;
     copy_left -= more;
   };
+  bf16x8 kv[D / 16];                     // role 0: K rows, role 1: V rows of the group's keys
+  {
+    const uint16_t* kv_row = reinterpret_cast<const uint16_t*>(pick(addr(p.k), addr(p.v))) +
+                          static_cast<int64_t>(pick(p.k_ld, p.v_ld)) * min(my_key, blk.hi - 1) + hk * D;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) kv[kk] = *reinterpret_cast<const bf16x8*>(kv_row + (2 * kk + (lane >> 5)) * 8);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) settle(kv[kk]);
+  }
   f32x16 s;                  // role 0: S -> P of a tile, role 1: its dP - delta
   bf16x8 x[2];               // role 0: P, role 1: dS (bf16)
   // role 0: P = exp(S - lse) of tile qt from its scores in s; bf16 into x, fp32 into handover hb
@@ -550,28 +551,29 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
           u32x2{pack2(acc[dt][4 * jj], acc[dt][4 * jj + 1]), pack2(acc[dt][4 * jj + 2], acc[dt][4 * jj + 3])};
 }
 
-// dK, dV = the sum of the slices' fp32 parts in order, for the rows that belong to
-// a document.  Eight columns per thread.
+// dK, dV = the sum of the slices' fp32 parts in order.
 template <int D>
 __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
-  const int64_t idx = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  const int64_t per_row = static_cast<int64_t>(p.kv_heads) * (D / 8);
-  const int64_t first = seq_start(p.pk, 0), end = seq_start(p.pk, p.pk.n_seqs);
-  const int64_t row = idx / per_row;
-  if (row >= p.pk.tokens || row < first || row >= end) return;
-  const int64_t col = idx % per_row * 8;                 // hk * D + d
+  const int slot = static_cast<int>(blockIdx.x), hk = static_cast<int>(blockIdx.y);
+  const SeqBlock blk = seq_block(p.pk, slot, 128, threadIdx.x & 63);
+  if (blk.row0 >= blk.hi) return;
   const int64_t step = static_cast<int64_t>(p.pk.tokens) * p.kv_heads * D;
+  constexpr int C = D / 8;                               // eight columns per thread
+  for (int u = threadIdx.x; u < min(blk.hi - blk.row0, 128) * C; u += 256) {
+    const int64_t row = blk.row0 + u / C;
+    const int col = hk * D + u % C * 8;
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const float* src = p.dkv_partial + which * p.n_split * step + row * p.kv_heads * D + col;
-    float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
-    for (int s = 1; s < p.n_split; ++s) {
-      const float4 x = *reinterpret_cast<const float4*>(src + s * step), y = *reinterpret_cast<const float4*>(src + s * step + 4);
-      a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-      b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+    for (int which = 0; which < 2; ++which) {
+      const float* src = p.dkv_partial + which * p.n_split * step + row * p.kv_heads * D + col;
+      float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
+      for (int s = 1; s < p.n_split; ++s) {
+        const float4 x = *reinterpret_cast<const float4*>(src + s * step), y = *reinterpret_cast<const float4*>(src + s * step + 4);
+        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+        b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+      }
+      uint16_t* dst = which ? p.dv + row * p.dv_ld + col : p.dk + row * p.dk_ld + col;
+      *reinterpret_cast<u32x4*>(dst) = u32x4{pack2(a.x, a.y), pack2(a.z, a.w), pack2(b.x, b.y), pack2(b.z, b.w)};
     }
-    uint16_t* dst = which ? p.dv + row * p.dv_ld + col : p.dk + row * p.dk_ld + col;
-    *reinterpret_cast<u32x4*>(dst) = u32x4{pack2(a.x, a.y), pack2(a.z, a.w), pack2(b.x, b.y), pack2(b.z, b.w)};
   }
 }
 
@@ -598,8 +600,8 @@ hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
     hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, grid, dim3(512), 0, stream, p);
   } else {
     if (p.n_split == 1) return hipSuccess;
-    const int64_t n = static_cast<int64_t>(p.pk.tokens) * p.kv_heads * (D / 8);
-    hipLaunchKernelGGL(attn_packed_reduce_kernel<D>, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, stream, p);
+    const dim3 grid(static_cast<unsigned>(packed_slots(p, 128)), p.kv_heads);
+    hipLaunchKernelGGL(attn_packed_reduce_kernel<D>, grid, dim3(256), 0, stream, p);
   }
   return hipGetLastError();
 }

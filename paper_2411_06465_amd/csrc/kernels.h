@@ -270,7 +270,7 @@ struct PackedAttn {
   int32_t n_split;          // slices of a kv head's query heads in the dK/dV pass
   float* dkv_partial;       // n_split > 1: dK [n_split][tokens][kv_heads][d_h], then dV
 };
-int attn_packed_splits(int64_t tokens, int64_t heads, int64_t kv_heads);
+int attn_packed_splits(int64_t tokens, int64_t n_seqs, int64_t heads, int64_t kv_heads);
 bool attn_packed_fits(const PackedAttn& p);      // every launch within the grid limits
 hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream);
 // part 2: dQ and delta; 1: dK, dV (after part 2); 3: the sum of the slices (n_split > 1).

@@ -31,10 +31,27 @@ __device__ __forceinline__ int last_not_above(int n_seqs, int x, int lane, Key k
 
 struct SeqRows {
   int lo, hi;      // the document's rows; lo == hi: none
+  int i;           // its index, -1: none
 };
-__device__ __forceinline__ SeqRows seq_rows(const Packing& p, int i) {
-  const int lo = seq_start(p, i);
-  return SeqRows{__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(max(lo, seq_start(p, i + 1)))};
+// The last document i with key(starts[i], i) <= x, key nondecreasing in i.  Up to 63
+// documents one load brings all starts, and the lanes that hold its rows hand them out.
+template <class Key>
+__device__ __forceinline__ SeqRows last_seq(const Packing& p, int x, int lane, Key key) {
+  if (p.n_seqs < 64) {
+    const int v = seq_start(p, min(lane, p.n_seqs));
+    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < p.n_seqs && key(v, lane) <= x));
+    if (c == 0) return SeqRows{0, 0, -1};
+    const int lo = __builtin_amdgcn_readlane(v, c - 1), hi = __builtin_amdgcn_readlane(v, c);
+    return SeqRows{lo, max(lo, hi), c - 1};
+  }
+  const int i = last_not_above(p.n_seqs, x, lane, [&](int j) { return key(seq_start(p, j), j); });
+  if (i < 0) return SeqRows{0, 0, -1};
+  const int lo = __builtin_amdgcn_readfirstlane(seq_start(p, i)), hi = __builtin_amdgcn_readfirstlane(seq_start(p, i + 1));
+  return SeqRows{lo, max(lo, hi), i};
+}
+// The document of a row; hi <= row: none.
+__device__ __forceinline__ SeqRows seq_of_row(const Packing& p, int row, int lane) {
+  return last_seq(p, row, lane, [](int v, int) { return v; });
 }
 
 // Blocks of `rows` rows that never cross a document: document i owns the slots
@@ -47,10 +64,9 @@ struct SeqBlock {
   int row0;        // the block's first row; hi <= row0: no block in this slot
 };
 __device__ __forceinline__ SeqBlock seq_block(const Packing& p, int slot, int rows, int lane) {
-  const int i = last_not_above(p.n_seqs, slot, lane, [&](int j) { return seq_start(p, j) / rows + j; });
-  if (i < 0) return SeqBlock{0, 0, 0};
-  const SeqRows s = seq_rows(p, i);
-  const int t = slot - (s.lo / rows + i);
+  const SeqRows s = last_seq(p, slot, lane, [rows](int v, int j) { return v / rows + j; });
+  if (s.i < 0) return SeqBlock{0, 0, 0};
+  const int t = slot - (s.lo / rows + s.i);
   if (t >= (s.hi - s.lo + rows - 1) / rows) return SeqBlock{0, 0, 0};
   return SeqBlock{s.lo, s.hi, s.lo + t * rows};
 }

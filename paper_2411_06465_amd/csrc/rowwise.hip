@@ -137,9 +137,7 @@ __global__ void __launch_bounds__(256) rope_rotate_kernel(RopeRotate p) {
   if (row >= p.tokens) return;
   int64_t pos = row;
   if (p.pk.n_seqs >= 0) {
-    const int i = last_not_above(p.pk.n_seqs, row, lane, [&](int j) { return seq_start(p.pk, j); });
-    if (i < 0) return;
-    const SeqRows s = seq_rows(p.pk, i);
+    const SeqRows s = seq_of_row(p.pk, row, lane);
     if (row >= s.hi) return;
     pos = row - s.lo;
   }
