@@ -458,6 +458,28 @@ int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void
                     int64_t dv_ld, l4d_arena* arena, void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * The layer over packed documents
+ *
+ * llama_layer_fwd / llama_layer_bwd with one row of packed documents as the
+ * micro-batch: attention stays within documents and positions count from their
+ * first rows.  par->micro_batch and par->cp must be 1 and par->seq equal
+ * packing->tokens; TP with sequence parallelism works as in those calls.  rope:
+ * NULL = the model's plain RoPE, else whole heads in the half layout with any
+ * scaling.  Rows of no document get zero context (their rows of y and dx are those of
+ * a layer without attention), so rows whose dy is zero add nothing to any gradient.
+ * The backward takes the stash of the packed forward, with the same packing and rope;
+ * workspace and stash are those of the unpacked calls.
+ * ---------------------------------------------------------------------- */
+int llama_layer_packed_fwd(const l4d_model* model, const l4d_parallel* par, const l4d_packing* packing,
+                           const l4d_rope* rope, const l4d_layer_weights* w, const void* x,
+                           const l4d_peer_inputs* peers, const l4d_peer_outputs* sends, void* y, l4d_arena* arena,
+                           l4d_stash** stash_out, void* hip_stream);
+int llama_layer_packed_bwd(const l4d_model* model, const l4d_parallel* par, const l4d_packing* packing,
+                           const l4d_rope* rope, const l4d_layer_weights* w, const l4d_peer_inputs* peers,
+                           const l4d_peer_outputs* sends, l4d_stash* stash, const void* dy, void* dx,
+                           const l4d_layer_grads* dw, l4d_arena* arena, void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * LM-head cross-entropy without stored logits
  *
  * Forward and backward of the loss of lm_head_xent for any number of tokens and

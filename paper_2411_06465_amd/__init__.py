@@ -129,6 +129,12 @@ def lib():
             "attn_packed_fwd": ([C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64, P, P], C.c_int),
             "attn_packed_bwd": ([C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64, P, P, i64,
                                  P, i64, P, i64, P, i64, P, P], C.c_int),
+            "llama_layer_packed_fwd": ([C.POINTER(Model), C.POINTER(Parallel), C.POINTER(PackingC), C.POINTER(Rope),
+                                        C.POINTER(LayerWeights), P, C.POINTER(PeerInputs), C.POINTER(PeerOutputs), P,
+                                        P, C.POINTER(P), P], C.c_int),
+            "llama_layer_packed_bwd": ([C.POINTER(Model), C.POINTER(Parallel), C.POINTER(PackingC), C.POINTER(Rope),
+                                        C.POINTER(LayerWeights), C.POINTER(PeerInputs), C.POINTER(PeerOutputs), P, P,
+                                        P, C.POINTER(LayerGrads), P, P], C.c_int),
             "l4d_attn_packed_workspace_bytes": ([C.POINTER(Attn), i64, C.POINTER(u64)], C.c_int),
             "l4d_lm_loss_workspace_bytes": ([i64, i64, i64, C.POINTER(u64), C.POINTER(u64)], C.c_int),
             "lm_loss_fwd": ([i64, i64, i64, i64, P, P, P, P, P, P, P, P, P, P], C.c_int),
@@ -494,6 +500,30 @@ def attn_packed_bwd(q, k, v, o, lse, d_o, dq, dk, dv, packing, arena, scale=0.0,
     with device:
         _check(lib().attn_packed_bwd(C.byref(Attn(a, g, d, scale)), C.byref(packing.c), *args[:8], _ptr(lse), *args[8:],
                                      arena.h, s))
+
+
+def llama_layer_packed_fwd(model, par, weights, x, y, arena, packing, rope=None, peers=None, sends=None, stream=None):
+    """llama_layer_fwd over one row of packed documents; returns the Stash for llama_layer_packed_bwd."""
+    st = C.c_void_p()
+    pi, so = _peers(peers), _sends(sends)
+    device, s = _on(x, stream)
+    with device:
+        _check(lib().llama_layer_packed_fwd(C.byref(model), C.byref(par), C.byref(packing.c),
+                                            None if rope is None else C.byref(rope), C.byref(_weights(weights)), _ptr(x),
+                                            C.byref(pi), C.byref(so), _ptr(y), arena.h, C.byref(st), s))
+    return Stash(st, arena)
+
+
+def llama_layer_packed_bwd(model, par, weights, stash, dy, dx, grads, arena, packing, rope=None, peers=None, sends=None,
+                           stream=None):
+    g = LayerGrads(*[grads[n].data_ptr() for n in ("norm1", "qkv", "o", "norm2", "gate_up", "down")])
+    pi, so = _peers(peers), _sends(sends)
+    device, s = _on(dy, stream)
+    with device:
+        _check(lib().llama_layer_packed_bwd(C.byref(model), C.byref(par), C.byref(packing.c),
+                                            None if rope is None else C.byref(rope), C.byref(_weights(weights)),
+                                            C.byref(pi), C.byref(so), stash.h, _ptr(dy), _ptr(dx), C.byref(g), arena.h, s))
+    stash.h = None
 
 
 # ------------------------------------------------------------------ loss without stored logits

@@ -416,6 +416,7 @@ struct l4d_stash {
   Shard shape;
   int kind = kLayerStash;
   int count = L4D_STASH_COUNT;
+  bool packed = false;       // a layer call over packed documents
 };
 
 namespace {
@@ -783,14 +784,225 @@ int check_peers(const Shard& x, const l4d_peer_inputs* pi, bool bwd) {
 }
 }  // namespace
 
+// ============================================================== packed documents: checks and plans
+
+namespace {
+int check_packing(const l4d_packing* pk) {
+  if (!pk) return fail(L4D_EINVAL, "packing is required");
+  if (pk->tokens < 0 || pk->tokens > (int64_t)1 << 30 || pk->n_seqs < 0 || pk->n_seqs > (int64_t)1 << 30)
+    return fail(L4D_EINVAL, "packing: tokens and n_seqs must lie in 0 .. 2^30");
+  if (pk->n_seqs > 0 && !pk->starts) return fail(L4D_EINVAL, "packing: starts is required");
+  if (reinterpret_cast<uintptr_t>(pk->starts) % 8) return fail(L4D_EINVAL, "packing: starts must be 8-byte aligned");
+  return L4D_OK;
+}
+Packing device_packing(const l4d_packing* pk) {
+  return Packing{pk->starts, (int32_t)pk->n_seqs, (int32_t)pk->tokens};
+}
+
+// ------------------------------------------------------------ rotary positions
+
+// f_j / 2 pi of every pair, in double.
+int rope_turns(const l4d_rope* r, double* turns) {
+  constexpr double kTwoPi = 6.283185307179586476925286766559;
+  if (r->head_dim < 2 || r->head_dim > 2 * kMaxRopePairs) return fail(L4D_EINVAL, "rope: head_dim must lie in 2 .. 512");
+  if (r->rot_dim < 2 || r->rot_dim > r->head_dim || r->rot_dim % 2)
+    return fail(L4D_EINVAL, "rope: rot_dim must be even and lie in 2 .. head_dim");
+  if (r->layout != L4D_ROPE_HALF && r->layout != L4D_ROPE_INTERLEAVED) return fail(L4D_EINVAL, "rope: unknown layout");
+  if (r->scaling < L4D_ROPE_PLAIN || r->scaling > L4D_ROPE_RAMP) return fail(L4D_EINVAL, "rope: unknown scaling");
+  if (!(r->base > 1.0) || !std::isfinite(r->base)) return fail(L4D_EINVAL, "rope: base must be finite and above 1");
+  if (!(r->amplitude > 0.0) || !std::isfinite((float)r->amplitude))
+    return fail(L4D_EINVAL, "rope: the amplitude must be finite and positive");
+  const bool scaled = r->scaling != L4D_ROPE_PLAIN, bands = r->scaling == L4D_ROPE_BANDS || r->scaling == L4D_ROPE_RAMP;
+  if (scaled && (!(r->factor > 0.0) || !std::isfinite(r->factor)))
+    return fail(L4D_EINVAL, "rope: factor must be finite and positive");
+  if (bands && (!(r->original > 0.0) || !std::isfinite(r->original) || !(r->low > 0.0) || !(r->high > r->low) ||
+                !std::isfinite(r->high)))
+    return fail(L4D_EINVAL, "rope: need original > 0 and 0 < low < high");
+  const double rot = (double)r->rot_dim, log_base = std::log(r->base);
+  double j0 = 0.0, j1 = 0.0;
+  if (r->scaling == L4D_ROPE_RAMP) {
+    // the pair that makes `t` turns over the original context: base^(-2j/rot) original = 2 pi t
+    const auto pair_of = [&](double t) { return rot * std::log(r->original / (kTwoPi * t)) / (2.0 * log_base); };
+    j0 = std::max(std::floor(pair_of(r->high)), 0.0);
+    j1 = std::min(std::ceil(pair_of(r->low)), rot - 1.0);
+  }
+  for (int64_t j = 0; j < r->rot_dim / 2; ++j) {
+    const double f = std::exp(-2.0 * (double)j / rot * log_base);
+    double keep = 1.0;                       // g_j
+    if (r->scaling == L4D_ROPE_LINEAR) keep = 0.0;
+    else if (r->scaling == L4D_ROPE_BANDS) keep = (r->original * f / kTwoPi - r->low) / (r->high - r->low);
+    else if (r->scaling == L4D_ROPE_RAMP) keep = 1.0 - std::min(std::max(((double)j - j0) / (j1 > j0 ? j1 - j0 : 0.001), 0.0), 1.0);
+    keep = std::min(std::max(keep, 0.0), 1.0);
+    turns[j] = (scaled ? f * ((1.0 - keep) / r->factor + keep) : f) / kTwoPi;
+  }
+  return L4D_OK;
+}
+
+int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk,
+              const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, int inverse, void* stream_ptr) {
+  if (!r || !q) return fail(L4D_EINVAL, "rope and q are required");
+  if (dtype != L4D_BF16 && dtype != L4D_F32) return fail(L4D_EINVAL, "rope: unknown dtype");
+  if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "rope: tokens must lie in 0 .. 2^30");
+  int rc;
+  if (pk && (rc = check_packing(pk))) return rc;
+  if (pk && pk->tokens != tokens) return fail(L4D_EINVAL, "rope: the packing is of another number of tokens");
+  if (reinterpret_cast<uintptr_t>(positions) % 8) return fail(L4D_EINVAL, "rope: positions must be 8-byte aligned");
+  RopeRotate a{};
+  if ((rc = rope_turns(r, a.turns))) return rc;
+  const int64_t size = dtype == L4D_F32 ? 4 : 2;
+  const l4d_rope_heads* in[2] = {q, k};
+  for (const l4d_rope_heads* t : in) {
+    if (!t) continue;
+    if (!t->x || !t->y) return fail(L4D_EINVAL, "rope: a tensor is NULL");
+    if (t->heads < 1 || t->heads > (int64_t)1 << 16) return fail(L4D_EINVAL, "rope: heads must lie in 1 .. 2^16");
+    const int64_t cols = t->heads * r->head_dim;
+    if (t->x_ld < cols || t->y_ld < cols || t->x_ld > (int64_t)1 << 31 || t->y_ld > (int64_t)1 << 31)
+      return fail(L4D_EINVAL, "rope: a row stride is shorter than the heads, or above 2^31");
+    const uintptr_t x = reinterpret_cast<uintptr_t>(t->x), y = reinterpret_cast<uintptr_t>(t->y);
+    if (x % size || y % size) return fail(L4D_EINVAL, "rope: a tensor is misaligned");
+    const uint64_t nx = tokens ? ((uint64_t)(tokens - 1) * t->x_ld + cols) * size : 0;
+    const uint64_t ny = tokens ? ((uint64_t)(tokens - 1) * t->y_ld + cols) * size : 0;
+    if (!(x == y && t->x_ld == t->y_ld) && x < y + ny && y < x + nx)
+      return fail(L4D_EINVAL, "rope: input and output overlap");
+    a.t[a.n_tensors++] = RopeHeads{t->x, t->y, t->x_ld, t->y_ld, (int32_t)t->heads};
+  }
+  if (tokens == 0 || (pk && pk->n_seqs == 0)) return L4D_OK;
+  a.pk = pk ? device_packing(pk) : Packing{nullptr, -1, (int32_t)tokens};
+  a.positions = positions;
+  a.tokens = (int32_t)tokens;
+  a.d_h = (int32_t)r->head_dim;
+  a.rot = (int32_t)r->rot_dim;
+  a.f32 = dtype == L4D_F32;
+  a.interleaved = r->layout == L4D_ROPE_INTERLEAVED;
+  a.inverse = inverse;
+  a.amplitude = (float)r->amplitude;
+  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
+  return launch(name, s, [&] { return rope_rotate(a, s); });
+}
+}  // namespace
+
+namespace {
+struct AttnRows {        // one tensor of a call
+  const char* name;
+  const void* p;
+  int64_t ld, heads;
+};
+int attn_shape(const l4d_attn* at, int64_t tokens, int64_t n_seqs, PackedAttn* p) {
+  if (!at) return fail(L4D_EINVAL, "attn is required");
+  if (at->head_dim != 64 && at->head_dim != 128)
+    return fail(L4D_EINVAL, "head dim %lld unsupported (64 or 128)", (long long)at->head_dim);
+  if (at->n_heads < 1 || at->n_heads > (int64_t)1 << 16 || at->n_kv_heads < 1 || at->n_heads % at->n_kv_heads)
+    return fail(L4D_EINVAL, "n_heads must lie in 1 .. 2^16 and be a multiple of n_kv_heads");
+  if (!(at->scale >= 0.f) || !std::isfinite(at->scale)) return fail(L4D_EINVAL, "the scale must be finite and >= 0");
+  p->heads = (int32_t)at->n_heads;
+  p->kv_heads = (int32_t)at->n_kv_heads;
+  p->d_h = (int32_t)at->head_dim;
+  p->scale = at->scale > 0.f ? at->scale : 1.0f / std::sqrt((float)at->head_dim);
+  p->n_split = attn_packed_splits(tokens, n_seqs, at->n_heads, at->n_kv_heads);
+  return L4D_OK;
+}
+int attn_rows(const AttnRows* t, int n, int64_t d) {
+  for (int i = 0; i < n; ++i) {
+    if (!t[i].p) return fail(L4D_EINVAL, "%s is required", t[i].name);
+    if (reinterpret_cast<uintptr_t>(t[i].p) % 16) return fail(L4D_EINVAL, "%s must be 16-byte aligned", t[i].name);
+    if (t[i].ld < t[i].heads * d || t[i].ld % 8 || t[i].ld > (int64_t)1 << 22)
+      return fail(L4D_EINVAL, "the row stride of %s must cover its heads, be a multiple of 8 and at most 2^22", t[i].name);
+  }
+  return L4D_OK;
+}
+// No output may start where another tensor does.
+int attn_distinct(const AttnRows* t, int n, int first_out) {
+  for (int i = first_out; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if (t[i].p == t[j].p) return fail(L4D_EINVAL, "%s and %s are the same array", t[i].name, t[j].name);
+  return L4D_OK;
+}
+// dQ first: it also writes delta, which dK/dV reads.
+int packed_attn_backward(const PackedAttn& p, hipStream_t s) {
+  int rc;
+  if ((rc = launch("attn_packed_dq", s, [&] { return attn_packed_bwd(p, 2, s); }))) return rc;
+  if ((rc = launch("attn_packed_dkdv", s, [&] { return attn_packed_bwd(p, 1, s); }))) return rc;
+  if (p.n_split > 1) return launch("attn_packed_reduce", s, [&] { return attn_packed_bwd(p, 3, s); });
+  return L4D_OK;
+}
+struct PackedWs {
+  uint64_t delta, partial, total;
+};
+PackedWs plan_packed(const PackedAttn& p, int64_t tokens) {
+  Carver cv;
+  PackedWs w{};
+  w.delta = cv.take((uint64_t)p.heads * tokens * 4);
+  w.partial = p.n_split > 1 ? cv.take(2ull * p.n_split * tokens * p.kv_heads * p.d_h * 4) : 0;
+  w.total = cv.used;
+  return w;
+}
+}  // namespace
+
+namespace {
+// A layer call over packed documents: what replaces the sequence of equal rows.
+struct LayerPacking {
+  const l4d_packing* pk;
+  RopeRotate rope;             // head size, angles and amplitude; no tensors
+};
+int layer_packing(const Shard& x, const l4d_packing* pk, const l4d_rope* rope, LayerPacking* lp) {
+  int rc = check_packing(pk);
+  if (rc) return rc;
+  if (x.c != 1 || x.b != 1) return fail(L4D_EINVAL, "packed documents need cp == 1 and micro_batch == 1");
+  if (pk->tokens != x.s) return fail(L4D_EINVAL, "the packing has %lld tokens, the layer %lld", (long long)pk->tokens, (long long)x.s);
+  if (pk->n_seqs == 0) return fail(L4D_EINVAL, "packing: a layer call needs at least one document");
+  l4d_rope plain{};
+  plain.head_dim = plain.rot_dim = x.d;
+  plain.base = x.base;
+  plain.amplitude = 1.0;
+  if (!rope) rope = &plain;
+  if (rope->head_dim != x.d || rope->rot_dim != x.d || rope->layout != L4D_ROPE_HALF)
+    return fail(L4D_EINVAL, "the layer turns whole heads of %lld in the half layout", (long long)x.d);
+  lp->pk = pk;
+  lp->rope = RopeRotate{};
+  if ((rc = rope_turns(rope, lp->rope.turns))) return rc;
+  lp->rope.pk = device_packing(pk);
+  lp->rope.tokens = (int32_t)pk->tokens;
+  lp->rope.d_h = lp->rope.rot = (int32_t)x.d;
+  lp->rope.amplitude = (float)rope->amplitude;
+  PackedAttn p{};
+  p.pk = device_packing(pk);
+  p.heads = (int32_t)x.a_t;
+  p.kv_heads = (int32_t)x.k_t;
+  p.d_h = (int32_t)x.d;
+  if (!attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
+  return L4D_OK;
+}
+// The layer's attention over its documents: Q, K, V, ctx and LSE of the stash.
+PackedAttn packed_layer_attn(const Shard& x, const LayerPacking& lp, const l4d_stash* st) {
+  PackedAttn p{};
+  p.pk = device_packing(lp.pk);
+  p.heads = (int32_t)x.a_t;
+  p.kv_heads = (int32_t)x.k_t;
+  p.d_h = (int32_t)x.d;
+  p.scale = 1.0f / std::sqrt((float)x.d);
+  p.n_split = attn_packed_splits(lp.pk->tokens, lp.pk->n_seqs, x.a_t, x.k_t);
+  p.q = sptr(st, L4D_STASH_Q);
+  p.k = sptr(st, L4D_STASH_K);
+  p.v = sptr(st, L4D_STASH_V);
+  p.o = sptr(st, L4D_STASH_CTX);
+  p.q_ld = p.o_ld = x.a_t * x.d;
+  p.k_ld = p.v_ld = x.k_t * x.d;
+  p.lse = sptr<float>(st, L4D_STASH_LSE);
+  return p;
+}
+}  // namespace
+
 // ============================================================== layer forward
 
-extern "C" int llama_layer_fwd(const l4d_model* m, const l4d_parallel* p, const l4d_layer_weights* w,
-                               const void* x_in, const l4d_peer_inputs* peers, const l4d_peer_outputs* sends,
-                               void* y, l4d_arena* A, l4d_stash** stash_out, void* stream_ptr) {
+// packing == nullptr: sequences of equal length, with the model's own RoPE.
+static int layer_forward(const l4d_model* m, const l4d_parallel* p, const l4d_packing* packing, const l4d_rope* scaled,
+                         const l4d_layer_weights* w, const void* x_in, const l4d_peer_inputs* peers,
+                         const l4d_peer_outputs* sends, void* y, l4d_arena* A, l4d_stash** stash_out, void* stream_ptr) {
   Shard x;
   int rc = make_shard(m, p, &x);
   if (rc) return rc;
+  LayerPacking lp{};
+  if (packing && (rc = layer_packing(x, packing, scaled, &lp))) return rc;
   if (!w || !w->norm1 || !w->qkv || !w->o || !w->norm2 || !w->gate_up || !w->down)
     return fail(L4D_EINVAL, "all six weights are required");
   if (!x_in || !y || !A || !stash_out) return fail(L4D_EINVAL, "x, y, arena and stash_out are required");
@@ -819,9 +1031,11 @@ extern "C" int llama_layer_fwd(const l4d_model* m, const l4d_parallel* p, const 
     // norm-1, stashing its input x as it goes, and the RoPE table
     if ((r = launch("rmsnorm1_fwd", s, [&] {
            return rmsnorm_fwd(static_cast<const uint16_t*>(x_in), static_cast<const uint16_t*>(w->norm1),
-                              sptr(st, L4D_STASH_XN1), x.b * x.s_sp, (int32_t)x.h, x.eps, s, sptr(st, L4D_STASH_X), &table);
+                              sptr(st, L4D_STASH_XN1), x.b * x.s_sp, (int32_t)x.h, x.eps, s, sptr(st, L4D_STASH_X),
+                              lp.pk ? nullptr : &table);
          })))
       return r;
+    if (lp.pk && (r = launch("rope_table_packed", s, [&] { return rope_table(lp.rope, rope, s); }))) return r;
     // [Q|K|V] = xn1_full W_qkv^T, RoPE on Q, K
     EpiParams eq{};
     eq.kind = EpiKind::QkvRope;
@@ -837,13 +1051,19 @@ extern "C" int llama_layer_fwd(const l4d_model* m, const l4d_parallel* p, const 
                       Layout::KC, op(RowSrc::plain(w->qkv, x.h), qkv_cols(x)), Layout::KC, eq)))
       return r;
     // attention
-    AttnParams ap = attn_params(x);
-    ap.q = sptr(st, L4D_STASH_Q);
-    ap.o = sptr(st, L4D_STASH_CTX);
-    ap.lse = sptr<float>(st, L4D_STASH_LSE);
-    key_segments(x, ap, sptr(st, L4D_STASH_K), sptr(st, L4D_STASH_V), static_cast<const uint16_t*>(pi.remote_k),
-                 static_cast<const uint16_t*>(pi.remote_v), nullptr, nullptr, nullptr, nullptr, nullptr);
-    if ((r = launch("attn_fwd", s, [&] { return attn_fwd(ap, s); }))) return r;
+    if (lp.pk) {
+      const PackedAttn pa = packed_layer_attn(x, lp, st);
+      if ((r = launch("clear_outside", s, [&] { return clear_outside(pa.pk, pa.o, pa.o_ld, nq, s); }))) return r;
+      if ((r = launch("attn_packed_fwd", s, [&] { return attn_packed_fwd(pa, s); }))) return r;
+    } else {
+      AttnParams ap = attn_params(x);
+      ap.q = sptr(st, L4D_STASH_Q);
+      ap.o = sptr(st, L4D_STASH_CTX);
+      ap.lse = sptr<float>(st, L4D_STASH_LSE);
+      key_segments(x, ap, sptr(st, L4D_STASH_K), sptr(st, L4D_STASH_V), static_cast<const uint16_t*>(pi.remote_k),
+                   static_cast<const uint16_t*>(pi.remote_v), nullptr, nullptr, nullptr, nullptr, nullptr);
+      if ((r = launch("attn_fwd", s, [&] { return attn_fwd(ap, s); }))) return r;
+    }
     // h1 = x + ctx W_o^T (own rows; peers' rows are sent)
     if ((r = run_gemm("gemm_o", s, tok, x.h, nq, op(RowSrc::plain(sptr(st, L4D_STASH_CTX), nq), tok), Layout::KC,
                       op(RowSrc::plain(w->o, nq), x.h), Layout::KC,
@@ -878,19 +1098,36 @@ extern "C" int llama_layer_fwd(const l4d_model* m, const l4d_parallel* p, const 
     l4d_stash_release(A, st);
     return rc;
   }
+  st->packed = lp.pk != nullptr;
   *stash_out = st;
   return L4D_OK;
 }
 
+extern "C" int llama_layer_fwd(const l4d_model* m, const l4d_parallel* p, const l4d_layer_weights* w,
+                               const void* x_in, const l4d_peer_inputs* peers, const l4d_peer_outputs* sends,
+                               void* y, l4d_arena* A, l4d_stash** stash_out, void* stream_ptr) {
+  return layer_forward(m, p, nullptr, nullptr, w, x_in, peers, sends, y, A, stash_out, stream_ptr);
+}
+
+extern "C" int llama_layer_packed_fwd(const l4d_model* m, const l4d_parallel* p, const l4d_packing* packing,
+                                      const l4d_rope* rope, const l4d_layer_weights* w, const void* x_in,
+                                      const l4d_peer_inputs* peers, const l4d_peer_outputs* sends, void* y,
+                                      l4d_arena* A, l4d_stash** stash_out, void* stream_ptr) {
+  if (!packing) return fail(L4D_EINVAL, "packing is required");
+  return layer_forward(m, p, packing, rope, w, x_in, peers, sends, y, A, stash_out, stream_ptr);
+}
+
 // ============================================================== layer backward
 
-extern "C" int llama_layer_bwd(const l4d_model* m, const l4d_parallel* p, const l4d_layer_weights* w,
-                               const l4d_peer_inputs* peers, const l4d_peer_outputs* sends, l4d_stash* st,
-                               const void* dy, void* dx, const l4d_layer_grads* dw, void* d_remote_k,
-                               void* d_remote_v, l4d_arena* A, void* stream_ptr) {
+static int layer_backward(const l4d_model* m, const l4d_parallel* p, const l4d_packing* packing, const l4d_rope* scaled,
+                          const l4d_layer_weights* w, const l4d_peer_inputs* peers, const l4d_peer_outputs* sends,
+                          l4d_stash* st, const void* dy, void* dx, const l4d_layer_grads* dw, void* d_remote_k,
+                          void* d_remote_v, l4d_arena* A, void* stream_ptr) {
   Shard x;
   int rc = make_shard(m, p, &x);
   if (rc) return rc;
+  LayerPacking lp{};
+  if (packing && (rc = layer_packing(x, packing, scaled, &lp))) return rc;
   if (!w || !w->norm1 || !w->qkv || !w->o || !w->norm2 || !w->gate_up || !w->down)
     return fail(L4D_EINVAL, "all six weights are required");
   if (!dw || !dw->norm1 || !dw->qkv || !dw->o || !dw->norm2 || !dw->gate_up || !dw->down)
@@ -902,6 +1139,7 @@ extern "C" int llama_layer_bwd(const l4d_model* m, const l4d_parallel* p, const 
   if (sx.h != x.h || sx.a != x.a || sx.k != x.k || sx.f != x.f || sx.s != x.s || sx.b != x.b || sx.t != x.t ||
       sx.c != x.c || sx.tr != x.tr || sx.cr != x.cr)
     return fail(L4D_EINVAL, "stash was made for another shape");
+  if (st->packed != (packing != nullptr)) return fail(L4D_EINVAL, "the stash is of %s layer call", st->packed ? "a packed" : "an unpacked");
   if (x.c > 1 && (!d_remote_k || !d_remote_v)) return fail(L4D_EINVAL, "cp > 1 needs d_remote_k and d_remote_v");
   if ((rc = check_peers(x, peers, true))) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream_ptr);
@@ -961,7 +1199,7 @@ extern "C" int llama_layer_bwd(const l4d_model* m, const l4d_parallel* p, const 
          })))
       return r;
     // the gain gradient's sum, and the RoPE table for the attention backward
-    if ((r = launch("reduce_gain", s, [&] { return reduce_rows_add(partial, npart, (int32_t)x.h, dw->norm2, s, &table); })))
+    if ((r = launch("reduce_gain", s, [&] { return reduce_rows_add(partial, npart, (int32_t)x.h, dw->norm2, s, lp.pk ? nullptr : &table); })))
       return r;
     // attention output projection
     const RowSrc dh1_full = gathered(dh1, pi.sp_peer_dh1, x);
@@ -972,33 +1210,52 @@ extern "C" int llama_layer_bwd(const l4d_model* m, const l4d_parallel* p, const 
                       op(RowSrc::plain(sptr(st, L4D_STASH_CTX), nq), nq), Layout::MN, epi_acc(dw->o, nq), proj_part)))
       return r;
     // attention backward -> dQKV (inverse RoPE applied), remote dK/dV
-    AttnParams ap = attn_params(x);
-    ap.q = sptr(st, L4D_STASH_Q);
-    ap.o = sptr(st, L4D_STASH_CTX);
-    ap.lse = sptr<float>(st, L4D_STASH_LSE);
-    ap.dout = dctx;
-    ap.delta = delta;
-    ap.dq = dqkv;
-    ap.dq_ld = qc;
-    ap.rope = rope;
-    key_segments(x, ap, sptr(st, L4D_STASH_K), sptr(st, L4D_STASH_V), static_cast<const uint16_t*>(pi.remote_k),
-                 static_cast<const uint16_t*>(pi.remote_v), dqkv, static_cast<uint16_t*>(d_remote_k),
-                 static_cast<uint16_t*>(d_remote_v), static_cast<const uint16_t*>(pi.cp_peer_dk),
-                 static_cast<const uint16_t*>(pi.cp_peer_dv));
-    ap.total_keys = 0;
-    for (int i = 0; i < ap.n_seg; ++i) {
-      ap.seg_key0[i] = ap.total_keys;
-      ap.total_keys += ap.seg[i].n;
+    if (lp.pk) {
+      PackedAttn pa = packed_layer_attn(x, lp, st);
+      pa.dout = dctx;
+      pa.do_ld = nq;
+      pa.delta = delta;
+      pa.dq = dqkv;
+      pa.dk = dqkv + nq;
+      pa.dv = dqkv + nq + x.k_t * x.d;
+      pa.dq_ld = pa.dk_ld = pa.dv_ld = qc;
+      pa.dkv_partial = reinterpret_cast<float*>(wsb + plan.dkv);
+      if ((r = launch("clear_outside", s, [&] { return clear_outside(pa.pk, dqkv, qc, qc, s); }))) return r;
+      if ((r = packed_attn_backward(pa, s))) return r;
+      RopeRotate back = lp.rope;      // dQ and dK, neighbouring columns, turned back in place
+      back.inverse = 1;
+      back.n_tensors = 1;
+      back.t[0] = RopeHeads{dqkv, dqkv, qc, qc, (int32_t)(x.a_t + x.k_t)};
+      if ((r = launch("rope_bwd", s, [&] { return rope_rotate(back, s); }))) return r;
+    } else {
+      AttnParams ap = attn_params(x);
+      ap.q = sptr(st, L4D_STASH_Q);
+      ap.o = sptr(st, L4D_STASH_CTX);
+      ap.lse = sptr<float>(st, L4D_STASH_LSE);
+      ap.dout = dctx;
+      ap.delta = delta;
+      ap.dq = dqkv;
+      ap.dq_ld = qc;
+      ap.rope = rope;
+      key_segments(x, ap, sptr(st, L4D_STASH_K), sptr(st, L4D_STASH_V), static_cast<const uint16_t*>(pi.remote_k),
+                   static_cast<const uint16_t*>(pi.remote_v), dqkv, static_cast<uint16_t*>(d_remote_k),
+                   static_cast<uint16_t*>(d_remote_v), static_cast<const uint16_t*>(pi.cp_peer_dk),
+                   static_cast<const uint16_t*>(pi.cp_peer_dv));
+      ap.total_keys = 0;
+      for (int i = 0; i < ap.n_seg; ++i) {
+        ap.seg_key0[i] = ap.total_keys;
+        ap.total_keys += ap.seg[i].n;
+      }
+      ap.n_split = attn_bwd_splits(ap);
+      if (ap.n_split > 1) {
+        ap.dkv_partial = reinterpret_cast<float*>(wsb + plan.dkv);
+        ap.partial_half = (int64_t)ap.n_split * x.b * ap.total_keys * x.k_t * x.d;
+      }
+      // dQ first: it also writes delta = rowsum(dO * O), which dK/dV reads
+      if ((r = launch("attn_bwd_dq", s, [&] { return attn_bwd(ap, 2, s); }))) return r;
+      if ((r = launch("attn_bwd_dkdv", s, [&] { return attn_bwd(ap, 1, s); }))) return r;
+      if (ap.n_split > 1 && (r = launch("attn_dkv_reduce", s, [&] { return attn_bwd(ap, 3, s); }))) return r;
     }
-    ap.n_split = attn_bwd_splits(ap);
-    if (ap.n_split > 1) {
-      ap.dkv_partial = reinterpret_cast<float*>(wsb + plan.dkv);
-      ap.partial_half = (int64_t)ap.n_split * x.b * ap.total_keys * x.k_t * x.d;
-    }
-    // dQ first: it also writes delta = rowsum(dO * O), which dK/dV reads
-    if ((r = launch("attn_bwd_dq", s, [&] { return attn_bwd(ap, 2, s); }))) return r;
-    if ((r = launch("attn_bwd_dkdv", s, [&] { return attn_bwd(ap, 1, s); }))) return r;
-    if (ap.n_split > 1 && (r = launch("attn_dkv_reduce", s, [&] { return attn_bwd(ap, 3, s); }))) return r;
     // QKV projection
     if ((r = run_gemm("gemm_qkv_dx", s, tok, x.h, qc, op(RowSrc::plain(dqkv, qc), tok), Layout::KC,
                       op(RowSrc::plain(w->qkv, x.h), x.h), Layout::MN,
@@ -1022,6 +1279,21 @@ extern "C" int llama_layer_bwd(const l4d_model* m, const l4d_parallel* p, const 
   rc = body();
   if (rc) return rc;
   return l4d_stash_release(A, st);
+}
+
+extern "C" int llama_layer_bwd(const l4d_model* m, const l4d_parallel* p, const l4d_layer_weights* w,
+                               const l4d_peer_inputs* peers, const l4d_peer_outputs* sends, l4d_stash* st,
+                               const void* dy, void* dx, const l4d_layer_grads* dw, void* d_remote_k,
+                               void* d_remote_v, l4d_arena* A, void* stream_ptr) {
+  return layer_backward(m, p, nullptr, nullptr, w, peers, sends, st, dy, dx, dw, d_remote_k, d_remote_v, A, stream_ptr);
+}
+
+extern "C" int llama_layer_packed_bwd(const l4d_model* m, const l4d_parallel* p, const l4d_packing* packing,
+                                      const l4d_rope* rope, const l4d_layer_weights* w, const l4d_peer_inputs* peers,
+                                      const l4d_peer_outputs* sends, l4d_stash* st, const void* dy, void* dx,
+                                      const l4d_layer_grads* dw, l4d_arena* A, void* stream_ptr) {
+  if (!packing) return fail(L4D_EINVAL, "packing is required");
+  return layer_backward(m, p, packing, rope, w, peers, sends, st, dy, dx, dw, nullptr, nullptr, A, stream_ptr);
 }
 
 // ============================================================== LM head
@@ -1302,101 +1574,6 @@ extern "C" int lm_head_bwd(const l4d_model* m, const l4d_parallel* p, const void
 
 // ============================================================== packed documents
 
-namespace {
-int check_packing(const l4d_packing* pk) {
-  if (!pk) return fail(L4D_EINVAL, "packing is required");
-  if (pk->tokens < 0 || pk->tokens > (int64_t)1 << 30 || pk->n_seqs < 0 || pk->n_seqs > (int64_t)1 << 30)
-    return fail(L4D_EINVAL, "packing: tokens and n_seqs must lie in 0 .. 2^30");
-  if (pk->n_seqs > 0 && !pk->starts) return fail(L4D_EINVAL, "packing: starts is required");
-  if (reinterpret_cast<uintptr_t>(pk->starts) % 8) return fail(L4D_EINVAL, "packing: starts must be 8-byte aligned");
-  return L4D_OK;
-}
-Packing device_packing(const l4d_packing* pk) {
-  return Packing{pk->starts, (int32_t)pk->n_seqs, (int32_t)pk->tokens};
-}
-
-// ------------------------------------------------------------ rotary positions
-
-// f_j / 2 pi of every pair, in double.
-int rope_turns(const l4d_rope* r, double* turns) {
-  constexpr double kTwoPi = 6.283185307179586476925286766559;
-  if (r->head_dim < 2 || r->head_dim > 2 * kMaxRopePairs) return fail(L4D_EINVAL, "rope: head_dim must lie in 2 .. 512");
-  if (r->rot_dim < 2 || r->rot_dim > r->head_dim || r->rot_dim % 2)
-    return fail(L4D_EINVAL, "rope: rot_dim must be even and lie in 2 .. head_dim");
-  if (r->layout != L4D_ROPE_HALF && r->layout != L4D_ROPE_INTERLEAVED) return fail(L4D_EINVAL, "rope: unknown layout");
-  if (r->scaling < L4D_ROPE_PLAIN || r->scaling > L4D_ROPE_RAMP) return fail(L4D_EINVAL, "rope: unknown scaling");
-  if (!(r->base > 1.0) || !std::isfinite(r->base)) return fail(L4D_EINVAL, "rope: base must be finite and above 1");
-  if (!(r->amplitude > 0.0) || !std::isfinite((float)r->amplitude))
-    return fail(L4D_EINVAL, "rope: the amplitude must be finite and positive");
-  const bool scaled = r->scaling != L4D_ROPE_PLAIN, bands = r->scaling == L4D_ROPE_BANDS || r->scaling == L4D_ROPE_RAMP;
-  if (scaled && (!(r->factor > 0.0) || !std::isfinite(r->factor)))
-    return fail(L4D_EINVAL, "rope: factor must be finite and positive");
-  if (bands && (!(r->original > 0.0) || !std::isfinite(r->original) || !(r->low > 0.0) || !(r->high > r->low) ||
-                !std::isfinite(r->high)))
-    return fail(L4D_EINVAL, "rope: need original > 0 and 0 < low < high");
-  const double rot = (double)r->rot_dim, log_base = std::log(r->base);
-  double j0 = 0.0, j1 = 0.0;
-  if (r->scaling == L4D_ROPE_RAMP) {
-    // the pair that makes `t` turns over the original context: base^(-2j/rot) original = 2 pi t
-    const auto pair_of = [&](double t) { return rot * std::log(r->original / (kTwoPi * t)) / (2.0 * log_base); };
-    j0 = std::max(std::floor(pair_of(r->high)), 0.0);
-    j1 = std::min(std::ceil(pair_of(r->low)), rot - 1.0);
-  }
-  for (int64_t j = 0; j < r->rot_dim / 2; ++j) {
-    const double f = std::exp(-2.0 * (double)j / rot * log_base);
-    double keep = 1.0;                       // g_j
-    if (r->scaling == L4D_ROPE_LINEAR) keep = 0.0;
-    else if (r->scaling == L4D_ROPE_BANDS) keep = (r->original * f / kTwoPi - r->low) / (r->high - r->low);
-    else if (r->scaling == L4D_ROPE_RAMP) keep = 1.0 - std::min(std::max(((double)j - j0) / (j1 > j0 ? j1 - j0 : 0.001), 0.0), 1.0);
-    keep = std::min(std::max(keep, 0.0), 1.0);
-    turns[j] = (scaled ? f * ((1.0 - keep) / r->factor + keep) : f) / kTwoPi;
-  }
-  return L4D_OK;
-}
-
-int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk,
-              const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, int inverse, void* stream_ptr) {
-  if (!r || !q) return fail(L4D_EINVAL, "rope and q are required");
-  if (dtype != L4D_BF16 && dtype != L4D_F32) return fail(L4D_EINVAL, "rope: unknown dtype");
-  if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "rope: tokens must lie in 0 .. 2^30");
-  int rc;
-  if (pk && (rc = check_packing(pk))) return rc;
-  if (pk && pk->tokens != tokens) return fail(L4D_EINVAL, "rope: the packing is of another number of tokens");
-  if (reinterpret_cast<uintptr_t>(positions) % 8) return fail(L4D_EINVAL, "rope: positions must be 8-byte aligned");
-  RopeRotate a{};
-  if ((rc = rope_turns(r, a.turns))) return rc;
-  const int64_t size = dtype == L4D_F32 ? 4 : 2;
-  const l4d_rope_heads* in[2] = {q, k};
-  for (const l4d_rope_heads* t : in) {
-    if (!t) continue;
-    if (!t->x || !t->y) return fail(L4D_EINVAL, "rope: a tensor is NULL");
-    if (t->heads < 1 || t->heads > (int64_t)1 << 16) return fail(L4D_EINVAL, "rope: heads must lie in 1 .. 2^16");
-    const int64_t cols = t->heads * r->head_dim;
-    if (t->x_ld < cols || t->y_ld < cols || t->x_ld > (int64_t)1 << 31 || t->y_ld > (int64_t)1 << 31)
-      return fail(L4D_EINVAL, "rope: a row stride is shorter than the heads, or above 2^31");
-    const uintptr_t x = reinterpret_cast<uintptr_t>(t->x), y = reinterpret_cast<uintptr_t>(t->y);
-    if (x % size || y % size) return fail(L4D_EINVAL, "rope: a tensor is misaligned");
-    const uint64_t nx = tokens ? ((uint64_t)(tokens - 1) * t->x_ld + cols) * size : 0;
-    const uint64_t ny = tokens ? ((uint64_t)(tokens - 1) * t->y_ld + cols) * size : 0;
-    if (!(x == y && t->x_ld == t->y_ld) && x < y + ny && y < x + nx)
-      return fail(L4D_EINVAL, "rope: input and output overlap");
-    a.t[a.n_tensors++] = RopeHeads{t->x, t->y, t->x_ld, t->y_ld, (int32_t)t->heads};
-  }
-  if (tokens == 0 || (pk && pk->n_seqs == 0)) return L4D_OK;
-  a.pk = pk ? device_packing(pk) : Packing{nullptr, -1, (int32_t)tokens};
-  a.positions = positions;
-  a.tokens = (int32_t)tokens;
-  a.d_h = (int32_t)r->head_dim;
-  a.rot = (int32_t)r->rot_dim;
-  a.f32 = dtype == L4D_F32;
-  a.interleaved = r->layout == L4D_ROPE_INTERLEAVED;
-  a.inverse = inverse;
-  a.amplitude = (float)r->amplitude;
-  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
-  return launch(name, s, [&] { return rope_rotate(a, s); });
-}
-}  // namespace
-
 extern "C" int rope_fwd(const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk, const int64_t* positions,
                         const l4d_rope_heads* q, const l4d_rope_heads* k, void* stream_ptr) {
   return rope_call("rope_fwd", r, dtype, tokens, pk, positions, q, k, 0, stream_ptr);
@@ -1408,55 +1585,6 @@ extern "C" int rope_bwd(const l4d_rope* r, int dtype, int64_t tokens, const l4d_
 }
 
 // ------------------------------------------------------------ packed attention
-
-namespace {
-struct AttnRows {        // one tensor of a call
-  const char* name;
-  const void* p;
-  int64_t ld, heads;
-};
-int attn_shape(const l4d_attn* at, int64_t tokens, int64_t n_seqs, PackedAttn* p) {
-  if (!at) return fail(L4D_EINVAL, "attn is required");
-  if (at->head_dim != 64 && at->head_dim != 128)
-    return fail(L4D_EINVAL, "head dim %lld unsupported (64 or 128)", (long long)at->head_dim);
-  if (at->n_heads < 1 || at->n_heads > (int64_t)1 << 16 || at->n_kv_heads < 1 || at->n_heads % at->n_kv_heads)
-    return fail(L4D_EINVAL, "n_heads must lie in 1 .. 2^16 and be a multiple of n_kv_heads");
-  if (!(at->scale >= 0.f) || !std::isfinite(at->scale)) return fail(L4D_EINVAL, "the scale must be finite and >= 0");
-  p->heads = (int32_t)at->n_heads;
-  p->kv_heads = (int32_t)at->n_kv_heads;
-  p->d_h = (int32_t)at->head_dim;
-  p->scale = at->scale > 0.f ? at->scale : 1.0f / std::sqrt((float)at->head_dim);
-  p->n_split = attn_packed_splits(tokens, n_seqs, at->n_heads, at->n_kv_heads);
-  return L4D_OK;
-}
-int attn_rows(const AttnRows* t, int n, int64_t d) {
-  for (int i = 0; i < n; ++i) {
-    if (!t[i].p) return fail(L4D_EINVAL, "%s is required", t[i].name);
-    if (reinterpret_cast<uintptr_t>(t[i].p) % 16) return fail(L4D_EINVAL, "%s must be 16-byte aligned", t[i].name);
-    if (t[i].ld < t[i].heads * d || t[i].ld % 8 || t[i].ld > (int64_t)1 << 22)
-      return fail(L4D_EINVAL, "the row stride of %s must cover its heads, be a multiple of 8 and at most 2^22", t[i].name);
-  }
-  return L4D_OK;
-}
-// No output may start where another tensor does.
-int attn_distinct(const AttnRows* t, int n, int first_out) {
-  for (int i = first_out; i < n; ++i)
-    for (int j = 0; j < i; ++j)
-      if (t[i].p == t[j].p) return fail(L4D_EINVAL, "%s and %s are the same array", t[i].name, t[j].name);
-  return L4D_OK;
-}
-struct PackedWs {
-  uint64_t delta, partial, total;
-};
-PackedWs plan_packed(const PackedAttn& p, int64_t tokens) {
-  Carver cv;
-  PackedWs w{};
-  w.delta = cv.take((uint64_t)p.heads * tokens * 4);
-  w.partial = p.n_split > 1 ? cv.take(2ull * p.n_split * tokens * p.kv_heads * p.d_h * 4) : 0;
-  w.total = cv.used;
-  return w;
-}
-}  // namespace
 
 extern "C" int l4d_attn_packed_workspace_bytes(const l4d_attn* at, int64_t tokens, uint64_t* bytes) {
   if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "tokens must lie in 0 .. 2^30");
@@ -1525,12 +1653,7 @@ extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const 
   p.dq_ld = dq_ld, p.dk_ld = dk_ld, p.dv_ld = dv_ld;
   p.delta = reinterpret_cast<float*>(wsb + plan.delta);
   p.dkv_partial = reinterpret_cast<float*>(wsb + plan.partial);
-  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
-  // dQ first: it also writes delta, which dK/dV reads
-  if ((rc = launch("attn_packed_dq", s, [&] { return attn_packed_bwd(p, 2, s); }))) return rc;
-  if ((rc = launch("attn_packed_dkdv", s, [&] { return attn_packed_bwd(p, 1, s); }))) return rc;
-  if (p.n_split > 1) return launch("attn_packed_reduce", s, [&] { return attn_packed_bwd(p, 3, s); });
-  return L4D_OK;
+  return packed_attn_backward(p, static_cast<hipStream_t>(stream_ptr));
 }
 
 // ============================================================== loss without stored logits

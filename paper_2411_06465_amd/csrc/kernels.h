@@ -300,6 +300,12 @@ struct RopeRotate {
   double turns[kMaxRopePairs];   // f_j / 2 pi
 };
 hipError_t rope_rotate(const RopeRotate& p, hipStream_t stream);
+// tab[row][j] = A (cos, sin) of pair j at the row's distance from its document's start
+// (0 for rows of no document): the table of the layer's QKV epilogue.
+hipError_t rope_table(const RopeRotate& p, float2* tab, hipStream_t stream);
+// Zeroes the first `cols` columns (a multiple of 8) of the rows of x (row stride ld)
+// that belong to no document.
+hipError_t clear_outside(const Packing& pk, uint16_t* x, int64_t ld, int64_t cols, hipStream_t stream);
 
 // ---------------------------------------------------------------- cross-entropy
 

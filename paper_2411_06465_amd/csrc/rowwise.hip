@@ -129,6 +129,35 @@ struct RopeVec {             // V consecutive elements: one or two 16-byte acces
   }
 };
 
+// A (cos, sin) of pair j at position pos
+__device__ __forceinline__ float2 rope_angle(const RopeRotate& p, int64_t pos, int j) {
+  double turn = static_cast<double>(pos) * p.turns[j];
+  turn -= rint(turn);
+  float s, c;
+  sincospif(static_cast<float>(2.0 * turn), &s, &c);
+  return make_float2(p.amplitude * c, p.amplitude * s);
+}
+
+// One wave per row.
+__global__ void __launch_bounds__(256) rope_table_kernel(RopeRotate p, float2* __restrict__ tab) {
+  const int lane = threadIdx.x & 63, row = static_cast<int>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (row >= p.tokens) return;
+  const SeqRows s = seq_of_row(p.pk, row, lane);
+  const int pos = row < s.hi ? row - s.lo : 0;
+  for (int j = lane; j < p.rot / 2; j += 64) tab[static_cast<int64_t>(row) * (p.rot / 2) + j] = rope_angle(p, pos, j);
+}
+
+__global__ void __launch_bounds__(256) clear_outside_kernel(Packing pk, uint16_t* __restrict__ x, int64_t ld, int64_t cols) {
+  const int first = seq_start(pk, 0), end = seq_start(pk, pk.n_seqs);
+  for (int64_t row = blockIdx.x; row < pk.tokens; row += gridDim.x) {
+    if (row >= first && row < end) {       // on to the first row behind the documents that is this block's
+      row += (end - row - 1) / gridDim.x * gridDim.x;
+      continue;
+    }
+    for (int64_t c = threadIdx.x * 8; c < cols; c += 256 * 8) *reinterpret_cast<u32x4*>(x + row * ld + c) = u32x4{0, 0, 0, 0};
+  }
+}
+
 template <typename T, int V, bool INTER>
 __global__ void __launch_bounds__(256) rope_rotate_kernel(RopeRotate p) {
   __shared__ __attribute__((aligned(16))) float2 table[4][kMaxRopePairs];
@@ -145,11 +174,9 @@ __global__ void __launch_bounds__(256) rope_rotate_kernel(RopeRotate p) {
   const int pairs = p.rot / 2;
   float2* tab = table[wave];
   for (int j = lane; j < pairs; j += 64) {
-    double turn = static_cast<double>(pos) * p.turns[j];
-    turn -= rint(turn);
-    float s, c;
-    sincospif(static_cast<float>(2.0 * turn), &s, &c);
-    tab[j] = make_float2(p.amplitude * c, p.amplitude * (p.inverse ? -s : s));
+    float2 cs = rope_angle(p, pos, j);
+    if (p.inverse) cs.y = -cs.y;
+    tab[j] = cs;
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   const int step = 64 * p.parts;
@@ -1164,6 +1191,14 @@ hipError_t rope_rotate(const RopeRotate& params, hipStream_t stream) {
   return p.f32 ? rope_launch<float>(p, vec, grid, stream) : rope_launch<uint16_t>(p, vec, grid, stream);
 }
 
+hipError_t rope_table(const RopeRotate& p, float2* tab, hipStream_t stream) {
+  hipLaunchKernelGGL(rope_table_kernel, dim3(static_cast<unsigned>((p.tokens + 3) / 4)), dim3(256), 0, stream, p, tab);
+  return hipGetLastError();
+}
+hipError_t clear_outside(const Packing& pk, uint16_t* x, int64_t ld, int64_t cols, hipStream_t stream) {
+  hipLaunchKernelGGL(clear_outside_kernel, dim3(256), dim3(256), 0, stream, pk, x, ld, cols);
+  return hipGetLastError();
+}
 hipError_t loss_join(const LossJoin& p, hipStream_t stream) {
   hipLaunchKernelGGL(loss_join_kernel, dim3(static_cast<unsigned>((p.n + 63) / 64)), dim3(kJoinWaves * 64), 0, stream, p);
   return hipGetLastError();
