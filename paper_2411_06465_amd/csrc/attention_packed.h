@@ -9,6 +9,14 @@
 // holds (an infinity or NaN in V, say, which a zero probability would not hide)
 // can reach another.
 
+// Tiles with a probability above this keep a second bf16 part of P (dV) and dS (dQ,
+// dK) in the backward's products (a wave-wide vote): there single elements decide a
+// gradient.  Relative error of dQ, dK, dV on short documents 1.8, 1.7, 1.7e-3, on
+// long ones 2.1, 2.1, 2.0e-3 (the output's own rounding is 1.7e-3), without second
+// parts 2.8, 2.4, 2.3e-3; for 1% of the backward's time on long documents, 6% on
+// short ones (16384 tokens in 160).
+constexpr float kLargeP = 1.f / 8;
+
 // ------------------------------------------------------------------ forward
 // One workgroup per block of query rows and hpb query heads of one kv head: 4
 // waves x 32 rows, wave w on head w % hpb.  Each lane holds one query's scores
@@ -193,12 +201,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 // sum_j dS_ij is 0 for the true delta and the p_ij add up to 1, the sum that comes
 // out is that error: it is added to the delta that the dK/dV pass reads.  The first
 // 32 rows of a document, which one tile covers, have it before dQ's product too.
-// The dQ of later rows uses the uncorrected delta; where a probability is large,
-// which is where the error counts, dS enters the product in two bf16 parts instead
-// of one (a wave-wide vote per tile).  Each gradient so carries about two roundings:
-// relative error 2.8e-3 -> 1.7e-3 of dQ, 2.8e-3 -> 2.4e-3 of dK on short documents
-// (the output's rounding alone is 1.7e-3), for 3% of dQ's time on long documents, 8%
-// where they have 400 tokens.
+// The dQ of later rows uses the uncorrected delta; where the error counts, a
+// probability is large and dS enters the product in two parts (kLargeP).
 template <int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) attn_packed_dq_kernel(PackedAttn p) {
   constexpr int KQ = 32;                     // keys per tile
@@ -257,7 +261,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   settle(my_lse);
   settle(my_delta);
   const float c = p.scale * kLog2e;
-  constexpr float kLargeP = 1.f / 32;
   float ds_sum = 0.f;
   f32x16 dq[D / 32];
 #pragma unroll
@@ -402,7 +405,18 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int kk = 0; kk < D / 16; ++kk) settle(kv[kk]);
   }
   f32x16 s;                  // role 0: S -> P of a tile, role 1: its dP - delta
-  bf16x8 x[2];               // role 0: P, role 1: dS (bf16)
+  bf16x8 x[2], lo[2] = {};   // role 0: P, role 1: dS (bf16), and their second parts
+  bool large = false;        // a probability of the tile is above kLargeP
+  const auto second_parts = [&](const f32x16& pr, const f32x16& v) __attribute__((always_inline)) {
+    float m = __builtin_fmaxf(pr[0], pr[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) m = __builtin_fmaxf(__builtin_fmaxf(m, pr[i]), pr[i + 1]);
+    large = __builtin_amdgcn_ballot_w64(m > kLargeP) != 0;
+    if (large) {
+      lo[0] = frag_acc_lo(v, 0, x[0]);
+      lo[1] = frag_acc_lo(v, 8, x[1]);
+    }
+  };
   // role 0: P = exp(S - lse) of tile qt from its scores in s; bf16 into x, fp32 into handover hb
   auto probs = [&](int qt, const float4 (&ls4)[4], float4 (*hb)[2][64]) __attribute__((always_inline)) {
     const int q0 = blk.row0 + qt * QT;
@@ -429,19 +443,24 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
       hb[g][0][lane] = make_float4(s[i0], s[i0 + 1], s[i0 + 2], s[i0 + 3]);
       hb[g][1][lane] = make_float4(s[i0 + 4], s[i0 + 5], s[i0 + 6], s[i0 + 7]);
     }
+    second_parts(s, s);
   };
   // role 1: dS = P (dP - delta) of the tile whose dP - delta is in s, into x
   auto grads = [&](const float4 (*hb)[2][64]) __attribute__((always_inline)) {
+    f32x16 pr, ds;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const float4 p0 = hb[g][0][lane], p1 = hb[g][1][lane];
       const float pv[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
-      float ds[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) ds[j] = pv[j] * s[8 * g + j];
-      x[g] = __builtin_bit_cast(
-          bf16x8, u32x4{pack2(ds[0], ds[1]), pack2(ds[2], ds[3]), pack2(ds[4], ds[5]), pack2(ds[6], ds[7])});
+      for (int j = 0; j < 8; ++j) {
+        pr[8 * g + j] = pv[j];
+        ds[8 * g + j] = pv[j] * s[8 * g + j];
+      }
     }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) x[g] = frag_acc(ds, 8 * g);
+    second_parts(pr, ds);
   };
   auto minus = [&](const float4 (&d4)[4]) __attribute__((always_inline)) {
 #pragma unroll
@@ -505,6 +524,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
+    if (large) accum_t<D, 2, kLookDq>(qg[b][0], lo, acc, la2);
     read_stat(bn);
     issue((b + kDkvStages - 1) % kDkvStages);     // under the last products
     if (++qt == n_qt) qt = 0;
