@@ -355,45 +355,58 @@ def lm_head_bwd(model, par, w_norm, w_lm, targets, stash, dx, d_w_norm, d_w_lm, 
 
 # ------------------------------------------------------------------ packed documents
 
-def _on(tensor, stream):
-    """The stream to launch on (default: the current one of the tensor's GPU) and that GPU as the current one."""
+def _launch(entry, tensor, stream, *args):
+    """entry(*args, stream) on the tensor's GPU; the stream defaults to that GPU's current one."""
     import torch
+    device = tensor.device
     if stream is None:
-        stream = torch.cuda.current_stream(tensor.device)
-    if stream.device != tensor.device:
-        raise ValueError(f"the stream is on {stream.device}, the tensors are on {tensor.device}")
-    return torch.cuda.device(tensor.device), C.c_void_p(stream.cuda_stream)
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
+    if device.index == torch.cuda.current_device():
+        rc = entry(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = entry(*args, stream.cuda_stream)
+    if rc:
+        _check(rc)
 
 
-def _want(name, t, dtype, shape=None, like=None):
-    """Refuse a tensor that the C entry point would read as something else."""
+# Tensors are checked before their addresses go to the C entry point, which would
+# read another type or layout as something else.  The checks run on every call, so
+# they are few: small calls are bound by this code.
+
+def _want(name, t, dtype, shape, like):
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    if like is not None and t.device != like.device:
+    if t.device != like.device:
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    return t
 
 
 def _flat(name, t, dtype, shape, like):
+    """The address of a contiguous tensor (None: of none)."""
+    if t is None:
+        return None
     _want(name, t, dtype, shape, like)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return t
+    return t.data_ptr()
 
 
-def _rows(name, t, dtype, like, shape=None):
+def _rows(name, t, dtype, shape, like):
     """Row stride of a [tokens][heads][head_dim] tensor whose heads are contiguous within a row."""
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [tokens][heads][head_dim]")
     _want(name, t, dtype, shape, like)
-    n, heads, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
+    n, heads, d = shape
+    ld, per_head, one = t.stride()
+    if (d > 1 and one != 1) or (heads > 1 and per_head != d):
         raise ValueError(f"the heads of {name} must be contiguous within a row")
-    if n > 1 and t.stride(0) < heads * d:
+    if n <= 1:
+        return heads * d
+    if ld < heads * d:
         raise ValueError(f"the rows of {name} overlap")
-    return t.stride(0) if n > 1 else heads * d
+    return ld
 
 
 class Packing:
@@ -404,7 +417,9 @@ class Packing:
         import torch
         if starts.dim() != 1 or starts.numel() < 1 or not starts.is_contiguous():
             raise ValueError("starts must be a contiguous vector of n_seqs + 1 rows")
-        self.starts = _want("starts", starts, torch.int64)
+        if starts.dtype != torch.int64:
+            raise TypeError(f"starts must be {torch.int64}, not {starts.dtype}")
+        self.starts = starts
         self.tokens = tokens
         self.c = PackingC(tokens, starts.numel() - 1, starts.data_ptr())
 
@@ -424,29 +439,31 @@ def make_rope(head_dim, rot_dim=None, layout="half", base=1e4, scaling="none", f
                 factor, low, high, original, amplitude)
 
 
+def _on_one_device(packing, like):
+    if packing.starts.device != like.device:
+        raise ValueError(f"starts is on {packing.starts.device}, not on {like.device}")
+    return packing.c
+
+
+def _rope_io(name, x, y, dtype, tokens, d, like):
+    if x.dim() != 3 or x.shape[0] != tokens or x.shape[2] != d:
+        raise ValueError(f"{name} must be [{tokens}][heads][{d}], not {tuple(x.shape)}")
+    shape = x.shape
+    x_ld = _rows(name, x, dtype, shape, like)
+    y_ld = x_ld if y is None else _rows(name + "_out", y, dtype, shape, like)
+    return RopeHeads(x.data_ptr(), x.data_ptr() if y is None else y.data_ptr(), shape[1], x_ld, y_ld)
+
+
 def _rope(entry, rope, q, q_out, k, k_out, positions, packing, stream):
     import torch
-    dtype = {torch.bfloat16: 0, torch.float32: 1}.get(q.dtype)
-    if dtype is None:
-        raise TypeError(f"q must be bfloat16 or float32, not {q.dtype}")
-    tokens, io = q.shape[0], []
-    for name, x, y in (("q", q, q_out), ("k", k, k_out)):
-        if x is None:
-            io.append(None)
-            continue
-        y = x if y is None else y
-        x_ld, y_ld = _rows(name, x, q.dtype, q), _rows(name + "_out", y, q.dtype, q, x.shape)
-        if x.shape[0] != tokens or x.shape[2] != rope.head_dim:
-            raise ValueError(f"{name} must be [{tokens}][heads][{rope.head_dim}]")
-        io.append(RopeHeads(x.data_ptr(), y.data_ptr(), x.shape[1], x_ld, y_ld))
-    if positions is not None:
-        _flat("positions", positions, torch.int64, (tokens,), q)
-    if packing is not None:
-        _want("starts", packing.starts, torch.int64, like=q)
-    device, s = _on(q, stream)
-    with device:
-        _check(entry(C.byref(rope), dtype, tokens, None if packing is None else C.byref(packing.c), _ptr(positions),
-                     C.byref(io[0]), None if io[1] is None else C.byref(io[1]), s))
+    dtype, tokens = q.dtype, q.shape[0]
+    if dtype != torch.bfloat16 and dtype != torch.float32:
+        raise TypeError(f"q must be bfloat16 or float32, not {dtype}")
+    io = _rope_io("q", q, q_out, dtype, tokens, rope.head_dim, q)
+    io_k = None if k is None else _rope_io("k", k, k_out, dtype, tokens, rope.head_dim, q)
+    _launch(entry, q, stream, rope, 0 if dtype == torch.bfloat16 else 1, tokens,
+            None if packing is None else _on_one_device(packing, q),
+            _flat("positions", positions, torch.int64, (tokens,), q), io, io_k)
 
 
 def rope_fwd(rope, q, q_out=None, k=None, k_out=None, positions=None, packing=None, stream=None):
@@ -459,27 +476,30 @@ def rope_bwd(rope, dq, dq_out=None, dk=None, dk_out=None, positions=None, packin
     _rope(lib().rope_bwd, rope, dq, dq_out, dk, dk_out, positions, packing, stream)
 
 
-def _attn_args(packing, q, tensors):
+def _attn_args(q, tensors):
     """Checks of a call's tensors [(name, tensor, shape)] -> [pointer, row stride, ..]."""
     import torch
     args = []
     for name, t, shape in tensors:
-        args += [_ptr(t), _rows(name, t, torch.bfloat16, q, shape)]
-    _want("starts", packing.starts, torch.int64, like=q)
+        args += t.data_ptr(), _rows(name, t, torch.bfloat16, shape, q)
     return args
+
+
+def _attn_shapes(q, k, packing):
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k and v must be [tokens][heads][head_dim]")
+    (_, a, d), g, n = q.shape, k.shape[1], packing.tokens
+    return n, a, g, d, (n, a, d), (n, g, d)
 
 
 def attn_packed_fwd(q, k, v, o, lse, packing, scale=0.0, stream=None):
     """Causal attention within the packing's documents.  q, o [tokens][heads][d], k, v
     [tokens][kv_heads][d] bf16; lse f32 [heads][tokens].  scale 0 = 1/sqrt(d)."""
     import torch
-    n, (a, d), g = packing.tokens, q.shape[1:], k.shape[1]
-    args = _attn_args(packing, q, [("q", q, (n, a, d)), ("k", k, (n, g, d)), ("v", v, (n, g, d)),
-                                      ("o", o, (n, a, d))])
-    _flat("lse", lse, torch.float32, (a, n), q)
-    device, s = _on(q, stream)
-    with device:
-        _check(lib().attn_packed_fwd(C.byref(Attn(a, g, d, scale)), C.byref(packing.c), *args, _ptr(lse), s))
+    n, a, g, d, qs, ks = _attn_shapes(q, k, packing)
+    args = _attn_args(q, (("q", q, qs), ("k", k, ks), ("v", v, ks), ("o", o, qs)))
+    _launch(lib().attn_packed_fwd, q, stream, Attn(a, g, d, scale), _on_one_device(packing, q), *args,
+            _flat("lse", lse, torch.float32, (a, n), q))
 
 
 def l4d_attn_packed_workspace_bytes(tokens, n_heads, n_kv_heads, head_dim):
@@ -491,38 +511,26 @@ def l4d_attn_packed_workspace_bytes(tokens, n_heads, n_kv_heads, head_dim):
 def attn_packed_bwd(q, k, v, o, lse, d_o, dq, dk, dv, packing, arena, scale=0.0, stream=None):
     """Gradients of attn_packed_fwd, overwriting dq, dk and dv."""
     import torch
-    n, (a, d), g = packing.tokens, q.shape[1:], k.shape[1]
-    qs, ks = (n, a, d), (n, g, d)
-    args = _attn_args(packing, q, [("q", q, qs), ("k", k, ks), ("v", v, ks), ("o", o, qs), ("d_o", d_o, qs),
-                                      ("dq", dq, qs), ("dk", dk, ks), ("dv", dv, ks)])
-    _flat("lse", lse, torch.float32, (a, n), q)
-    device, s = _on(q, stream)
-    with device:
-        _check(lib().attn_packed_bwd(C.byref(Attn(a, g, d, scale)), C.byref(packing.c), *args[:8], _ptr(lse), *args[8:],
-                                     arena.h, s))
+    n, a, g, d, qs, ks = _attn_shapes(q, k, packing)
+    args = _attn_args(q, (("q", q, qs), ("k", k, ks), ("v", v, ks), ("o", o, qs), ("d_o", d_o, qs), ("dq", dq, qs),
+                          ("dk", dk, ks), ("dv", dv, ks)))
+    _launch(lib().attn_packed_bwd, q, stream, Attn(a, g, d, scale), _on_one_device(packing, q), *args[:8],
+            _flat("lse", lse, torch.float32, (a, n), q), *args[8:], arena.h)
 
 
 def llama_layer_packed_fwd(model, par, weights, x, y, arena, packing, rope=None, peers=None, sends=None, stream=None):
     """llama_layer_fwd over one row of packed documents; returns the Stash for llama_layer_packed_bwd."""
     st = C.c_void_p()
-    pi, so = _peers(peers), _sends(sends)
-    device, s = _on(x, stream)
-    with device:
-        _check(lib().llama_layer_packed_fwd(C.byref(model), C.byref(par), C.byref(packing.c),
-                                            None if rope is None else C.byref(rope), C.byref(_weights(weights)), _ptr(x),
-                                            C.byref(pi), C.byref(so), _ptr(y), arena.h, C.byref(st), s))
+    _launch(lib().llama_layer_packed_fwd, x, stream, model, par, _on_one_device(packing, x), rope, _weights(weights),
+            x.data_ptr(), _peers(peers), _sends(sends), y.data_ptr(), arena.h, C.byref(st))
     return Stash(st, arena)
 
 
 def llama_layer_packed_bwd(model, par, weights, stash, dy, dx, grads, arena, packing, rope=None, peers=None, sends=None,
                            stream=None):
     g = LayerGrads(*[grads[n].data_ptr() for n in ("norm1", "qkv", "o", "norm2", "gate_up", "down")])
-    pi, so = _peers(peers), _sends(sends)
-    device, s = _on(dy, stream)
-    with device:
-        _check(lib().llama_layer_packed_bwd(C.byref(model), C.byref(par), C.byref(packing.c),
-                                            None if rope is None else C.byref(rope), C.byref(_weights(weights)),
-                                            C.byref(pi), C.byref(so), stash.h, _ptr(dy), _ptr(dx), C.byref(g), arena.h, s))
+    _launch(lib().llama_layer_packed_bwd, dy, stream, model, par, _on_one_device(packing, dy), rope, _weights(weights),
+            _peers(peers), _sends(sends), stash.h, dy.data_ptr(), dx.data_ptr(), g, arena.h)
     stash.h = None
 
 
@@ -535,46 +543,38 @@ def l4d_lm_loss_workspace_bytes(n, h, v_t):
     return f.value, b.value
 
 
-def _loss_args(hidden, w_lm, targets):
+def _loss_args(hidden, w_lm, targets, vocab_start):
+    """(token vector's shape, [n, h, v_t, vocab_start, hidden, w_lm, targets])."""
     import torch
     if hidden.dim() != 2 or w_lm.dim() != 2:
         raise ValueError("hidden must be [tokens][h], w_lm [vocab][h]")
     (n, h), v_t = hidden.shape, w_lm.shape[0]
-    _flat("hidden", hidden, torch.bfloat16, (n, h), hidden)
-    _flat("w_lm", w_lm, torch.bfloat16, (v_t, h), hidden)
-    _flat("targets", targets, torch.int64, (n,), hidden)
-    return n, h, v_t
+    return (n,), [n, h, v_t, vocab_start, _flat("hidden", hidden, torch.bfloat16, (n, h), hidden),
+                  _flat("w_lm", w_lm, torch.bfloat16, (v_t, h), hidden),
+                  _flat("targets", targets, torch.int64, (n,), hidden)]
 
 
 def lm_loss_fwd(hidden, w_lm, targets, loss, lse, arena, vocab_start=0, peer_lse=None, peer_target_logit=None,
                 target_logit=None, stream=None):
     """Cross-entropy of every token (0 where the target is negative) and its log-sum-exp, without stored logits."""
     import torch
-    n, h, v_t = _loss_args(hidden, w_lm, targets)
-    for name, t in (("loss", loss), ("lse", lse), ("peer_lse", peer_lse), ("peer_target_logit", peer_target_logit),
-                    ("target_logit", target_logit)):
-        if t is not None:
-            _flat(name, t, torch.float32, (n,), hidden)
-    device, s = _on(hidden, stream)
-    with device:
-        _check(lib().lm_loss_fwd(n, h, v_t, vocab_start, _ptr(hidden), _ptr(w_lm), _ptr(targets), _ptr(peer_lse),
-                                 _ptr(peer_target_logit), _ptr(loss), _ptr(lse), _ptr(target_logit), arena.h, s))
+    n, args = _loss_args(hidden, w_lm, targets, vocab_start)
+    f32 = torch.float32
+    _launch(lib().lm_loss_fwd, hidden, stream, *args, _flat("peer_lse", peer_lse, f32, n, hidden),
+            _flat("peer_target_logit", peer_target_logit, f32, n, hidden), _flat("loss", loss, f32, n, hidden),
+            _flat("lse", lse, f32, n, hidden), _flat("target_logit", target_logit, f32, n, hidden), arena.h)
 
 
 def lm_loss_bwd(hidden, w_lm, targets, lse, d_hidden, d_w_lm, arena, d_loss=None, grad_scale=1.0, vocab_start=0,
                 stream=None):
     """Gradients of lm_loss_fwd's losses weighted by d_loss * grad_scale: d_hidden overwritten, d_w_lm added to."""
     import torch
-    n, h, v_t = _loss_args(hidden, w_lm, targets)
-    _flat("lse", lse, torch.float32, (n,), hidden)
-    _flat("d_hidden", d_hidden, torch.bfloat16, (n, h), hidden)
-    _flat("d_w_lm", d_w_lm, torch.float32, (v_t, h), hidden)
-    if d_loss is not None:
-        _flat("d_loss", d_loss, torch.float32, (n,), hidden)
-    device, s = _on(hidden, stream)
-    with device:
-        _check(lib().lm_loss_bwd(n, h, v_t, vocab_start, _ptr(hidden), _ptr(w_lm), _ptr(targets), _ptr(lse),
-                                 _ptr(d_loss), grad_scale, _ptr(d_hidden), _ptr(d_w_lm), arena.h, s))
+    n, args = _loss_args(hidden, w_lm, targets, vocab_start)
+    f32 = torch.float32
+    _launch(lib().lm_loss_bwd, hidden, stream, *args, _flat("lse", lse, f32, n, hidden),
+            _flat("d_loss", d_loss, f32, n, hidden), grad_scale,
+            _flat("d_hidden", d_hidden, torch.bfloat16, hidden.shape, hidden),
+            _flat("d_w_lm", d_w_lm, f32, w_lm.shape, hidden), arena.h)
 
 
 # ------------------------------------------------------------------ optimizer step

@@ -1825,8 +1825,7 @@ extern "C" int lm_loss_bwd(int64_t n, int64_t h, int64_t v_t, int64_t v0, const 
   }
   const LossTargets t{n, v0, v_t, (int32_t)h, targets, gt, plan.parts, dh, static_cast<const uint16_t*>(hidden),
                       static_cast<const uint16_t*>(w_lm), static_cast<uint16_t*>(d_hidden), d_w};
-  if ((rc = launch("loss_finish_dh", s, [&] { return loss_finish_dh(t, s); }))) return rc;
-  return launch("loss_finish_dw", s, [&] { return loss_finish_dw(t, s); });
+  return launch("loss_finish_grad", s, [&] { return loss_finish_grad(t, s); });
 }
 
 // ============================================================== optimizer

@@ -351,8 +351,7 @@ struct LossTargets {
   uint16_t* d_hidden;
   float* d_w;
 };
-hipError_t loss_finish_dh(const LossTargets& p, hipStream_t stream);
-hipError_t loss_finish_dw(const LossTargets& p, hipStream_t stream);
+hipError_t loss_finish_grad(const LossTargets& p, hipStream_t stream);
 // y = the n elements (a multiple of 8) of x, `times` times one behind another (bf16).
 hipError_t repeat_bf16(const uint16_t* x, uint16_t* y, int64_t n, int32_t times, hipStream_t stream);
 hipError_t zero_f32(float* x, int64_t n, hipStream_t stream);      // n a multiple of 4

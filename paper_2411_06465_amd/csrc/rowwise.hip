@@ -770,43 +770,32 @@ __global__ void __launch_bounds__(kJoinWaves * 64) loss_join_kernel(LossJoin p) 
   p.loss[row] = id >= 0 ? lse - z : 0.f;
 }
 
-// One wave per row: d_hidden = dh + (g - hi) W[target].
-__global__ void __launch_bounds__(256) loss_finish_dh_kernel(LossTargets p) {
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (row >= p.n) return;
-  const int64_t id = p.targets[row], t = id - p.v0;
-  const bool here = id >= 0 && t >= 0 && t < p.v_t;
-  float r = 0.f;
-  if (here) {
-    const float g = p.gt[row];
-    r = g - __uint_as_float(static_cast<uint32_t>(f2bf(g)) << 16);
-  }
-  const float* x = p.dh + row * p.h;
-  const uint16_t* w = p.w + (here ? t : 0) * p.h;
-  for (int c = lane * 8; c < p.h; c += 512) {
-    const float4 a = *reinterpret_cast<const float4*>(x + c), b = *reinterpret_cast<const float4*>(x + c + 4);
-    float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    if (r != 0.f) {
-      float q[8];
-      unpack8(*reinterpret_cast<const u32x4*>(w + c), q);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = fmaf(r, q[j], v[j]);
-    }
-    *reinterpret_cast<u32x4*>(p.d_hidden + row * p.h + c) = pack8(v);
-  }
-}
-
-// d_w[target] += what the parts of g leave x hidden.  A workgroup per token (and 2048
-// columns): the first token of a target adds the rows of all of them, in order, so
-// that the sum does not depend on timing.
+// A workgroup per token and 2048 columns: d_hidden = dh + (g - hi) W[target], and
+// d_w[target] += what the parts of g leave x hidden, where the first token of a target
+// adds the rows of all of them, in order, so that the sum does not depend on timing.
 constexpr int kScan = 1024;          // tokens compared between two barriers
-__global__ void __launch_bounds__(256) loss_finish_dw_kernel(LossTargets p) {
+__global__ void __launch_bounds__(256) loss_finish_grad_kernel(LossTargets p) {
   __shared__ float rest[kScan];
   __shared__ uint64_t hits[kScan / 64];
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t i = blockIdx.x, id = p.targets[i], t = id - p.v0;
-  if (id < 0 || t < 0 || t >= p.v_t) return;
+  const bool here = id >= 0 && t >= 0 && t < p.v_t;
+  const int c = static_cast<int>(blockIdx.y) * 2048 + tid * 8;
+  const bool mine = c < p.h;
+  if (mine) {
+    const float4* x = reinterpret_cast<const float4*>(p.dh + i * p.h + c);
+    const float4 a = x[0], b = x[1];
+    float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (here) {
+      const float g = p.gt[i], r = g - __uint_as_float(static_cast<uint32_t>(f2bf(g)) << 16);
+      float q[8];
+      unpack8(*reinterpret_cast<const u32x4*>(p.w + t * p.h + c), q);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = fmaf(r, q[j], v[j]);
+    }
+    *reinterpret_cast<u32x4*>(p.d_hidden + i * p.h + c) = pack8(v);
+  }
+  if (!here) return;
   for (int64_t j0 = 0; j0 < i; j0 += kScan) {
     bool seen = false;
 #pragma unroll
@@ -816,8 +805,6 @@ __global__ void __launch_bounds__(256) loss_finish_dw_kernel(LossTargets p) {
     }
     if (__syncthreads_or(seen)) return;
   }
-  const int c = static_cast<int>(blockIdx.y) * 2048 + tid * 8;
-  const bool mine = c < p.h;
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (int64_t j0 = i; j0 < p.n; j0 += kScan) {
 #pragma unroll
@@ -1203,10 +1190,6 @@ hipError_t loss_join(const LossJoin& p, hipStream_t stream) {
   hipLaunchKernelGGL(loss_join_kernel, dim3(static_cast<unsigned>((p.n + 63) / 64)), dim3(kJoinWaves * 64), 0, stream, p);
   return hipGetLastError();
 }
-hipError_t loss_finish_dh(const LossTargets& p, hipStream_t stream) {
-  hipLaunchKernelGGL(loss_finish_dh_kernel, dim3(static_cast<unsigned>((p.n + 3) / 4)), dim3(256), 0, stream, p);
-  return hipGetLastError();
-}
 hipError_t repeat_bf16(const uint16_t* x, uint16_t* y, int64_t n, int32_t times, hipStream_t stream) {
   hipLaunchKernelGGL(repeat_bf16_kernel, dim3(static_cast<unsigned>((n / 8 + 255) / 256)), dim3(256), 0, stream, x, y, n / 8,
                      times);
@@ -1216,8 +1199,8 @@ hipError_t zero_f32(float* x, int64_t n, hipStream_t stream) {
   hipLaunchKernelGGL(zero_f32_kernel, dim3(static_cast<unsigned>((n / 4 + 255) / 256)), dim3(256), 0, stream, x, n / 4);
   return hipGetLastError();
 }
-hipError_t loss_finish_dw(const LossTargets& p, hipStream_t stream) {
-  hipLaunchKernelGGL(loss_finish_dw_kernel, dim3(static_cast<unsigned>(p.n), (p.h + 2047) / 2048), dim3(256), 0, stream, p);
+hipError_t loss_finish_grad(const LossTargets& p, hipStream_t stream) {
+  hipLaunchKernelGGL(loss_finish_grad_kernel, dim3(static_cast<unsigned>(p.n), (p.h + 2047) / 2048), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
