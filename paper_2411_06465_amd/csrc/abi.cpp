@@ -887,7 +887,7 @@ struct AttnRows {        // one tensor of a call
   const void* p;
   int64_t ld, heads;
 };
-int attn_shape(const l4d_attn* at, int64_t tokens, int64_t n_seqs, PackedAttn* p) {
+int attn_shape(const l4d_attn* at, PackedAttn* p) {
   if (!at) return fail(L4D_EINVAL, "attn is required");
   if (at->head_dim != 64 && at->head_dim != 128)
     return fail(L4D_EINVAL, "head dim %lld unsupported (64 or 128)", (long long)at->head_dim);
@@ -898,7 +898,6 @@ int attn_shape(const l4d_attn* at, int64_t tokens, int64_t n_seqs, PackedAttn* p
   p->kv_heads = (int32_t)at->n_kv_heads;
   p->d_h = (int32_t)at->head_dim;
   p->scale = at->scale > 0.f ? at->scale : 1.0f / std::sqrt((float)at->head_dim);
-  p->n_split = attn_packed_splits(tokens, n_seqs, at->n_heads, at->n_kv_heads);
   return L4D_OK;
 }
 int attn_rows(const AttnRows* t, int n, int64_t d) {
@@ -932,7 +931,8 @@ PackedWs plan_packed(const PackedAttn& p, int64_t tokens) {
   Carver cv;
   PackedWs w{};
   w.delta = cv.take((uint64_t)p.heads * tokens * 4);
-  w.partial = p.n_split > 1 ? cv.take(2ull * p.n_split * tokens * p.kv_heads * p.d_h * 4) : 0;
+  const int splits = attn_packed_most_splits(tokens, p.heads, p.kv_heads);
+  w.partial = splits > 1 ? cv.take(2ull * splits * tokens * p.kv_heads * p.d_h * 4) : 0;
   w.total = cv.used;
   return w;
 }
@@ -980,7 +980,7 @@ PackedAttn packed_layer_attn(const Shard& x, const LayerPacking& lp, const l4d_s
   p.kv_heads = (int32_t)x.k_t;
   p.d_h = (int32_t)x.d;
   p.scale = 1.0f / std::sqrt((float)x.d);
-  p.n_split = attn_packed_splits(lp.pk->tokens, lp.pk->n_seqs, x.a_t, x.k_t);
+  attn_packed_plan(&p);
   p.q = sptr(st, L4D_STASH_Q);
   p.k = sptr(st, L4D_STASH_K);
   p.v = sptr(st, L4D_STASH_V);
@@ -1589,7 +1589,7 @@ extern "C" int rope_bwd(const l4d_rope* r, int dtype, int64_t tokens, const l4d_
 extern "C" int l4d_attn_packed_workspace_bytes(const l4d_attn* at, int64_t tokens, uint64_t* bytes) {
   if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "tokens must lie in 0 .. 2^30");
   PackedAttn p{};
-  int rc = attn_shape(at, tokens, 1, &p);     // one document: the most slices
+  int rc = attn_shape(at, &p);
   if (rc) return rc;
   if (bytes) *bytes = align_up(plan_packed(p, tokens).total);
   return L4D_OK;
@@ -1601,7 +1601,7 @@ extern "C" int attn_packed_fwd(const l4d_attn* at, const l4d_packing* pk, const 
   int rc = check_packing(pk);
   if (rc) return rc;
   PackedAttn p{};
-  if ((rc = attn_shape(at, pk->tokens, pk->n_seqs, &p))) return rc;
+  if ((rc = attn_shape(at, &p))) return rc;
   const AttnRows t[4] = {{"q", q, q_ld, at->n_heads}, {"k", k, k_ld, at->n_kv_heads}, {"v", v, v_ld, at->n_kv_heads},
                          {"o", o, o_ld, at->n_heads}};
   if ((rc = attn_rows(t, 4, at->head_dim)) || (rc = attn_distinct(t, 4, 3))) return rc;
@@ -1626,7 +1626,7 @@ extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const 
   int rc = check_packing(pk);
   if (rc) return rc;
   PackedAttn p{};
-  if ((rc = attn_shape(at, pk->tokens, pk->n_seqs, &p))) return rc;
+  if ((rc = attn_shape(at, &p))) return rc;
   const int64_t a = at->n_heads, g = at->n_kv_heads;
   const AttnRows t[8] = {{"q", q, q_ld, a}, {"k", k, k_ld, g}, {"v", v, v_ld, g}, {"o", o, o_ld, a},
                          {"d_o", d_o, do_ld, a}, {"dq", dq, dq_ld, a}, {"dk", dk, dk_ld, g}, {"dv", dv, dv_ld, g}};
@@ -1653,6 +1653,7 @@ extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const 
   p.dq_ld = dq_ld, p.dk_ld = dk_ld, p.dv_ld = dv_ld;
   p.delta = reinterpret_cast<float*>(wsb + plan.delta);
   p.dkv_partial = reinterpret_cast<float*>(wsb + plan.partial);
+  attn_packed_plan(&p);
   return packed_attn_backward(p, static_cast<hipStream_t>(stream_ptr));
 }
 

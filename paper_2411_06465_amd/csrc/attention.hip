@@ -1126,22 +1126,39 @@ hipError_t attn_bwd(const AttnParams& p, int part, hipStream_t stream) {
   return hipErrorInvalidValue;
 }
 
-// Slices of a kv head's query heads in the dK/dV pass: one workgroup runs on a CU at
-// a time, and the longest document's first keys make the longest one, so the heads
-// are cut (by 2, by 4) until there are two workgroups a CU, at the price of fp32
-// partial sums, which also push the next kernels' inputs out of the caches.  Four a
-// CU pay where documents are long (the sums grow with the rows, the work with the
-// pairs).  Forward and backward in 1, 2, 4 slices: 32768 tokens in 6 documents, 8/1
-// heads of 128: 4.71, 3.32, 3.05 ms; 8192 tokens in 23, 32/8 heads: 441, 456, 510 us;
-// 16384 tokens in 160, 16/4 heads of 64: 216, 215, 255.  Cutting only the blocks that
-// turn out long on the GPU was slower: the empty workgroups of the other slices
-// upset the order and the spread over the XCDs.
-int attn_packed_splits(int64_t tokens, int64_t n_seqs, int64_t heads, int64_t kv_heads) {
-  const int64_t base = (tokens + 127) / 128 * kv_heads, want = tokens >= 2048 * n_seqs ? 1024 : 512;
-  const int most = packed_hpb(static_cast<int>(heads), static_cast<int>(kv_heads));
+// Slices of a kv head's query heads in the dK/dV pass.  One workgroup runs on a CU at
+// a time, and the longest document's first keys make the longest one; cutting its
+// heads costs fp32 partial sums, which also push the next kernels' inputs out of the
+// caches.
+//  * Fewer than two workgroups a CU: all are cut (by 2, by 4) until there are two a
+//    CU, or four where documents are long (the sums grow with the rows, the work with
+//    the pairs).  32768 tokens in 6 documents, 8/1 heads of 128, forward and backward
+//    in 1, 2, 4 slices: 4.71, 3.32, 3.05 ms.
+//  * Else only the blocks with more query tiles than 64 and than a CU would get if
+//    all documents were equally long, by 2.  8192 tokens in 23 documents, 32/8
+//    heads of 128: none cut 454 us, these 389, all 447; 16384 tokens in 160, 16/4 heads
+//    of 64: 222, 205, 234.
+static int splits_of_all(int64_t base, int64_t want, int most) {
   int n = 1;
   while (base * n < want && n < most) n *= 2;
   return n;
+}
+void attn_packed_plan(PackedAttn* p) {
+  const int64_t tokens = p->pk.tokens, n_seqs = std::max(p->pk.n_seqs, 1), group = p->heads / p->kv_heads;
+  const int64_t base = (tokens + 127) / 128 * p->kv_heads;
+  p->work_cap = 0;
+  if (base < 512) {
+    p->n_split = splits_of_all(base, tokens >= 2048 * n_seqs ? 1024 : 512, packed_hpb(p->heads, p->kv_heads));
+    return;
+  }
+  const double even = static_cast<double>(tokens) * tokens / n_seqs * p->heads / (2.0 * 128 * QT) / 256;
+  p->work_cap = static_cast<int32_t>(std::min(std::max(64.0, even), 1e9));
+  p->n_split = group % 2 == 0 && (tokens + QT - 1) / QT * group > p->work_cap ? 2 : 1;
+}
+int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads) {
+  const int64_t base = (tokens + 127) / 128 * kv_heads;
+  return base < 512 ? splits_of_all(base, 1024, packed_hpb(static_cast<int>(heads), static_cast<int>(kv_heads)))
+                    : (heads / kv_heads % 2 == 0 ? 2 : 1);
 }
 
 bool attn_packed_fits(const PackedAttn& p) {

@@ -338,6 +338,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 //
 // Tiles of 32 queries, from the block's own first row to the document's end, of
 // each head in turn, stream through a ring of four stages.
+// Slices of a kv head's query heads that the keys of a block get whose document goes
+// on for n_rows rows from the block's first one: see attn_packed_plan.
+__device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
+  if (p.work_cap == 0) return p.n_split;
+  return (n_rows + QT - 1) / QT * (p.heads / p.kv_heads) > p.work_cap ? p.n_split : 1;
+}
+
 template <int D>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) attn_packed_dkdv_kernel(PackedAttn p) {
   constexpr int TB = QT * D * 2;
@@ -348,12 +355,20 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = wave & 3, role = wave >> 2;
   const int group = p.heads / p.kv_heads;
-  const int nyz = p.kv_heads * p.n_split;
-  const int slot = static_cast<int>(blockIdx.x) / nyz, yz = static_cast<int>(blockIdx.x) % nyz;
-  const int hk = yz / p.n_split, split = yz % p.n_split, hps = group / p.n_split, head0 = hk * group + split * hps;
+  // Workgroups go to the 8 XCDs in turn.  All blocks cut alike: the slices of a block
+  // are neighbours, so that an XCD keeps to the same heads, whose rows it then has in
+  // its L2.  Only long blocks cut: their further slices come first, all others'
+  // return at once, and nothing is left waiting behind empty workgroups.
+  const int id = static_cast<int>(blockIdx.x), nyz = p.kv_heads * p.n_split, per_split = p.n_slots * p.kv_heads;
+  const bool alike = p.work_cap == 0;
+  const int slot = alike ? id / nyz : id % per_split / p.kv_heads, hk = alike ? id % nyz / p.n_split : id % p.kv_heads;
+  const int split = alike ? id % p.n_split : p.n_split - 1 - id / per_split;
   const SeqBlock blk = seq_block(p.pk, slot, 128, lane);
   if (blk.row0 >= blk.hi) return;
   const int n_rows = blk.hi - blk.row0, n_qt = (n_rows + QT - 1) / QT;
+  const int slices = packed_slices(p, n_rows);
+  if (split >= slices) return;
+  const int hps = group / slices, head0 = hk * group + split * hps;
   const int grp_k0 = blk.row0 + grp * 32;
   const int my_key = grp_k0 + (lane & 31);
   const bool key_ok = my_key < blk.hi;
@@ -549,7 +564,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) acc[dt] *= p.scale;
   }
-  if (p.n_split > 1) {
+  if (slices > 1) {
     const int64_t half = static_cast<int64_t>(p.n_split) * p.pk.tokens * p.kv_heads * D;
     float* out = p.dkv_partial + (role == 1 ? 0 : half) +
                  ((static_cast<int64_t>(split) * p.pk.tokens + my_key) * p.kv_heads + hk) * D;
@@ -571,28 +586,43 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
           u32x2{pack2(acc[dt][4 * jj], acc[dt][4 * jj + 1]), pack2(acc[dt][4 * jj + 2], acc[dt][4 * jj + 3])};
 }
 
-// dK, dV = the sum of the slices' fp32 parts in order.
+// dK, dV = the sum of the slices' fp32 parts in order, for the blocks that were cut:
+// a workgroup per block, kv head and quarter of its rows, eight columns per thread.
 template <int D>
 __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
-  const int slot = static_cast<int>(blockIdx.x), hk = static_cast<int>(blockIdx.y);
+  const int slot = static_cast<int>(blockIdx.x) / 4, hk = static_cast<int>(blockIdx.y);
   const SeqBlock blk = seq_block(p.pk, slot, 128, threadIdx.x & 63);
   if (blk.row0 >= blk.hi) return;
+  const int n_rows = blk.hi - blk.row0, slices = packed_slices(p, n_rows);
+  if (slices == 1) return;
   const int64_t step = static_cast<int64_t>(p.pk.tokens) * p.kv_heads * D;
-  constexpr int C = D / 8;                               // eight columns per thread
-  for (int u = threadIdx.x; u < min(blk.hi - blk.row0, 128) * C; u += 256) {
-    const int64_t row = blk.row0 + u / C;
-    const int col = hk * D + u % C * 8;
+  constexpr int C = D / 8, R = 256 / C;                  // rows at a time
+  const int first = static_cast<int>(blockIdx.x) % 4 * 32;
+  const int col = hk * D + static_cast<int>(threadIdx.x) % C * 8;
+#pragma unroll
+  for (int u = 0; u < 32 / R; ++u) {
+    const int r = first + u * R + static_cast<int>(threadIdx.x) / C;
+    if (r >= n_rows) return;
+    const int64_t row = blk.row0 + r;
+    const float* src = p.dkv_partial + row * p.kv_heads * D + col;
+    float4 v[2][2];
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) v[which][h] = *reinterpret_cast<const float4*>(src + which * p.n_split * step + 4 * h);
+    for (int s = 1; s < slices; ++s)
+#pragma unroll
+      for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 x = *reinterpret_cast<const float4*>(src + (which * p.n_split + s) * step + 4 * h);
+          v[which][h].x += x.x; v[which][h].y += x.y; v[which][h].z += x.z; v[which][h].w += x.w;
+        }
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-      const float* src = p.dkv_partial + which * p.n_split * step + row * p.kv_heads * D + col;
-      float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
-      for (int s = 1; s < p.n_split; ++s) {
-        const float4 x = *reinterpret_cast<const float4*>(src + s * step), y = *reinterpret_cast<const float4*>(src + s * step + 4);
-        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-        b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
-      }
       uint16_t* dst = which ? p.dv + row * p.dv_ld + col : p.dk + row * p.dk_ld + col;
-      *reinterpret_cast<u32x4*>(dst) = u32x4{pack2(a.x, a.y), pack2(a.z, a.w), pack2(b.x, b.y), pack2(b.z, b.w)};
+      *reinterpret_cast<u32x4*>(dst) = u32x4{pack2(v[which][0].x, v[which][0].y), pack2(v[which][0].z, v[which][0].w),
+                                             pack2(v[which][1].x, v[which][1].y), pack2(v[which][1].z, v[which][1].w)};
     }
   }
 }
@@ -620,7 +650,7 @@ hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
     hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, grid, dim3(512), 0, stream, p);
   } else {
     if (p.n_split == 1) return hipSuccess;
-    const dim3 grid(static_cast<unsigned>(packed_slots(p, 128)), p.kv_heads);
+    const dim3 grid(static_cast<unsigned>(packed_slots(p, 128)) * 4, p.kv_heads);
     hipLaunchKernelGGL(attn_packed_reduce_kernel<D>, grid, dim3(256), 0, stream, p);
   }
   return hipGetLastError();

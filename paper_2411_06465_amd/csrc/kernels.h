@@ -267,10 +267,13 @@ struct PackedAttn {
   uint16_t *dq, *dk, *dv;
   int64_t dq_ld, dk_ld, dv_ld;
   float* delta;             // [heads][tokens]: rowsum(dO * O)
-  int32_t n_split;          // slices of a kv head's query heads in the dK/dV pass
+  // dK/dV, set by attn_packed_plan: the query heads of a kv head go in n_split slices, for
+  // all blocks (work_cap 0) or those with more than work_cap query tiles
+  int32_t n_split, work_cap;
   float* dkv_partial;       // n_split > 1: dK [n_split][tokens][kv_heads][d_h], then dV
 };
-int attn_packed_splits(int64_t tokens, int64_t n_seqs, int64_t heads, int64_t kv_heads);
+void attn_packed_plan(PackedAttn* p);                                      // from pk, heads and kv_heads
+int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads);   // over every packing of the tokens
 bool attn_packed_fits(const PackedAttn& p);      // every launch within the grid limits
 hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream);
 // part 2: dQ and delta; 1: dK, dV (after part 2); 3: the sum of the slices (n_split > 1).
