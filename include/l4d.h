@@ -16,7 +16,8 @@
  *    the caller creates over memory it owns.
  *  - Work is enqueued on the caller's HIP stream (hipStream_t passed as
  *    void*, NULL = the null stream); no call synchronizes the device.  An
- *    arena must only be used from one stream at a time.
+ *    arena must only be used from one stream at a time (a captured call keeps its
+ *    arena memory: graphs that share an arena must not run at once).
  *  - bf16 = IEEE-style bfloat16 stored as 16-bit words; f32 = float.
  *  - Activations are token-major: [b][tokens][features], row-major.
  *    Weights are [out_features][in_features], row-major (y = x W^T).
@@ -392,7 +393,7 @@ typedef struct {
  *   columns of a fused [tokens][(a_t + 2 k_t) d_h] array are addressed in place.
  *   y == x with y_ld == x_ld rotates in place; other overlaps of a tensor's input
  *   and output ranges are refused.
- * L4D_EINVAL: head_dim outside 2 .. 512, rot_dim odd or outside 2 .. head_dim, an
+ * L4D_EINVAL: more than 2^25 tokens or 8192 heads, head_dim outside 2 .. 512, rot_dim odd or outside 2 .. head_dim, an
  * unknown enum value, base <= 1, factor <= 0, amplitude <= 0, original <= 0 or not
  * 0 < low < high where the scaling uses them, ld < heads head_dim, NULL or
  * misaligned tensors (element size).  tokens == 0 launches nothing.
@@ -436,7 +437,8 @@ int rope_bwd(const l4d_rope* rope, int dtype, int64_t tokens, const l4d_packing*
  *   the backward.  Outputs must not overlap inputs or each other.
  * The backward overwrites dq, dk, dv with the gradients for d_o (dk and dv summed
  * over the query heads of their head); its sums have a fixed order.  A value that
- * is not finite in one document reaches no other document.
+ * is not finite in one document reaches no other document; within its own it may
+ * reach rows that the mask keeps from it, as 0 x infinity does in a plain product.
  * L4D_EINVAL: head_dim not 64 or 128, n_heads % n_kv_heads != 0, more than 2^16
  * heads, a scale that is negative or not finite, an ld that is smaller than the
  * heads' columns, no multiple of 8 or above 2^22, a NULL tensor or one not 16-byte
@@ -449,7 +451,7 @@ typedef struct {
 
 int attn_packed_fwd(const l4d_attn* attn, const l4d_packing* packing, const void* q, int64_t q_ld, const void* k,
                     int64_t k_ld, const void* v, int64_t v_ld, void* o, int64_t o_ld, float* lse, void* hip_stream);
-/* Arena room of the backward (rowsum(d_o * o) per row and head, and fp32 partial
+/* Arena room of the backward (two floats per row and query head, and fp32 partial
  * sums of dk and dv where the query heads of a key head are split). */
 int l4d_attn_packed_workspace_bytes(const l4d_attn* attn, int64_t tokens, uint64_t* bytes);
 int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void* q, int64_t q_ld, const void* k,

@@ -801,6 +801,8 @@ Packing device_packing(const l4d_packing* pk) {
 
 // ------------------------------------------------------------ rotary positions
 
+constexpr int64_t kMaxRopeRows = (int64_t)1 << 25;   // a wave per row: 2^31 threads of a launch's 2^32
+
 // f_j / 2 pi of every pair, in double.
 int rope_turns(const l4d_rope* r, double* turns) {
   constexpr double kTwoPi = 6.283185307179586476925286766559;
@@ -842,7 +844,7 @@ int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, co
               const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, int inverse, void* stream_ptr) {
   if (!r || !q) return fail(L4D_EINVAL, "rope and q are required");
   if (dtype != L4D_BF16 && dtype != L4D_F32) return fail(L4D_EINVAL, "rope: unknown dtype");
-  if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "rope: tokens must lie in 0 .. 2^30");
+  if (tokens < 0 || tokens > kMaxRopeRows) return fail(L4D_EINVAL, "rope: tokens must lie in 0 .. 2^25");
   int rc;
   if (pk && (rc = check_packing(pk))) return rc;
   if (pk && pk->tokens != tokens) return fail(L4D_EINVAL, "rope: the packing is of another number of tokens");
@@ -854,7 +856,7 @@ int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, co
   for (const l4d_rope_heads* t : in) {
     if (!t) continue;
     if (!t->x || !t->y) return fail(L4D_EINVAL, "rope: a tensor is NULL");
-    if (t->heads < 1 || t->heads > (int64_t)1 << 16) return fail(L4D_EINVAL, "rope: heads must lie in 1 .. 2^16");
+    if (t->heads < 1 || t->heads > 8192) return fail(L4D_EINVAL, "rope: heads must lie in 1 .. 8192");
     const int64_t cols = t->heads * r->head_dim;
     if (t->x_ld < cols || t->y_ld < cols || t->x_ld > (int64_t)1 << 31 || t->y_ld > (int64_t)1 << 31)
       return fail(L4D_EINVAL, "rope: a row stride is shorter than the heads, or above 2^31");
@@ -925,12 +927,13 @@ int packed_attn_backward(const PackedAttn& p, hipStream_t s) {
   return L4D_OK;
 }
 struct PackedWs {
-  uint64_t delta, partial, total;
+  uint64_t delta, lse2, partial, total;
 };
 PackedWs plan_packed(const PackedAttn& p, int64_t tokens) {
   Carver cv;
   PackedWs w{};
   w.delta = cv.take((uint64_t)p.heads * tokens * 4);
+  w.lse2 = cv.take((uint64_t)p.heads * tokens * 4);
   const int splits = attn_packed_most_splits(tokens, p.heads, p.kv_heads);
   w.partial = splits > 1 ? cv.take(2ull * splits * tokens * p.kv_heads * p.d_h * 4) : 0;
   w.total = cv.used;
@@ -969,7 +972,7 @@ int layer_packing(const Shard& x, const l4d_packing* pk, const l4d_rope* rope, L
   p.heads = (int32_t)x.a_t;
   p.kv_heads = (int32_t)x.k_t;
   p.d_h = (int32_t)x.d;
-  if (!attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
+  if (!attn_packed_fits(p) || pk->tokens > kMaxRopeRows) return fail(L4D_EINVAL, "problem too large");
   return L4D_OK;
 }
 // The layer's attention over its documents: Q, K, V, ctx and LSE of the stash.
@@ -1215,6 +1218,7 @@ static int layer_backward(const l4d_model* m, const l4d_parallel* p, const l4d_p
       pa.dout = dctx;
       pa.do_ld = nq;
       pa.delta = delta;
+      pa.lse2 = dxn1;                 // written after the attention; has room for a float per row and head
       pa.dq = dqkv;
       pa.dk = dqkv + nq;
       pa.dv = dqkv + nq + x.k_t * x.d;
@@ -1652,6 +1656,7 @@ extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const 
   p.q_ld = q_ld, p.k_ld = k_ld, p.v_ld = v_ld, p.o_ld = o_ld, p.do_ld = do_ld;
   p.dq_ld = dq_ld, p.dk_ld = dk_ld, p.dv_ld = dv_ld;
   p.delta = reinterpret_cast<float*>(wsb + plan.delta);
+  p.lse2 = reinterpret_cast<float*>(wsb + plan.lse2);
   p.dkv_partial = reinterpret_cast<float*>(wsb + plan.partial);
   attn_packed_plan(&p);
   return packed_attn_backward(p, static_cast<hipStream_t>(stream_ptr));

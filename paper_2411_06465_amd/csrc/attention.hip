@@ -1136,8 +1136,8 @@ hipError_t attn_bwd(const AttnParams& p, int part, hipStream_t stream) {
 //    in 1, 2, 4 slices: 4.71, 3.32, 3.05 ms.
 //  * Else only the blocks with more query tiles than 64 and than a CU would get if
 //    all documents were equally long, by 2.  8192 tokens in 23 documents, 32/8
-//    heads of 128: none cut 454 us, these 389, all 447; 16384 tokens in 160, 16/4 heads
-//    of 64: 222, 205, 234.
+//    heads of 128: none cut 408 us, these 397; 16384 tokens in 160, 16/4 heads of 64:
+//    234 and 215 (all cut: 10% more than none).
 static int splits_of_all(int64_t base, int64_t want, int most) {
   int n = 1;
   while (base * n < want && n < most) n *= 2;

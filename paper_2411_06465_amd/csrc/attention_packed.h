@@ -309,7 +309,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 
   ds_sum += __shfl_xor(ds_sum, 32, 64);
   if (!q_ok) return;
-  if (lane < 32) p.delta[sidx] = my_delta + ds_sum;
+  if (lane < 32) {
+    p.delta[sidx] = my_delta + ds_sum;
+    p.lse2[sidx] = my_lse;
+  }
   uint16_t* out = p.dq + static_cast<int64_t>(my_q) * p.dq_ld + hq * D;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
@@ -349,7 +352,7 @@ template <int D>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) attn_packed_dkdv_kernel(PackedAttn p) {
   constexpr int TB = QT * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t qg[kDkvStages][2][TB];   // per stage: Q tile, then dO tile
-  __shared__ __attribute__((aligned(16))) float st[kDkvStages][2][QT];     // lse, delta
+  __shared__ __attribute__((aligned(16))) float st[kDkvStages][2][QT];     // lse (base 2), delta
   __shared__ __attribute__((aligned(16))) float4 xp[2][4][QT / 16][2][64]; // P handover: [buffer][group][16 queries][half][lane]
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -392,7 +395,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   const uint32_t qg_addr = lds_addr(qg) + role * TB, st_addr = lds_addr(st) + (role * QT + grp * (QT / 4)) * 4;
   // the next tile to copy: its first row, its head's statistics from the block's first row on, its query tile, tiles left after it
   uint64_t src = pick(addr(p.q), addr(p.dout)) + (blk.row0 * ld + head0 * D) * 2;
-  uint64_t row = pick(addr(p.lse), addr(p.delta)) + (static_cast<int64_t>(head0) * p.pk.tokens + blk.row0) * 4;
+  uint64_t row = pick(addr(p.lse2), addr(p.delta)) + (static_cast<int64_t>(head0) * p.pk.tokens + blk.row0) * 4;
   const int64_t tile_step = QT * ld * 2, head_step = D * 2 - (n_qt - 1) * tile_step;
   int copy_qt = 0, copy_left = hps * n_qt - 1;
   // Copies that tile into stage b, kCopies per wave, and moves on; past the last
@@ -438,7 +441,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
     for (int jj = 0; jj < 4; ++jj) {
       const float4 ls = ls4[jj];
-      const float lsv[4] = {ls.x * kLog2e, ls.y * kLog2e, ls.z * kLog2e, ls.w * kLog2e};
+      const float lsv[4] = {ls.x, ls.y, ls.z, ls.w};      // in base 2, as dQ left it
 #pragma unroll
       for (int u = 0; u < 4; ++u) s[4 * jj + u] = fast_exp2(fmaf(s[4 * jj + u], c, -lsv[u]));
     }

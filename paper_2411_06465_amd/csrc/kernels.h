@@ -266,7 +266,7 @@ struct PackedAttn {
   int64_t do_ld;
   uint16_t *dq, *dk, *dv;
   int64_t dq_ld, dk_ld, dv_ld;
-  float* delta;             // [heads][tokens]: rowsum(dO * O)
+  float *delta, *lse2;      // [heads][tokens], written by the dQ pass: rowsum(dO * O), lse in base 2
   // dK/dV, set by attn_packed_plan: the query heads of a kv head go in n_split slices, for
   // all blocks (work_cap 0) or those with more than work_cap query tiles
   int32_t n_split, work_cap;

@@ -1168,6 +1168,7 @@ hipError_t rope_rotate(const RopeRotate& params, hipStream_t stream) {
     const bool in_place = p.t[t].x == p.t[t].y;      // the rest of a head stays where it is
     p.first_rest[t] = p.rot / 2 / V;
     p.units[t] = p.first_rest[t] + (in_place ? 0 : (p.d_h - p.rot) / V);
+    // exact for fewer than 2^32 / units units: 8192 heads of at most 511 units
     p.magic[t] = static_cast<uint32_t>(((uint64_t{1} << 32) + p.units[t] - 1) / p.units[t]);
     most = std::max(most, static_cast<int64_t>(p.units[t]) * p.t[t].heads);
   }

@@ -48,6 +48,7 @@ CASES = [  # n, heads, kv, d, rot, layout, scaling, dtype, inverse
     (17, 3, 1, 66, 66, "interleaved", "linear", BF16, True),
     (9, 2, 2, 512, 512, "half", "none", F32, False),       # the largest head
     (2050, 16, 4, 64, 32, "half", "bands", BF16, False),
+    (2, 8192, 1, 512, 2, "half", "none", BF16, False),     # the most units per row, in pairs and single elements
 ]
 
 

@@ -60,12 +60,12 @@ def test_rope_refuses_arguments():
     assert rope_rc(r) == L.L4D_EINVAL
     assert rope_rc(dtype=2) == L.L4D_EINVAL
     assert rope_rc(tokens=-1) == L.L4D_EINVAL
-    assert rope_rc(tokens=(1 << 30) + 1) == L.L4D_EINVAL
+    assert rope_rc(tokens=(1 << 25) + 1) == L.L4D_EINVAL
     assert rope_rc(packing=pack(63)) == L.L4D_EINVAL
     assert rope_rc(packing=pack(64, 2, None)) == L.L4D_EINVAL
     assert rope_rc(packing=pack(64, -1)) == L.L4D_EINVAL
     assert rope_rc(positions=C.c_void_p(BASE + 4)) == L.L4D_EINVAL
-    for q in (heads(x=None), heads(y=None), heads(n=0), heads(n=(1 << 16) + 1), heads(x_ld=255), heads(y_ld=255),
+    for q in (heads(x=None), heads(y=None), heads(n=0), heads(n=8193, x_ld=1 << 20, y_ld=1 << 20), heads(x_ld=255), heads(y_ld=255),
               heads(x=BASE + 1), heads(y=BASE + 1), heads(y=BASE + 512), heads(y=BASE, y_ld=512)):
         assert rope_rc(q=q) == L.L4D_EINVAL
         assert rope_rc(k=q) == L.L4D_EINVAL
