@@ -17,6 +17,44 @@
 // short ones (16384 tokens in 160).
 constexpr float kLargeP = 1.f / 8;
 
+// Stores 32 rows of D columns (times mul) that a wave holds transposed (the lane's row
+// lane % 32, register i of tile dt column 32 dt + acc_row(i)) as bf16, rows [0, n_rows)
+// of them, through 64 D bytes of LDS that no other wave uses: stored straight from
+// the registers, an instruction wrote 16 bytes to each of 32 rows (16384 tokens in
+// documents of 128, 32/8 heads of 128: forward 97 -> 84 us, dQ 152 -> 137, dK/dV 221 ->
+// 201).
+template <int D>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float mul, uint8_t* lds, uint16_t* out, int64_t ld,
+                                           int n_rows, int lane) {
+  constexpr int C = D / 8;                       // 16-byte chunks of a row; chunk c of row r sits at c ^ (r % C)
+  const int r = lane & 31, upper = lane >> 5;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int jj = 0; jj < 4; jj += 2) {
+      // the half-waves hold columns 0-3 and 4-7 of every 8: the lower one collects chunk jj, the upper chunk jj + 1
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int i = 4 * jj + 2 * k;
+        const u32x2 x = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_permlane32_swap(pack2(acc[dt][i] * mul, acc[dt][i + 1] * mul),
+                                                    pack2(acc[dt][i + 4] * mul, acc[dt][i + 5] * mul), false, false));
+        w[k] = x[0];
+        w[k + 2] = x[1];
+      }
+      const int c = 4 * dt + jj + upper;
+      *reinterpret_cast<u32x4*>(lds + r * (2 * D) + ((c ^ (r & (C - 1))) << 4)) = u32x4{w[0], w[1], w[2], w[3]};
+    }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 32 * C / 64; ++j) {
+    const int row = j * (64 / C) + lane / C, c = lane % C;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + row * (2 * D) + ((c ^ (row & (C - 1))) << 4));
+    if (row < n_rows) *reinterpret_cast<u32x4*>(out + row * ld + c * 8) = v;
+  }
+}
+
 // ------------------------------------------------------------------ forward
 // One workgroup per block of query rows and hpb query heads of one kv head: 4
 // waves x 32 rows, wave w on head w % hpb.  Each lane holds one query's scores
@@ -179,18 +217,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
 
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-  if (!q_ok) return;
-  const float inv = 1.0f / l_tot;
-  uint16_t* ob = p.o + static_cast<int64_t>(my_q) * p.o_ld + hq * D;
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int jj = 0; jj < 4; ++jj) {
-      const int d = dt * 32 + 8 * jj + rbase;
-      *reinterpret_cast<u32x2*>(ob + d) = u32x2{pack2(o[dt][4 * jj] * inv, o[dt][4 * jj + 1] * inv),
-                                                pack2(o[dt][4 * jj + 2] * inv, o[dt][4 * jj + 3] * inv)};
-    }
-  if (lane < 32) p.lse[static_cast<int64_t>(hq) * p.pk.tokens + my_q] = (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2;
+  ring_barrier();                        // every wave is done with the tiles: each takes a quarter of a buffer
+  uint8_t* mine = (wave == 0 ? k0 : wave == 1 ? k1 : wave == 2 ? v0 : v1);
+  store_rows<D>(o, 1.0f / l_tot, mine, p.o + static_cast<int64_t>(wave_q0) * p.o_ld + hq * D, p.o_ld, blk.hi - wave_q0, lane);
+  if (q_ok && lane < 32)
+    p.lse[static_cast<int64_t>(hq) * p.pk.tokens + my_q] = (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2;
 }
 
 // ------------------------------------------------------------------ backward: dQ
@@ -308,21 +339,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
 
   ds_sum += __shfl_xor(ds_sum, 32, 64);
-  if (!q_ok) return;
-  if (lane < 32) {
+  if (q_ok && lane < 32) {
     p.delta[sidx] = my_delta + ds_sum;
     p.lse2[sidx] = my_lse;
   }
-  uint16_t* out = p.dq + static_cast<int64_t>(my_q) * p.dq_ld + hq * D;
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int jj = 0; jj < 4; ++jj) {
-      const int d = dt * 32 + 8 * jj + rbase;
-      *reinterpret_cast<u32x2*>(out + d) =
-          u32x2{pack2(dq[dt][4 * jj] * p.scale, dq[dt][4 * jj + 1] * p.scale),
-                pack2(dq[dt][4 * jj + 2] * p.scale, dq[dt][4 * jj + 3] * p.scale)};
-    }
+  ring_barrier();                        // every wave is done with the tiles: each takes a buffer
+  store_rows<D>(dq, p.scale, wave < 2 ? kbuf[wave & 1] : vbuf[wave & 1], p.dq + static_cast<int64_t>(wave_q0) * p.dq_ld + hq * D,
+                p.dq_ld, blk.hi - wave_q0, lane);
 }
 
 // ------------------------------------------------------------------ backward: dK, dV
@@ -341,6 +364,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 //
 // Tiles of 32 queries, from the block's own first row to the document's end, of
 // each head in turn, stream through a ring of four stages.
+// Windows of 128 rows from row 0 on.
+__host__ __device__ __forceinline__ int packed_windows(const PackedAttn& p) { return (p.pk.tokens + 127) / 128; }
+
 // Slices of a kv head's query heads that the keys of a block get whose document goes
 // on for n_rows rows from the block's first one: see attn_packed_plan.
 __device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
@@ -360,13 +386,17 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int group = p.heads / p.kv_heads;
   // Workgroups go to the 8 XCDs in turn.  All blocks cut alike: the slices of a block
   // are neighbours, so that an XCD keeps to the same heads, whose rows it then has in
-  // its L2.  Only long blocks cut: their further slices come first, all others'
+  // its L2.  Only long blocks cut: their second slices come first, found by the one
+  // multiple of 128 among a block's rows (long blocks are whole), the other blocks'
   // return at once, and nothing is left waiting behind empty workgroups.
-  const int id = static_cast<int>(blockIdx.x), nyz = p.kv_heads * p.n_split, per_split = p.n_slots * p.kv_heads;
+  const int id = static_cast<int>(blockIdx.x), nyz = p.kv_heads * p.n_split;
   const bool alike = p.work_cap == 0;
-  const int slot = alike ? id / nyz : id % per_split / p.kv_heads, hk = alike ? id % nyz / p.n_split : id % p.kv_heads;
-  const int split = alike ? id % p.n_split : p.n_split - 1 - id / per_split;
-  const SeqBlock blk = seq_block(p.pk, slot, 128, lane);
+  const int extra = alike ? 0 : (p.n_split - 1) * packed_windows(p) * p.kv_heads;
+  const bool second = id < extra;
+  const int hk = alike ? id % nyz / p.n_split : (second ? id : id - extra) % p.kv_heads;
+  const int split = alike ? id % p.n_split : second;
+  const SeqBlock blk = second ? block_at(p.pk, id / p.kv_heads * 128, lane)
+                              : seq_block(p.pk, alike ? id / nyz : (id - extra) / p.kv_heads, 128, lane);
   if (blk.row0 >= blk.hi) return;
   const int n_rows = blk.hi - blk.row0, n_qt = (n_rows + QT - 1) / QT;
   const int slices = packed_slices(p, n_rows);
@@ -561,13 +591,10 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
   wait_copies<0>();      // no copy may land after the end
 
-  if (!key_ok) return;
-  // lane owns key my_key; register i of tile dt is d = 32 dt + acc_row(i)
-  if (role == 1) {
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) acc[dt] *= p.scale;
-  }
+  const float mul = role == 1 ? p.scale : 1.f;
   if (slices > 1) {
+    if (!key_ok) return;
+    // lane owns key my_key; register i of tile dt is d = 32 dt + acc_row(i)
     const int64_t half = static_cast<int64_t>(p.n_split) * p.pk.tokens * p.kv_heads * D;
     float* out = p.dkv_partial + (role == 1 ? 0 : half) +
                  ((static_cast<int64_t>(split) * p.pk.tokens + my_key) * p.kv_heads + hk) * D;
@@ -576,25 +603,22 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int jj = 0; jj < 4; ++jj)
         *reinterpret_cast<float4*>(out + dt * 32 + 8 * jj + rbase) =
-            make_float4(acc[dt][4 * jj], acc[dt][4 * jj + 1], acc[dt][4 * jj + 2], acc[dt][4 * jj + 3]);
+            make_float4(acc[dt][4 * jj] * mul, acc[dt][4 * jj + 1] * mul, acc[dt][4 * jj + 2] * mul, acc[dt][4 * jj + 3] * mul);
     return;
   }
+  ring_barrier();          // every wave is done with the ring, which takes the rows now
   uint16_t* out = reinterpret_cast<uint16_t*>(pick(addr(p.dv), addr(p.dk))) +
-                  static_cast<int64_t>(pick(p.dv_ld, p.dk_ld)) * my_key + hk * D;
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int jj = 0; jj < 4; ++jj)
-      *reinterpret_cast<u32x2*>(out + dt * 32 + 8 * jj + rbase) =
-          u32x2{pack2(acc[dt][4 * jj], acc[dt][4 * jj + 1]), pack2(acc[dt][4 * jj + 2], acc[dt][4 * jj + 3])};
+                  static_cast<int64_t>(pick(p.dv_ld, p.dk_ld)) * grp_k0 + hk * D;
+  // a wave's 64 D bytes of the ring
+  store_rows<D>(acc, mul, &qg[0][0][0] + wave * (64 * D), out, pick(p.dv_ld, p.dk_ld), blk.hi - grp_k0, lane);
 }
 
 // dK, dV = the sum of the slices' fp32 parts in order, for the blocks that were cut:
 // a workgroup per block, kv head and quarter of its rows, eight columns per thread.
 template <int D>
 __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
-  const int slot = static_cast<int>(blockIdx.x) / 4, hk = static_cast<int>(blockIdx.y);
-  const SeqBlock blk = seq_block(p.pk, slot, 128, threadIdx.x & 63);
+  const int hk = static_cast<int>(blockIdx.y), lane = static_cast<int>(threadIdx.x) & 63, at = static_cast<int>(blockIdx.x) / 4;
+  const SeqBlock blk = p.work_cap ? block_at(p.pk, at * 128, lane) : seq_block(p.pk, at, 128, lane);
   if (blk.row0 >= blk.hi) return;
   const int n_rows = blk.hi - blk.row0, slices = packed_slices(p, n_rows);
   if (slices == 1) return;
@@ -649,11 +673,11 @@ hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
     else hipLaunchKernelGGL(attn_packed_dq_kernel<D>, grid, dim3(256), 0, stream, p);
   } else if (part == 1) {
     p.n_slots = static_cast<int32_t>(packed_slots(p, 128));
-    const dim3 grid(static_cast<unsigned>(p.n_slots) * p.kv_heads * p.n_split);
-    hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, grid, dim3(512), 0, stream, p);
+    const unsigned blocks = p.work_cap ? p.n_slots + (p.n_split - 1) * packed_windows(p) : p.n_slots * p.n_split;
+    hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, dim3(blocks * p.kv_heads), dim3(512), 0, stream, p);
   } else {
     if (p.n_split == 1) return hipSuccess;
-    const dim3 grid(static_cast<unsigned>(packed_slots(p, 128)) * 4, p.kv_heads);
+    const dim3 grid(static_cast<unsigned>(p.work_cap ? packed_windows(p) : packed_slots(p, 128)) * 4, p.kv_heads);
     hipLaunchKernelGGL(attn_packed_reduce_kernel<D>, grid, dim3(256), 0, stream, p);
   }
   return hipGetLastError();

@@ -71,4 +71,10 @@ __device__ __forceinline__ SeqBlock seq_block(const Packing& p, int slot, int ro
   return SeqBlock{s.lo, s.hi, s.lo + t * rows};
 }
 
+// The block of 128 rows that holds `row`.
+__device__ __forceinline__ SeqBlock block_at(const Packing& p, int row, int lane) {
+  const SeqRows s = seq_of_row(p, row, lane);
+  return row < s.hi ? SeqBlock{s.lo, s.hi, s.lo + (row - s.lo) / 128 * 128} : SeqBlock{0, 0, 0};
+}
+
 }  // namespace l4d
