@@ -927,13 +927,14 @@ int packed_attn_backward(const PackedAttn& p, hipStream_t s) {
   return L4D_OK;
 }
 struct PackedWs {
-  uint64_t delta, lse2, partial, total;
+  uint64_t delta, lse2, items, partial, total;
 };
 PackedWs plan_packed(const PackedAttn& p, int64_t tokens) {
   Carver cv;
   PackedWs w{};
   w.delta = cv.take((uint64_t)p.heads * tokens * 4);
   w.lse2 = cv.take((uint64_t)p.heads * tokens * 4);
+  w.items = cv.take((uint64_t)attn_packed_items(tokens) * 8);
   const int splits = attn_packed_most_splits(tokens, p.heads, p.kv_heads);
   w.partial = splits > 1 ? cv.take(2ull * splits * tokens * p.kv_heads * p.d_h * 4) : 0;
   w.total = cv.used;
@@ -1219,6 +1220,7 @@ static int layer_backward(const l4d_model* m, const l4d_parallel* p, const l4d_p
       pa.do_ld = nq;
       pa.delta = delta;
       pa.lse2 = dxn1;                 // written after the attention; has room for a float per row and head
+      pa.items = reinterpret_cast<int32_t*>(rope);   // no table of equal rows here; its 8 (d/2) bytes per row are enough
       pa.dq = dqkv;
       pa.dk = dqkv + nq;
       pa.dv = dqkv + nq + x.k_t * x.d;
@@ -1657,6 +1659,7 @@ extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const 
   p.dq_ld = dq_ld, p.dk_ld = dk_ld, p.dv_ld = dv_ld;
   p.delta = reinterpret_cast<float*>(wsb + plan.delta);
   p.lse2 = reinterpret_cast<float*>(wsb + plan.lse2);
+  p.items = reinterpret_cast<int32_t*>(wsb + plan.items);
   p.dkv_partial = reinterpret_cast<float*>(wsb + plan.partial);
   attn_packed_plan(&p);
   return packed_attn_backward(p, static_cast<hipStream_t>(stream_ptr));

@@ -66,7 +66,7 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float mu
 // per CU.  The output and the row sum are rescaled only on tiles where some row's
 // maximum grew (a wave-wide vote).
 template <int D>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) attn_packed_fwd_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_fwd_kernel(PackedAttn p) {
   constexpr int TB = KT * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t k0[TB], v0[TB], k1[TB], v1[TB];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -224,6 +224,69 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     p.lse[static_cast<int64_t>(hq) * p.pk.tokens + my_q] = (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2;
 }
 
+// ------------------------------------------------------------------ backward: order of the blocks of keys
+// Windows of 128 rows from row 0 on.
+__host__ __device__ __forceinline__ int packed_windows(const PackedAttn& p) { return (p.pk.tokens + 127) / 128; }
+
+// Slices of a kv head's query heads that the keys of a block get whose document goes
+// on for n_rows rows from the block's first one: see attn_packed_plan.
+__device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
+  if (p.work_cap == 0) return p.n_split;
+  return (n_rows + QT - 1) / QT * (p.heads / p.kv_heads) > p.work_cap ? p.n_split : 1;
+}
+
+// Workgroup 0 of the dQ pass lists the blocks of keys for the dK/dV pass, longest
+// first, as {first row, sign bit: second slice; end of the document} behind their
+// number: a counting sort by work in steps of 1/16 octave.  Workgroups start in order
+// and last as long as their document has rows left; in the order of the rows, long ones
+// started last and the dispatch waited on shader engines that held long ones.
+constexpr int kOrderBins = 512;
+__device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n_slots = p.pk.tokens / 128 + p.pk.n_seqs, room = p.pk.tokens + packed_windows(p);
+  const int group = p.heads / p.kv_heads;
+  int2* items = reinterpret_cast<int2*>(p.items) + 1;
+  for (int i = tid; i < kOrderBins; i += 256) bin[i] = 0;
+  __syncthreads();
+  const auto each = [&](auto visit) __attribute__((always_inline)) {
+    for (int s0 = wave * 64; s0 < n_slots; s0 += 256) {
+      const SeqBlock b = seq_blocks(p.pk, s0, 128, lane);
+      if (s0 + lane >= n_slots || b.row0 >= b.hi) continue;
+      const int n_rows = b.hi - b.row0, slices = packed_slices(p, n_rows);
+      const float work = static_cast<float>((n_rows + QT - 1) / QT) * (group / slices);
+      visit(b, static_cast<int>(__float_as_uint(work) >> 19) - (127 << 4), p.work_cap ? slices : 1);
+    }
+  };
+  each([&](const SeqBlock&, int k, int n) { atomicAdd(&bin[k], n); });
+  __syncthreads();
+  if (wave == 0) {                       // entries in fuller bins, for every bin
+    constexpr int M = kOrderBins / 64;
+    int* mine = bin + (63 - lane) * M;
+    int sum = 0;
+#pragma unroll
+    for (int i = M - 1; i >= 0; --i) sum += mine[i];
+    int upto = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int x = __shfl_up(upto, d, 64);
+      if (lane >= d) upto += x;
+    }
+    if (lane == 63) p.items[0] = min(upto, room);
+    int at = upto - sum;
+#pragma unroll
+    for (int i = M - 1; i >= 0; --i) {
+      const int n = mine[i];
+      mine[i] = at;
+      at += n;
+    }
+  }
+  __syncthreads();
+  each([&](const SeqBlock& b, int k, int n) {
+    const int at = atomicAdd(&bin[k], n);
+    for (int j = 0; j < n && at + j < room; ++j) items[at + j] = make_int2(b.row0 | (j ? INT32_MIN : 0), b.hi);
+  });
+}
+
 // ------------------------------------------------------------------ backward: dQ
 // The forward's blocks.  Per key tile: S^T = K Q^T and dP^T = V dO^T, then
 // dS^T = P^T (dP^T - delta) feeds dQ^T += K^T dS^T from registers.
@@ -235,14 +298,15 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 // The dQ of later rows uses the uncorrected delta; where the error counts, a
 // probability is large and dS enters the product in two parts (kLargeP).
 template <int D>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) attn_packed_dq_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_dq_kernel(PackedAttn p) {
   constexpr int KQ = 32;                     // keys per tile
   constexpr int TB = KQ * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t kbuf[2][TB], vbuf[2][TB];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_hg = p.heads / p.hpb, rows = 128 / p.hpb;
-  const int slot = p.n_slots - 1 - static_cast<int>(blockIdx.x) / n_hg, h0 = static_cast<int>(blockIdx.x) % n_hg * p.hpb;
+  if (blockIdx.x == 0) return packed_order(p, reinterpret_cast<int*>(kbuf));
+  const int id = static_cast<int>(blockIdx.x) - 1, slot = p.n_slots - 1 - id / n_hg, h0 = id % n_hg * p.hpb;
   const SeqBlock blk = seq_block(p.pk, slot, rows, lane);
   if (blk.row0 >= blk.hi) return;
   const int hq = h0 + wave % p.hpb, hk = h0 / (p.heads / p.kv_heads);
@@ -364,18 +428,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 //
 // Tiles of 32 queries, from the block's own first row to the document's end, of
 // each head in turn, stream through a ring of four stages.
-// Windows of 128 rows from row 0 on.
-__host__ __device__ __forceinline__ int packed_windows(const PackedAttn& p) { return (p.pk.tokens + 127) / 128; }
-
-// Slices of a kv head's query heads that the keys of a block get whose document goes
-// on for n_rows rows from the block's first one: see attn_packed_plan.
-__device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
-  if (p.work_cap == 0) return p.n_split;
-  return (n_rows + QT - 1) / QT * (p.heads / p.kv_heads) > p.work_cap ? p.n_split : 1;
-}
-
 template <int D>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) attn_packed_dkdv_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) attn_packed_dkdv_kernel(PackedAttn p) {
   constexpr int TB = QT * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t qg[kDkvStages][2][TB];   // per stage: Q tile, then dO tile
   __shared__ __attribute__((aligned(16))) float st[kDkvStages][2][QT];     // lse (base 2), delta
@@ -384,23 +438,17 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = wave & 3, role = wave >> 2;
   const int group = p.heads / p.kv_heads;
-  // Workgroups go to the 8 XCDs in turn.  All blocks cut alike: the slices of a block
-  // are neighbours, so that an XCD keeps to the same heads, whose rows it then has in
-  // its L2.  Only long blocks cut: their second slices come first, found by the one
-  // multiple of 128 among a block's rows (long blocks are whole), the other blocks'
-  // return at once, and nothing is left waiting behind empty workgroups.
-  const int id = static_cast<int>(blockIdx.x), nyz = p.kv_heads * p.n_split;
-  const bool alike = p.work_cap == 0;
-  const int extra = alike ? 0 : (p.n_split - 1) * packed_windows(p) * p.kv_heads;
-  const bool second = id < extra;
-  const int hk = alike ? id % nyz / p.n_split : (second ? id : id - extra) % p.kv_heads;
-  const int split = alike ? id % p.n_split : second;
-  const SeqBlock blk = second ? block_at(p.pk, id / p.kv_heads * 128, lane)
-                              : seq_block(p.pk, alike ? id / nyz : (id - extra) / p.kv_heads, 128, lane);
-  if (blk.row0 >= blk.hi) return;
+  // Workgroups go to the 8 XCDs in turn: the kv heads of a block are neighbours, and the
+  // slices where all blocks are cut, so that an XCD keeps to the same heads, whose
+  // rows it then has in its L2.
+  const int id = static_cast<int>(blockIdx.x), cut = p.work_cap ? 1 : p.n_split, at = id / (p.kv_heads * cut);
+  const int n_items = p.items[0];
+  const int2 item = reinterpret_cast<const int2*>(p.items)[1 + at];
+  if (at >= n_items) return;
+  const int hk = id % (p.kv_heads * cut) / cut, split = p.work_cap ? item.x < 0 : id % cut;
+  const struct { int row0, hi; } blk{item.x & INT32_MAX, item.y};
   const int n_rows = blk.hi - blk.row0, n_qt = (n_rows + QT - 1) / QT;
   const int slices = packed_slices(p, n_rows);
-  if (split >= slices) return;
   const int hps = group / slices, head0 = hk * group + split * hps;
   const int grp_k0 = blk.row0 + grp * 32;
   const int my_key = grp_k0 + (lane & 31);
@@ -668,12 +716,12 @@ hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
   if (part == 0 || part == 2) {
     p.hpb = packed_hpb(p.heads, p.kv_heads);
     p.n_slots = static_cast<int32_t>(packed_slots(p, 128 / p.hpb));
-    const dim3 grid(static_cast<unsigned>(p.n_slots) * (p.heads / p.hpb));
+    const dim3 grid(static_cast<unsigned>(p.n_slots) * (p.heads / p.hpb) + (part == 2));    // and the workgroup that lists
     if (part == 0) hipLaunchKernelGGL(attn_packed_fwd_kernel<D>, grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL(attn_packed_dq_kernel<D>, grid, dim3(256), 0, stream, p);
   } else if (part == 1) {
-    p.n_slots = static_cast<int32_t>(packed_slots(p, 128));
-    const unsigned blocks = p.work_cap ? p.n_slots + (p.n_split - 1) * packed_windows(p) : p.n_slots * p.n_split;
+    const int64_t most = std::min<int64_t>(packed_slots(p, 128), p.pk.tokens);     // blocks with a row
+    const unsigned blocks = static_cast<unsigned>(p.work_cap ? most + (p.n_split - 1) * packed_windows(p) : most * p.n_split);
     hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, dim3(blocks * p.kv_heads), dim3(512), 0, stream, p);
   } else {
     if (p.n_split == 1) return hipSuccess;

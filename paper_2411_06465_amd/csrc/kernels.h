@@ -270,12 +270,14 @@ struct PackedAttn {
   // dK/dV, set by attn_packed_plan: the query heads of a kv head go in n_split slices, for
   // all blocks (work_cap 0) or those with more than work_cap query tiles
   int32_t n_split, work_cap;
+  int32_t* items;           // attn_packed_items(pk.tokens) x 8 bytes, written by the dQ pass: its blocks of keys in order
   float* dkv_partial;       // n_split > 1: dK [n_split][tokens][kv_heads][d_h], then dV
 };
 void attn_packed_plan(PackedAttn* p);                                      // from pk, heads and kv_heads
 int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads);   // over every packing of the tokens
 bool attn_packed_fits(const PackedAttn& p);      // every launch within the grid limits
 hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream);
+inline int64_t attn_packed_items(int64_t tokens) { return tokens ? 1 + tokens + (tokens + 127) / 128 : 0; }
 // part 2: dQ and delta; 1: dK, dV (after part 2); 3: the sum of the slices (n_split > 1).
 hipError_t attn_packed_bwd(PackedAttn p, int part, hipStream_t stream);
 
