@@ -451,8 +451,8 @@ typedef struct {
 
 int attn_packed_fwd(const l4d_attn* attn, const l4d_packing* packing, const void* q, int64_t q_ld, const void* k,
                     int64_t k_ld, const void* v, int64_t v_ld, void* o, int64_t o_ld, float* lse, void* hip_stream);
-/* Arena room of the backward (two floats per row and query head, and fp32 partial
- * sums of dk and dv where the query heads of a key head are split). */
+/* Arena room of the backward: two floats per row and query head, about 8 bytes per row,
+ * and fp32 partial sums of dk and dv where the query heads of a key head are split. */
 int l4d_attn_packed_workspace_bytes(const l4d_attn* attn, int64_t tokens, uint64_t* bytes);
 int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void* q, int64_t q_ld, const void* k,
                     int64_t k_ld, const void* v, int64_t v_ld, const void* o, int64_t o_ld, const float* lse,

@@ -1133,11 +1133,13 @@ hipError_t attn_bwd(const AttnParams& p, int part, hipStream_t stream) {
 //  * Fewer than two workgroups a CU: all are cut (by 2, by 4) until there are two a
 //    CU, or four where documents are long (the sums grow with the rows, the work with
 //    the pairs).  32768 tokens in 6 documents, 8/1 heads of 128, forward and backward
-//    in 1, 2, 4 slices: 4.71, 3.32, 3.05 ms.
+//    in 1, 2, 4 slices: 4.82, 3.38, 2.98 ms.
 //  * Else only the blocks with more query tiles than 64 and than a CU would get if
 //    all documents were equally long, by 2.  8192 tokens in 23 documents, 32/8
-//    heads of 128: none cut 408 us, these 397; 16384 tokens in 160, 16/4 heads of 64:
-//    234 and 215 (all cut: 10% more than none).
+//    heads of 128: none cut 361 us, these 351; 16384 tokens in 160, 16/4 heads of 64:
+//    172 and 138.  Limits of 1, 2.25, 4 times the even share, backward: 6 documents of
+//    8192 tokens, 32/8 heads of 128, 588, 606, 625 us; 23: 313, 301, 320; 200 of
+//    65536, 8/1 heads of 64, 285, 276, 346.
 static int splits_of_all(int64_t base, int64_t want, int most) {
   int n = 1;
   while (base * n < want && n < most) n *= 2;
@@ -1164,7 +1166,7 @@ int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads) {
 bool attn_packed_fits(const PackedAttn& p) {
   // a grid holds less than 2^32 threads; slots of the smallest query blocks (32 rows) and of the key blocks
   const int64_t q = packed_slots(p, 32) * p.heads, k = packed_slots(p, 128) * p.heads;
-  return q < (int64_t{1} << 24) && k < (int64_t{1} << 23);
+  return q + 1 < (int64_t{1} << 24) && k < (int64_t{1} << 23);
 }
 
 hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream) {

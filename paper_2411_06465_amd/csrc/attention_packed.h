@@ -63,8 +63,14 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float mu
 // Key tiles of 64; while tile j's softmax runs, the products of tile j + 1's scores
 // are issued between its exponentials, and then tile j's P V products.  Two
 // buffers each for K and V; 64 KB of LDS and at most 256 registers, two workgroups
-// per CU.  The output and the row sum are rescaled only on tiles where some row's
-// maximum grew (a wave-wide vote).
+// per CU (heads of 64: half the LDS, three; 38 -> 34 us for 16384 tokens in 160
+// documents, 16/4 heads).  The output and the row sum are rescaled only on tiles
+// where some row's maximum grew (a wave-wide vote).
+//
+// Long documents are bound by exponentials and other vector work beside the products,
+// at a power-limited clock: 32768 tokens in 6, 8/1 heads of 128, 670 us, 1.0 PFLOP/s,
+// matrix cores busy 51% at 1.76 GHz.  Short ones by the way to the first products, about
+// 4 us of a workgroup's 6 to 20: 8192 tokens in 23, 32/8 heads of 128, 85 us.
 template <int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_fwd_kernel(PackedAttn p) {
   constexpr int TB = KT * D * 2;
@@ -239,7 +245,11 @@ __device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
 // first, as {first row, sign bit: second slice; end of the document} behind their
 // number: a counting sort by work in steps of 1/16 octave.  Workgroups start in order
 // and last as long as their document has rows left; in the order of the rows, long ones
-// started last and the dispatch waited on shader engines that held long ones.
+// started last, and short ones waited behind parts of the chip that held long ones
+// (8192 tokens in 23 documents, 32/8 heads of 128: 157 of 256 CUs busy on average).  dK/dV
+// 187 -> 152 us there, 1378 -> 1305 for 32768 tokens in 6, 8/1 heads, 90 -> 59 for 16384
+// in 160, 16/4 heads of 64.  The list hides behind the other workgroups' dQ.  Its order
+// within a step varies, the sums do not.
 constexpr int kOrderBins = 512;
 __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -297,6 +307,10 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
 // 32 rows of a document, which one tile covers, have it before dQ's product too.
 // The dQ of later rows uses the uncorrected delta; where the error counts, a
 // probability is large and dS enters the product in two parts (kLargeP).
+//
+// Bound as the forward is: 32768 tokens in 6 documents, 8/1 heads of 128, 965 us (1.0
+// PFLOP/s, busy 52% at 1.86 GHz); 8192 in 23, 32/8 heads, 120 us; 16384 in 160, 16/4
+// heads of 64, 43 us (48 with two workgroups per CU, here three).
 template <int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_dq_kernel(PackedAttn p) {
   constexpr int KQ = 32;                     // keys per tile
@@ -422,12 +436,18 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 //    accumulates dK^T += Q^T dS.
 // Each then needs one operand and one accumulator block, which fits 256 registers
 // (two waves per SIMD), and the softmax of one wave runs under the products of
-// the other.  One wave per group doing both (one wave per SIMD) took 4064 us where
-// this takes 1580 (32768 tokens in 6 documents, 8/1 heads of 128), 441 and 200 (8192
-// tokens in 23, 32/8 heads).
+// the other.  One wave per group doing both (one wave per SIMD) took 2.6 times as long
+// (32768 tokens in 6 documents, 8/1 heads of 128), and 2.2 times (8192 tokens in 23,
+// 32/8 heads).
 //
 // Tiles of 32 queries, from the block's own first row to the document's end, of
-// each head in turn, stream through a ring of four stages.
+// each head in turn, stream through a ring of four stages.  Heads of 64 take 128
+// registers and 65 KB: two workgroups per CU (103 -> 90 us for 16384 tokens in 160
+// documents, 16/4 heads).
+//
+// Bound by the chain of a tile (scores, exponentials, handover, products; 1.0 to 1.3 us)
+// and on long documents by the clock: 32768 tokens in 6, 8/1 heads of 128, 1305 us
+// (1.0 PFLOP/s, matrix cores busy 49% at 1.83 GHz); 8192 in 23, 32/8 heads, 152 us.
 template <int D>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) attn_packed_dkdv_kernel(PackedAttn p) {
   constexpr int TB = QT * D * 2;
@@ -663,6 +683,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
 
 // dK, dV = the sum of the slices' fp32 parts in order, for the blocks that were cut:
 // a workgroup per block, kv head and quarter of its rows, eight columns per thread.
+// Four slices of 32768 rows and one head of 128: 28 us for 151 MB.
 template <int D>
 __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
   const int hk = static_cast<int>(blockIdx.y), lane = static_cast<int>(threadIdx.x) & 63, at = static_cast<int>(blockIdx.x) / 4;

