@@ -90,6 +90,22 @@ def test_more_documents_than_a_wave_probes_at_once():
     compare(run(q, k, v, do, packing(starts, n)), q, k, v, do, starts)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_blocks_cut_among_many_short_ones(d):
+    """Enough blocks that only those of the long document are cut; four of the 32 kv heads are compared."""
+    starts, a, g = starts_of([40, 1600, 3, 0, 300] + [1] * 9 + [100], 10), 64, 32
+    n = starts[-1] + 47
+    q, k, v, do = (t.cuda() for t in draw(n, a, g, d, 31))
+    out = run(q, k, v, do, packing(starts, n), fill=7.0)
+    again = run(q, k, v, do, packing(starts, n), fill=7.0)
+    for t in out:
+        assert torch.equal(out[t], again[t]), t       # whatever the order of the blocks
+    for h in (0, 1, 17, 31):
+        hq, hk = slice(2 * h, 2 * h + 2), slice(h, h + 1)
+        part = {t: x[hq] if t == "lse" else x[:, hk if t in ("dk", "dv") else hq] for t, x in out.items()}
+        compare(part, q[:, hq], k[:, hk], v[:, hk], do[:, hq], starts, fill=7.0)
+
+
 @pytest.mark.parametrize("scale,spread", [(0.5, 4.0), (1e-3, 1.0), (1.0, 30.0)])
 def test_scales_and_large_scores(scale, spread):
     starts = starts_of([90, 210])
