@@ -253,21 +253,24 @@ __device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
 constexpr int kOrderBins = 512;
 __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n_slots = p.pk.tokens / 128 + p.pk.n_seqs, room = p.pk.tokens + packed_windows(p);
+  const int room = p.pk.tokens + packed_windows(p);
   const int group = p.heads / p.kv_heads;
   int2* items = reinterpret_cast<int2*>(p.items) + 1;
   for (int i = tid; i < kOrderBins; i += 256) bin[i] = 0;
   __syncthreads();
+  // a document per thread: a document of n blocks takes the pass n^2 tiles, this loop n steps
   const auto each = [&](auto visit) __attribute__((always_inline)) {
-    for (int s0 = wave * 64; s0 < n_slots; s0 += 256) {
-      const SeqBlock b = seq_blocks(p.pk, s0, 128, lane);
-      if (s0 + lane >= n_slots || b.row0 >= b.hi) continue;
-      const int n_rows = b.hi - b.row0, slices = packed_slices(p, n_rows);
-      const float work = static_cast<float>((n_rows + QT - 1) / QT) * (group / slices);
-      visit(b, static_cast<int>(__float_as_uint(work) >> 19) - (127 << 4), p.work_cap ? slices : 1);
+    int left = room;                     // no more blocks than that, whatever starts holds
+    for (int i = tid; i < p.pk.n_seqs; i += 256) {
+      const int hi = seq_start(p.pk, i + 1);
+      for (int row0 = seq_start(p.pk, i); row0 < hi && left > 0; row0 += 128, --left) {
+        const int n_rows = hi - row0, slices = packed_slices(p, n_rows);
+        const float work = static_cast<float>((n_rows + QT - 1) / QT) * (group / slices);
+        visit(row0, hi, static_cast<int>(__float_as_uint(work) >> 19) - (127 << 4), p.work_cap ? slices : 1);
+      }
     }
   };
-  each([&](const SeqBlock&, int k, int n) { atomicAdd(&bin[k], n); });
+  each([&](int, int, int k, int n) { atomicAdd(&bin[k], n); });
   __syncthreads();
   if (wave == 0) {                       // entries in fuller bins, for every bin
     constexpr int M = kOrderBins / 64;
@@ -291,9 +294,9 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
     }
   }
   __syncthreads();
-  each([&](const SeqBlock& b, int k, int n) {
+  each([&](int row0, int hi, int k, int n) {
     const int at = atomicAdd(&bin[k], n);
-    for (int j = 0; j < n && at + j < room; ++j) items[at + j] = make_int2(b.row0 | (j ? INT32_MIN : 0), b.hi);
+    for (int j = 0; j < n && at + j < room; ++j) items[at + j] = make_int2(row0 | (j ? INT32_MIN : 0), hi);
   });
 }
 

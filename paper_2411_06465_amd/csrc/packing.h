@@ -71,22 +71,6 @@ __device__ __forceinline__ SeqBlock seq_block(const Packing& p, int slot, int ro
   return SeqBlock{s.lo, s.hi, s.lo + t * rows};
 }
 
-// The blocks in slots slot0 .. slot0 + 63, one per lane: they belong to the 64
-// documents from the last one that starts at or below slot0 on, as every document's
-// first slot is a new one.
-__device__ __forceinline__ SeqBlock seq_blocks(const Packing& p, int slot0, int rows, int lane) {
-  const int i0 = max(last_seq(p, slot0, lane, [rows](int v, int j) { return v / rows + j; }).i, 0), i = min(i0 + lane, p.n_seqs);
-  const int lo = seq_start(p, i), hi = seq_start(p, min(i + 1, p.n_seqs)), slot = slot0 + lane;
-  const int first = i < p.n_seqs ? lo / rows + i : INT32_MAX;
-  int c = 0;
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2)
-    if (__shfl(first, c + d, 64) <= slot) c += d;
-  const int t = slot - __shfl(first, c, 64), my_lo = __shfl(lo, c, 64), my_hi = max(my_lo, __shfl(hi, c, 64));
-  if (t < 0 || t >= (my_hi - my_lo + rows - 1) / rows) return SeqBlock{0, 0, 0};
-  return SeqBlock{my_lo, my_hi, my_lo + t * rows};
-}
-
 // The block of 128 rows that holds `row`.
 __device__ __forceinline__ SeqBlock block_at(const Packing& p, int row, int lane) {
   const SeqRows s = seq_of_row(p, row, lane);
