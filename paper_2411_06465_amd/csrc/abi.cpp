@@ -866,6 +866,7 @@ int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, co
     const uint64_t ny = tokens ? ((uint64_t)(tokens - 1) * t->y_ld + cols) * size : 0;
     if (!(x == y && t->x_ld == t->y_ld) && x < y + ny && y < x + nx)
       return fail(L4D_EINVAL, "rope: input and output overlap");
+    if (a.n_tensors && a.t[0].y == t->y) return fail(L4D_EINVAL, "rope: q and k have the same output");
     a.t[a.n_tensors++] = RopeHeads{t->x, t->y, t->x_ld, t->y_ld, (int32_t)t->heads};
   }
   if (tokens == 0 || (pk && pk->n_seqs == 0)) return L4D_OK;

@@ -51,6 +51,10 @@ def test_rope_refuses_parameters(bad):
     assert rope_rc(**bad) == L.L4D_EINVAL and "rope" in message()
 
 
+def test_rope_refuses_one_output_for_both():
+    assert rope_rc(q=heads(), k=heads()) == L.L4D_EINVAL and "same output" in message()
+
+
 def test_rope_refuses_arguments():
     r = L.make_rope(64)
     r.layout = 2
