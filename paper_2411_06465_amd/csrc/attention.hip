@@ -1134,6 +1134,8 @@ hipError_t attn_bwd(const AttnParams& p, int part, hipStream_t stream) {
 //    CU, or four where documents are long (the sums grow with the rows, the work with
 //    the pairs).  32768 tokens in 6 documents, 8/1 heads of 128, forward and backward
 //    in 1, 2, 4 slices: 4.82, 3.38, 2.98 ms.
+//    Many short documents make more blocks than rows suggest (16384 tokens in 450, 8/1
+//    heads of 64: backward 71 us in two slices, 59 uncut).
 //  * Else only the blocks with more query tiles than 64 and than a CU would get if
 //    all documents were equally long, by 2.  8192 tokens in 23 documents, 32/8
 //    heads of 128: none cut 361 us, these 351; 16384 tokens in 160, 16/4 heads of 64:
@@ -1147,7 +1149,7 @@ static int splits_of_all(int64_t base, int64_t want, int most) {
 }
 void attn_packed_plan(PackedAttn* p) {
   const int64_t tokens = p->pk.tokens, n_seqs = std::max(p->pk.n_seqs, 1), group = p->heads / p->kv_heads;
-  const int64_t base = (tokens + 127) / 128 * p->kv_heads;
+  const int64_t base = std::min(tokens / 128 + n_seqs, tokens) * p->kv_heads;      // at most that many blocks
   p->work_cap = 0;
   if (base < 512) {
     p->n_split = splits_of_all(base, tokens >= 2048 * n_seqs ? 1024 : 512, packed_hpb(p->heads, p->kv_heads));
