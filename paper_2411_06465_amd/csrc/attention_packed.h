@@ -55,6 +55,15 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float mu
   }
 }
 
+// The query blocks of the forward and of dQ, the i-th to start: those with most keys
+// first, where one load shows all documents (32768 tokens in 6 documents, 8/1 heads of 128:
+// forward 653 -> 625 us, dQ 933 -> 886; 8192 tokens in 23, 32/8 heads: forward 85 -> 81, dQ
+// as it was), else the documents one after another, last blocks first.
+__device__ __forceinline__ SeqBlock query_block(const PackedAttn& p, int i, int rows, int lane) {
+  return p.pk.n_seqs > 1 && p.pk.n_seqs < 64 ? ranked_block(p.pk, i, rows, lane)
+                                             : seq_block(p.pk, p.n_slots - 1 - i, rows, lane);
+}
+
 // ------------------------------------------------------------------ forward
 // One workgroup per block of query rows and hpb query heads of one kv head: 4
 // waves x 32 rows, wave w on head w % hpb.  Each lane holds one query's scores
@@ -68,9 +77,9 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float mu
 // where some row's maximum grew (a wave-wide vote).
 //
 // Long documents are bound by exponentials and other vector work beside the products,
-// at a power-limited clock: 32768 tokens in 6, 8/1 heads of 128, 670 us, 1.0 PFLOP/s,
+// at a power-limited clock: 32768 tokens in 6, 8/1 heads of 128, 625 us, 1.1 PFLOP/s,
 // matrix cores busy 51% at 1.76 GHz.  Short ones by the way to the first products, about
-// 4 us of a workgroup's 6 to 20: 8192 tokens in 23, 32/8 heads of 128, 85 us.
+// 4 us of a workgroup's 6 to 20: 8192 tokens in 23, 32/8 heads of 128, 81 us.
 template <int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_fwd_kernel(PackedAttn p) {
   constexpr int TB = KT * D * 2;
@@ -78,8 +87,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_hg = p.heads / p.hpb, rows = 128 / p.hpb;
-  const int slot = p.n_slots - 1 - static_cast<int>(blockIdx.x) / n_hg, h0 = static_cast<int>(blockIdx.x) % n_hg * p.hpb;
-  const SeqBlock blk = seq_block(p.pk, slot, rows, lane);
+  const int id = static_cast<int>(blockIdx.x), h0 = id % n_hg * p.hpb;
+  const SeqBlock blk = query_block(p, id / n_hg, rows, lane);
   if (blk.row0 >= blk.hi) return;
   const int hq = h0 + wave % p.hpb, hk = h0 / (p.heads / p.kv_heads);
   const int wave_q0 = blk.row0 + wave / p.hpb * 32;
@@ -311,7 +320,7 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
 // The dQ of later rows uses the uncorrected delta; where the error counts, a
 // probability is large and dS enters the product in two parts (kLargeP).
 //
-// Bound as the forward is: 32768 tokens in 6 documents, 8/1 heads of 128, 965 us (1.0
+// Bound as the forward is: 32768 tokens in 6 documents, 8/1 heads of 128, 886 us (1.1
 // PFLOP/s, busy 52% at 1.86 GHz); 8192 in 23, 32/8 heads, 120 us; 16384 in 160, 16/4
 // heads of 64, 43 us (48 with two workgroups per CU, here three).
 template <int D>
@@ -323,8 +332,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_hg = p.heads / p.hpb, rows = 128 / p.hpb;
   if (blockIdx.x == 0) return packed_order(p, reinterpret_cast<int*>(kbuf));
-  const int id = static_cast<int>(blockIdx.x) - 1, slot = p.n_slots - 1 - id / n_hg, h0 = id % n_hg * p.hpb;
-  const SeqBlock blk = seq_block(p.pk, slot, rows, lane);
+  const int id = static_cast<int>(blockIdx.x) - 1, h0 = id % n_hg * p.hpb;
+  const SeqBlock blk = query_block(p, id / n_hg, rows, lane);
   if (blk.row0 >= blk.hi) return;
   const int hq = h0 + wave % p.hpb, hk = h0 / (p.heads / p.kv_heads);
   const int wave_q0 = blk.row0 + wave / p.hpb * 32;

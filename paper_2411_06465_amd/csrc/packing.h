@@ -71,6 +71,32 @@ __device__ __forceinline__ SeqBlock seq_block(const Packing& p, int slot, int ro
   return SeqBlock{s.lo, s.hi, s.lo + t * rows};
 }
 
+__device__ __forceinline__ int wave_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return __builtin_amdgcn_readlane(x, 63);
+}
+// The block of rank `rank` when the blocks of up to 63 documents stand by their place in
+// the document, the last places first.  sum_i max(n_i - t, 0) of them, n_i the blocks of
+// document i, stand at place t or behind it: a search over t.
+__device__ __forceinline__ SeqBlock ranked_block(const Packing& p, int rank, int rows, int lane) {
+  const int v = seq_start(p, min(lane, p.n_seqs)), next = __shfl_down(v, 1, 64);
+  const int n = lane < p.n_seqs ? (max(next - v, 0) + rows - 1) / rows : 0;
+  if (wave_sum(n) <= rank) return SeqBlock{0, 0, 0};
+  int t = 0;
+  for (int step = 1 << (31 - __builtin_clz(p.tokens / rows + 1)); step > 0; step /= 2)
+    if (wave_sum(max(n - t - step, 0)) > rank) t += step;
+  const uint64_t at = __builtin_amdgcn_ballot_w64(n > t);
+  const int before = __builtin_popcountll(at & ((uint64_t{1} << lane) - 1)), k = rank - wave_sum(max(n - t - 1, 0));
+  const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > t && before == k) | uint64_t{1} << 62);
+  const int lo = __builtin_amdgcn_readlane(v, i), hi = __builtin_amdgcn_readlane(v, i + 1);
+  return SeqBlock{lo, max(lo, hi), lo + t * rows};
+}
+
 // The block of 128 rows that holds `row`.
 __device__ __forceinline__ SeqBlock block_at(const Packing& p, int row, int lane) {
   const SeqRows s = seq_of_row(p, row, lane);

@@ -106,6 +106,16 @@ def test_long_blocks_cut_among_many_short_ones(d):
         compare(part, q[:, hq], k[:, hk], v[:, hk], do[:, hq], starts, fill=7.0)
 
 
+@pytest.mark.parametrize("docs", [2, 62, 63, 64, 65])
+def test_documents_around_a_wave(docs):
+    lens = [(i * 37) % 71 for i in range(docs)]
+    lens[docs // 2] = 333
+    starts = starts_of(lens, 3)
+    n = starts[-1] + 2
+    q, k, v, do = (t.cuda() for t in draw(n, 4, 2, 64, docs))
+    compare(run(q, k, v, do, packing(starts, n), fill=7.0), q, k, v, do, starts, fill=7.0)
+
+
 @pytest.mark.parametrize("scale,spread", [(0.5, 4.0), (1e-3, 1.0), (1.0, 30.0)])
 def test_scales_and_large_scores(scale, spread):
     starts = starts_of([90, 210])
