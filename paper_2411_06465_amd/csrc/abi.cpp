@@ -1786,6 +1786,7 @@ extern "C" int lm_loss_bwd(int64_t n, int64_t h, int64_t v_t, int64_t v0, const 
   int rc = loss_check(n, h, v_t, v0, {hidden, w_lm, d_hidden}, {lse, d_w}, targets);
   if (rc) return rc;
   if (!std::isfinite(grad_scale)) return fail(L4D_EINVAL, "grad_scale must be finite");
+  if (d_hidden == hidden || d_hidden == w_lm) return fail(L4D_EINVAL, "d_hidden is an input's array");
   if (!A) return fail(L4D_EINVAL, "arena is required");
   if (n == 0) return L4D_OK;
   const LossWs plan = plan_loss(n, h, v_t);

@@ -181,6 +181,14 @@ def test_loss_refuses(backward):
     L.lib().l4d_arena_destroy(ar)
 
 
+def test_loss_gradient_is_no_input():
+    ar = C.c_void_p()
+    assert L.lib().l4d_arena_create(C.c_void_p(BASE), 256, C.byref(ar)) == L.L4D_OK
+    for i in (0, 1):
+        assert loss_rc(True, arena=ar, over={4: at(i)}) == L.L4D_EINVAL and "d_hidden" in message()
+    L.lib().l4d_arena_destroy(ar)
+
+
 def test_loss_workspace_does_not_grow_with_the_logits():
     n, v = 65536, 128256
     f, b = L.l4d_lm_loss_workspace_bytes(n, 4096, v)
