@@ -252,14 +252,15 @@ __device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
 
 // Workgroup 0 of the dQ pass lists the blocks of keys for the dK/dV pass, longest
 // first, as {first row, sign bit: second slice; end of the document} behind their
-// number: a counting sort by work in steps of 1/16 octave.  Workgroups start in order
+// number: a counting sort by work in steps of 1/64 octave.  Workgroups start in order
 // and last as long as their document has rows left; in the order of the rows, long ones
 // started last, and short ones waited behind parts of the chip that held long ones
 // (8192 tokens in 23 documents, 32/8 heads of 128: 157 of 256 CUs busy on average).  dK/dV
 // 187 -> 152 us there, 1378 -> 1305 for 32768 tokens in 6, 8/1 heads, 90 -> 59 for 16384
 // in 160, 16/4 heads of 64.  The list hides behind the other workgroups' dQ.  Its order
-// within a step varies, the sums do not.
-constexpr int kOrderBins = 512;
+// within a step varies, the sums do not; steps of 1/16 scatter a document's neighbours,
+// which read the same rows (1305 -> 1280 us on the long documents).
+constexpr int kOrderBins = 2048;
 __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int room = p.pk.tokens + packed_windows(p);
@@ -275,7 +276,7 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
       for (int row0 = seq_start(p.pk, i); row0 < hi && left > 0; row0 += 128, --left) {
         const int n_rows = hi - row0, slices = packed_slices(p, n_rows);
         const float work = static_cast<float>((n_rows + QT - 1) / QT) * (group / slices);
-        visit(row0, hi, static_cast<int>(__float_as_uint(work) >> 19) - (127 << 4), p.work_cap ? slices : 1);
+        visit(row0, hi, static_cast<int>(__float_as_uint(work) >> 17) - (127 << 6), p.work_cap ? slices : 1);
       }
     }
   };
@@ -331,6 +332,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_hg = p.heads / p.hpb, rows = 128 / p.hpb;
+  static_assert(sizeof(kbuf) >= kOrderBins * sizeof(int), "the bins lie in the K tiles");
   if (blockIdx.x == 0) return packed_order(p, reinterpret_cast<int*>(kbuf));
   const int id = static_cast<int>(blockIdx.x) - 1, h0 = id % n_hg * p.hpb;
   const SeqBlock blk = query_block(p, id / n_hg, rows, lane);
@@ -458,7 +460,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 // documents, 16/4 heads).
 //
 // Bound by the chain of a tile (scores, exponentials, handover, products; 1.0 to 1.3 us)
-// and on long documents by the clock: 32768 tokens in 6, 8/1 heads of 128, 1305 us
+// and on long documents by the clock: 32768 tokens in 6, 8/1 heads of 128, 1280 us
 // (1.0 PFLOP/s, matrix cores busy 49% at 1.83 GHz); 8192 in 23, 32/8 heads, 152 us.
 template <int D>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) attn_packed_dkdv_kernel(PackedAttn p) {
