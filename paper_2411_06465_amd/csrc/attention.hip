@@ -1136,8 +1136,10 @@ hipError_t attn_bwd(const AttnParams& p, int part, hipStream_t stream) {
 //    in 1, 2, 4 slices: 4.82, 3.38, 2.98 ms.
 //    Many short documents make more blocks than rows suggest (16384 tokens in 450, 8/1
 //    heads of 64: backward 71 us in two slices, 59 uncut).
-//  * Else only the blocks with more query tiles than 64 and than a CU would get if
-//    all documents were equally long, by 2.  8192 tokens in 23 documents, 32/8
+//  * Else only the blocks with more tiles (of 32 queries and one query head) than 64 and
+//    than a CU would get if all documents were equally long, by 2, and never one of
+//    fewer than 128 rows (packed_windows; from 17 query heads per kv head on, four query
+//    tiles are more than 64).  8192 tokens in 23 documents, 32/8
 //    heads of 128: none cut 361 us, these 351; 16384 tokens in 160, 16/4 heads of 64:
 //    172 and 138.  Limits of 1, 2.25, 4 times the even share, backward: 6 documents of
 //    8192 tokens, 32/8 heads of 128, 588, 606, 625 us; 23: 313, 301, 320; 200 of
@@ -1150,14 +1152,19 @@ static int splits_of_all(int64_t base, int64_t want, int most) {
 void attn_packed_plan(PackedAttn* p) {
   const int64_t tokens = p->pk.tokens, n_seqs = std::max(p->pk.n_seqs, 1), group = p->heads / p->kv_heads;
   const int64_t base = std::min(tokens / 128 + n_seqs, tokens) * p->kv_heads;      // at most that many blocks
-  p->work_cap = 0;
+  p->cut_rows = 0;
   if (base < 512) {
     p->n_split = splits_of_all(base, tokens >= 2048 * n_seqs ? 1024 : 512, packed_hpb(p->heads, p->kv_heads));
     return;
   }
   const double even = static_cast<double>(tokens) * tokens / n_seqs * p->heads / (2.0 * 128 * QT) / 256;
-  p->work_cap = static_cast<int32_t>(std::min(std::max(64.0, even), 1e9));
-  p->n_split = group % 2 == 0 && (tokens + QT - 1) / QT * group > p->work_cap ? 2 : 1;
+  const int64_t most = static_cast<int64_t>(std::min(std::max(64.0, even), 1e9)) / group;      // query tiles that stay whole
+  p->cut_rows = static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(most * QT + 1, 128), INT32_MAX));
+  p->n_split = group % 2 == 0 && tokens >= p->cut_rows ? 2 : 1;
+}
+int64_t attn_packed_places(const PackedAttn& p) {
+  const int64_t most = std::min<int64_t>(packed_slots(p, 128), p.pk.tokens);     // blocks with a row
+  return p.cut_rows ? most + (p.n_split - 1) * packed_windows(p) : most * p.n_split;
 }
 int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads) {
   const int64_t base = (tokens + 127) / 128 * kv_heads;

@@ -240,14 +240,15 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 }
 
 // ------------------------------------------------------------------ backward: order of the blocks of keys
-// Windows of 128 rows from row 0 on.
+// Windows of 128 rows from row 0 on.  Where only some blocks are cut, a cut one has 128
+// rows, so it holds the first row of exactly one window: no more second slices than
+// windows are listed, and the pass that adds them up finds every cut block from its window.
 __host__ __device__ __forceinline__ int packed_windows(const PackedAttn& p) { return (p.pk.tokens + 127) / 128; }
 
 // Slices of a kv head's query heads that the keys of a block get whose document goes
 // on for n_rows rows from the block's first one: see attn_packed_plan.
 __device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
-  if (p.work_cap == 0) return p.n_split;
-  return (n_rows + QT - 1) / QT * (p.heads / p.kv_heads) > p.work_cap ? p.n_split : 1;
+  return n_rows >= p.cut_rows ? p.n_split : 1;
 }
 
 // Workgroup 0 of the dQ pass lists the blocks of keys for the dK/dV pass, longest
@@ -276,7 +277,7 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
       for (int row0 = seq_start(p.pk, i); row0 < hi && left > 0; row0 += 128, --left) {
         const int n_rows = hi - row0, slices = packed_slices(p, n_rows);
         const float work = static_cast<float>((n_rows + QT - 1) / QT) * (group / slices);
-        visit(row0, hi, static_cast<int>(__float_as_uint(work) >> 17) - (127 << 6), p.work_cap ? slices : 1);
+        visit(row0, hi, static_cast<int>(__float_as_uint(work) >> 17) - (127 << 6), p.cut_rows ? slices : 1);
       }
     }
   };
@@ -475,11 +476,11 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
   // Workgroups go to the 8 XCDs in turn: the kv heads of a block are neighbours, and the
   // slices where all blocks are cut, so that an XCD keeps to the same heads, whose
   // rows it then has in its L2.
-  const int id = static_cast<int>(blockIdx.x), cut = p.work_cap ? 1 : p.n_split, at = id / (p.kv_heads * cut);
+  const int id = static_cast<int>(blockIdx.x), cut = p.cut_rows ? 1 : p.n_split, at = id / (p.kv_heads * cut);
   const int n_items = p.items[0];
   const int2 item = reinterpret_cast<const int2*>(p.items)[1 + at];
   if (at >= n_items) return;
-  const int hk = id % (p.kv_heads * cut) / cut, split = p.work_cap ? item.x < 0 : id % cut;
+  const int hk = id % (p.kv_heads * cut) / cut, split = p.cut_rows ? item.x < 0 : id % cut;
   const struct { int row0, hi; } blk{item.x & INT32_MAX, item.y};
   const int n_rows = blk.hi - blk.row0, n_qt = (n_rows + QT - 1) / QT;
   const int slices = packed_slices(p, n_rows);
@@ -701,7 +702,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
 template <int D>
 __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
   const int hk = static_cast<int>(blockIdx.y), lane = static_cast<int>(threadIdx.x) & 63, at = static_cast<int>(blockIdx.x) / 4;
-  const SeqBlock blk = p.work_cap ? block_at(p.pk, at * 128, lane) : seq_block(p.pk, at, 128, lane);
+  const SeqBlock blk = p.cut_rows ? block_at(p.pk, at * 128, lane) : seq_block(p.pk, at, 128, lane);
   if (blk.row0 >= blk.hi) return;
   const int n_rows = blk.hi - blk.row0, slices = packed_slices(p, n_rows);
   if (slices == 1) return;
@@ -755,12 +756,11 @@ hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
     if (part == 0) hipLaunchKernelGGL(attn_packed_fwd_kernel<D>, grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL(attn_packed_dq_kernel<D>, grid, dim3(256), 0, stream, p);
   } else if (part == 1) {
-    const int64_t most = std::min<int64_t>(packed_slots(p, 128), p.pk.tokens);     // blocks with a row
-    const unsigned blocks = static_cast<unsigned>(p.work_cap ? most + (p.n_split - 1) * packed_windows(p) : most * p.n_split);
-    hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, dim3(blocks * p.kv_heads), dim3(512), 0, stream, p);
+    const unsigned blocks = static_cast<unsigned>(attn_packed_places(p)) * p.kv_heads;
+    hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, dim3(blocks), dim3(512), 0, stream, p);
   } else {
     if (p.n_split == 1) return hipSuccess;
-    const dim3 grid(static_cast<unsigned>(p.work_cap ? packed_windows(p) : packed_slots(p, 128)) * 4, p.kv_heads);
+    const dim3 grid(static_cast<unsigned>(p.cut_rows ? packed_windows(p) : packed_slots(p, 128)) * 4, p.kv_heads);
     hipLaunchKernelGGL(attn_packed_reduce_kernel<D>, grid, dim3(256), 0, stream, p);
   }
   return hipGetLastError();

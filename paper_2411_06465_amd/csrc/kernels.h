@@ -268,14 +268,16 @@ struct PackedAttn {
   int64_t dq_ld, dk_ld, dv_ld;
   float *delta, *lse2;      // [heads][tokens], written by the dQ pass: rowsum(dO * O), lse in base 2
   // dK/dV, set by attn_packed_plan: the query heads of a kv head go in n_split slices, for
-  // all blocks (work_cap 0) or those with more than work_cap query tiles
-  int32_t n_split, work_cap;
+  // all blocks of keys (cut_rows 0), or in two for those with at least cut_rows rows left of
+  // their document.  cut_rows is 0 or at least 128: see packed_windows.
+  int32_t n_split, cut_rows;
   int32_t* items;           // attn_packed_items(pk.tokens) x 8 bytes, written by the dQ pass: its blocks of keys in order
   float* dkv_partial;       // n_split > 1: dK [n_split][tokens][kv_heads][d_h], then dV
 };
 void attn_packed_plan(PackedAttn* p);                                      // from pk, heads and kv_heads
 int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads);   // over every packing of the tokens
 bool attn_packed_fits(const PackedAttn& p);      // every launch within the grid limits
+int64_t attn_packed_places(const PackedAttn& p); // workgroups per kv head of the dK/dV pass: at least as many as its list is long
 hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream);
 inline int64_t attn_packed_items(int64_t tokens) { return tokens ? 1 + tokens + (tokens + 127) / 128 : 0; }
 // part 2: dQ and delta; 1: dK, dV (after part 2); 3: the sum of the slices (n_split > 1).
