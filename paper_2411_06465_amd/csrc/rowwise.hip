@@ -763,7 +763,9 @@ __global__ void __launch_bounds__(kJoinWaves * 64) loss_join_kernel(LossJoin p) 
   float lse = m + logf(s), z = here ? p.zt[row] : -INFINITY;
   if (p.target_logit) p.target_logit[row] = z;
   if (p.peer_lse) {
-    const float q = p.peer_lse[row], big = fmaxf(lse, q), small = fminf(lse, q);
+    const float q = p.peer_lse[row];
+    const bool up = lse > q;             // not fmaxf and fminf, which would drop a NaN of either side
+    const float big = up ? lse : q, small = up ? q : lse;
     lse = big + log1pf(expf(small - big));
     if (!here) z = p.peer_z[row];
   }
