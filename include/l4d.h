@@ -392,7 +392,9 @@ typedef struct {
  *   NULL).  Row i starts at x + i x_ld, heads are contiguous within a row, so the
  *   columns of a fused [tokens][(a_t + 2 k_t) d_h] array are addressed in place.
  *   y == x with y_ld == x_ld rotates in place; other overlaps of a tensor's input
- *   and output ranges are refused, and so are two outputs that start at one address.
+ *   and output ranges are refused, and so is an output that shares an element with the
+ *   other tensor's input or output (tensors with one stride may interleave as columns of
+ *   one array; with different strides their ranges must not meet).
  * L4D_EINVAL: more than 2^25 tokens or 8192 heads, head_dim outside 2 .. 512, rot_dim odd or outside 2 .. head_dim, an
  * unknown enum value, base <= 1, factor <= 0, amplitude <= 0, original <= 0 or not
  * 0 < low < high where the scaling uses them, ld < heads head_dim, NULL or

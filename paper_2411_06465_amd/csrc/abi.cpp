@@ -840,6 +840,21 @@ int rope_turns(const l4d_rope* r, double* turns) {
   return L4D_OK;
 }
 
+// The rows that a tensor of a call occupies, in bytes: n rows of `width` bytes, `ld` apart.
+struct RowRange {
+  uintptr_t p;
+  uint64_t width, ld, n;
+  uint64_t span() const { return n ? (n - 1) * ld + width : 0; }
+};
+// Whether two tensors of n rows share a byte.  With equal strides rows may interleave
+// (columns of one fused array); with different ones ranges that meet count as shared.
+bool rows_meet(const RowRange& a, const RowRange& b) {
+  if (a.p >= b.p + b.span() || b.p >= a.p + a.span()) return false;
+  if (a.ld != b.ld) return true;
+  const uint64_t off = b.p >= a.p ? (b.p - a.p) % a.ld : (a.ld - (a.p - b.p) % a.ld) % a.ld;   // b's column in a's rows
+  return off < a.width || off + b.width > a.ld;
+}
+
 int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk,
               const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, int inverse, void* stream_ptr) {
   if (!r || !q) return fail(L4D_EINVAL, "rope and q are required");
@@ -853,6 +868,7 @@ int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, co
   if ((rc = rope_turns(r, a.turns))) return rc;
   const int64_t size = dtype == L4D_F32 ? 4 : 2;
   const l4d_rope_heads* in[2] = {q, k};
+  RowRange from[2], to[2];
   for (const l4d_rope_heads* t : in) {
     if (!t) continue;
     if (!t->x || !t->y) return fail(L4D_EINVAL, "rope: a tensor is NULL");
@@ -862,11 +878,15 @@ int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, co
       return fail(L4D_EINVAL, "rope: a row stride is shorter than the heads, or above 2^31");
     const uintptr_t x = reinterpret_cast<uintptr_t>(t->x), y = reinterpret_cast<uintptr_t>(t->y);
     if (x % size || y % size) return fail(L4D_EINVAL, "rope: a tensor is misaligned");
-    const uint64_t nx = tokens ? ((uint64_t)(tokens - 1) * t->x_ld + cols) * size : 0;
-    const uint64_t ny = tokens ? ((uint64_t)(tokens - 1) * t->y_ld + cols) * size : 0;
-    if (!(x == y && t->x_ld == t->y_ld) && x < y + ny && y < x + nx)
+    const RowRange rx{x, (uint64_t)(cols * size), (uint64_t)(t->x_ld * size), (uint64_t)tokens};
+    const RowRange ry{y, (uint64_t)(cols * size), (uint64_t)(t->y_ld * size), (uint64_t)tokens};
+    if (!(x == y && t->x_ld == t->y_ld) && x < y + ry.span() && y < x + rx.span())
       return fail(L4D_EINVAL, "rope: input and output overlap");
     if (a.n_tensors && a.t[0].y == t->y) return fail(L4D_EINVAL, "rope: q and k have the same output");
+    // one launch turns both: what it writes of one tensor must be nothing it reads or writes of the other
+    if (a.n_tensors && (rows_meet(ry, from[0]) || rows_meet(to[0], rx) || rows_meet(to[0], ry)))
+      return fail(L4D_EINVAL, "rope: an output of q or k overlaps the other tensor");
+    from[a.n_tensors] = rx, to[a.n_tensors] = ry;
     a.t[a.n_tensors++] = RopeHeads{t->x, t->y, t->x_ld, t->y_ld, (int32_t)t->heads};
   }
   if (tokens == 0 || (pk && pk->n_seqs == 0)) return L4D_OK;
