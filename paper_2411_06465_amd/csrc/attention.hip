@@ -1153,6 +1153,9 @@ void attn_packed_plan(PackedAttn* p) {
   const int64_t tokens = p->pk.tokens, n_seqs = std::max(p->pk.n_seqs, 1), group = p->heads / p->kv_heads;
   const int64_t base = std::min(tokens / 128 + n_seqs, tokens) * p->kv_heads;      // at most that many blocks
   p->cut_rows = 0;
+  // The documents of one of the 256 threads have at most that many blocks.  Starts that are
+  // not in order may make more: the list's counts then still stay below 2^31.
+  p->list_steps = static_cast<int32_t>(tokens / 128 + p->pk.n_seqs / 256 + 1);
   if (base < 512) {
     p->n_split = splits_of_all(base, tokens >= 2048 * n_seqs ? 1024 : 512, packed_hpb(p->heads, p->kv_heads));
     return;

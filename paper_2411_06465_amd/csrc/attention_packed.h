@@ -271,7 +271,7 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
   __syncthreads();
   // a document per thread: a document of n blocks takes the pass n^2 tiles, this loop n steps
   const auto each = [&](auto visit) __attribute__((always_inline)) {
-    int left = room;                     // no more blocks than that, whatever starts holds
+    int left = p.list_steps;             // no more blocks than that, whatever starts holds
     for (int i = tid; i < p.pk.n_seqs; i += 256) {
       const int hi = seq_start(p.pk, i + 1);
       for (int row0 = seq_start(p.pk, i); row0 < hi && left > 0; row0 += 128, --left) {

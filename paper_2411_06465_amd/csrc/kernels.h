@@ -271,6 +271,7 @@ struct PackedAttn {
   // all blocks of keys (cut_rows 0), or in two for those with at least cut_rows rows left of
   // their document.  cut_rows is 0 or at least 128: see packed_windows.
   int32_t n_split, cut_rows;
+  int32_t list_steps;       // blocks of keys that a thread of the listing workgroup counts at most
   int32_t* items;           // attn_packed_items(pk.tokens) x 8 bytes, written by the dQ pass: its blocks of keys in order
   float* dkv_partial;       // n_split > 1: dK [n_split][tokens][kv_heads][d_h], then dV
 };

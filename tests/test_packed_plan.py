@@ -19,7 +19,8 @@ class PackedAttn(C.Structure):
                [(n, C.c_int32) for n in ("heads", "kv_heads", "d_h", "hpb", "n_slots")] + [("scale", C.c_float)] + \
                [(n, C.c_int64) for n in ("q", "k", "v", "q_ld", "k_ld", "v_ld", "o", "o_ld", "lse", "dout", "do_ld",
                                          "dq", "dk", "dv", "dq_ld", "dk_ld", "dv_ld", "delta", "lse2")] + \
-               [("n_split", C.c_int32), ("cut_rows", C.c_int32), ("items", C.c_int64), ("dkv_partial", C.c_int64)]
+               [("n_split", C.c_int32), ("cut_rows", C.c_int32), ("list_steps", C.c_int32), ("items", C.c_int64),
+                ("dkv_partial", C.c_int64)]
 
 
 def plan(starts, tokens, heads, kv):
@@ -37,6 +38,10 @@ def replay(starts, tokens, heads, kv):
     group = heads // kv
     assert p.n_split >= 1 and group % p.n_split == 0
     blocks = [(row0, hi) for lo, hi in zip(starts[:-1], starts[1:]) for row0 in range(lo, hi, 128)]
+    # the listing workgroup's 256 threads take the documents in turn, and none stops early
+    for thread in range(256):
+        docs = range(thread, len(starts) - 1, 256)
+        assert sum(-(-(starts[i + 1] - starts[i]) // 128) for i in docs) <= p.list_steps
     if p.cut_rows == 0:        # all cut alike: a place per block and slice
         assert len(blocks) * p.n_split <= places
         return 0
@@ -73,3 +78,25 @@ def test_short_documents_of_many_query_heads(lens, heads, kv):
     starts = starts_of(lens)
     cut = replay(starts, starts[-1], heads, kv)
     assert cut == (0 if max(lens) < 128 else len(lens))
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (2, 1), (2, 2), (8, 1), (32, 8)])
+def test_counts_of_the_list_stay_in_32_bits(heads, kv):
+    """Starts out of order (0, tokens, 0, tokens, ..) make every other document hold all rows: the
+    listing workgroup counts list_steps blocks per thread, each in up to two slices, and no sum
+    of them passes 2^31, over all packings that a launch takes."""
+    fits = L.lib()._ZN3l4d16attn_packed_fitsERKNS_10PackedAttnE
+    fits.argtypes, fits.restype = [C.POINTER(PackedAttn)], C.c_bool
+    largest = 0
+    for t in range(31):
+        for s in range(25):
+            for tokens, n_seqs in (((1 << t) - 1, (1 << s) - 1), (1 << t, 1 << s), (3 << t >> 1, 3 << s >> 1)):
+                p = PackedAttn(n_seqs=n_seqs, tokens=tokens, heads=heads, kv_heads=kv, d_h=64)
+                if tokens < 1 or n_seqs < 1 or not fits(C.byref(p)):
+                    continue
+                L.lib()._ZN3l4d16attn_packed_planEPNS_10PackedAttnE(C.byref(p))
+                assert p.list_steps >= 1
+                per_block = p.n_split if p.cut_rows else 1
+                assert 256 * p.list_steps * per_block < 1 << 31, (tokens, n_seqs)
+                largest = max(largest, tokens)
+    assert largest >= 1 << 23
