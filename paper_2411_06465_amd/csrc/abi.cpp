@@ -1240,20 +1240,18 @@ static int layer_backward(const l4d_model* m, const l4d_parallel* p, const l4d_p
       pa.dout = dctx;
       pa.do_ld = nq;
       pa.delta = delta;
-      pa.lse2 = dxn1;                 // written after the attention; has room for a float per row and head
-      pa.items = reinterpret_cast<int32_t*>(rope);   // no table of equal rows here; its 8 (d/2) bytes per row are enough
+      // dxn1 is written after the attention: its 4 d bytes per row and head hold lse2 and, behind it, the list
+      pa.lse2 = dxn1;
+      pa.items = reinterpret_cast<int32_t*>(dxn1 + (x.a_t * x.s + 3) / 4 * 4);
+      pa.rope = rope;                 // dQ and dK are turned back before their one rounding, as in the unpacked layer
       pa.dq = dqkv;
       pa.dk = dqkv + nq;
       pa.dv = dqkv + nq + x.k_t * x.d;
       pa.dq_ld = pa.dk_ld = pa.dv_ld = qc;
       pa.dkv_partial = reinterpret_cast<float*>(wsb + plan.dkv);
       if ((r = launch("clear_outside", s, [&] { return clear_outside(pa.pk, dqkv, qc, qc, s); }))) return r;
+      if ((r = launch("rope_table_packed", s, [&] { return rope_table(lp.rope, rope, s); }))) return r;
       if ((r = packed_attn_backward(pa, s))) return r;
-      RopeRotate back = lp.rope;      // dQ and dK, neighbouring columns, turned back in place
-      back.inverse = 1;
-      back.n_tensors = 1;
-      back.t[0] = RopeHeads{dqkv, dqkv, qc, qc, (int32_t)(x.a_t + x.k_t)};
-      if ((r = launch("rope_bwd", s, [&] { return rope_rotate(back, s); }))) return r;
     } else {
       AttnParams ap = attn_params(x);
       ap.q = sptr(st, L4D_STASH_Q);

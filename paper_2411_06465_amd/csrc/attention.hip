@@ -1182,11 +1182,12 @@ bool attn_packed_fits(const PackedAttn& p) {
 }
 
 hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream) {
-  return p.d_h == 128 ? packed_launch<128>(p, 0, stream) : packed_launch<64>(p, 0, stream);
+  return p.d_h == 128 ? packed_launch<128, false>(p, 0, stream) : packed_launch<64, false>(p, 0, stream);
 }
 
 hipError_t attn_packed_bwd(PackedAttn p, int part, hipStream_t stream) {
-  return p.d_h == 128 ? packed_launch<128>(p, part, stream) : packed_launch<64>(p, part, stream);
+  if (p.rope) return p.d_h == 128 ? packed_launch<128, true>(p, part, stream) : packed_launch<64, true>(p, part, stream);
+  return p.d_h == 128 ? packed_launch<128, false>(p, part, stream) : packed_launch<64, false>(p, part, stream);
 }
 
 }  // namespace l4d

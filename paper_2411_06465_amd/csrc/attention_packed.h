@@ -55,6 +55,22 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], float mu
   }
 }
 
+// Turns a row of D columns that a lane pair holds as in store_rows back by the angles of
+// its row tab of the table (and multiplies by their amplitude), still in fp32: the gradient
+// with respect to a rotated q or k becomes that of the projection's output, and is rounded once.
+template <int D>
+__device__ __forceinline__ void turn_back(f32x16 (&acc)[D / 32], const float2* tab, int lane) {
+#pragma unroll
+  for (int dt = 0; dt < D / 64; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float2 cs = tab[dt * 32 + acc_row(i, lane)];
+      const float a = acc[dt][i], b = acc[dt + D / 64][i];
+      acc[dt][i] = a * cs.x + b * cs.y;
+      acc[dt + D / 64][i] = b * cs.x - a * cs.y;
+    }
+}
+
 // The query blocks of the forward and of dQ, the i-th to start: those with most keys
 // first, where one load shows all documents (32768 tokens in 6 documents, 8/1 heads of 128:
 // forward 653 -> 625 us, dQ 933 -> 886; 8192 tokens in 23, 32/8 heads: forward 85 -> 81, dQ
@@ -325,7 +341,7 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
 // Bound as the forward is: 32768 tokens in 6 documents, 8/1 heads of 128, 886 us (1.1
 // PFLOP/s, busy 52% at 1.86 GHz); 8192 in 23, 32/8 heads, 120 us; 16384 in 160, 16/4
 // heads of 64, 43 us (48 with two workgroups per CU, here three).
-template <int D>
+template <int D, bool ROPE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_dq_kernel(PackedAttn p) {
   constexpr int KQ = 32;                     // keys per tile
   constexpr int TB = KQ * D * 2;
@@ -436,6 +452,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     p.delta[sidx] = my_delta + ds_sum;
     p.lse2[sidx] = my_lse;
   }
+  if constexpr (ROPE) turn_back<D>(dq, p.rope + static_cast<int64_t>(row) * (D / 2), lane);
   ring_barrier();                        // every wave is done with the tiles: each takes a buffer
   store_rows<D>(dq, p.scale, wave < 2 ? kbuf[wave & 1] : vbuf[wave & 1], p.dq + static_cast<int64_t>(wave_q0) * p.dq_ld + hq * D,
                 p.dq_ld, blk.hi - wave_q0, lane);
@@ -463,7 +480,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 // Bound by the chain of a tile (scores, exponentials, handover, products; 1.0 to 1.3 us)
 // and on long documents by the clock: 32768 tokens in 6, 8/1 heads of 128, 1280 us
 // (1.0 PFLOP/s, matrix cores busy 49% at 1.83 GHz); 8192 in 23, 32/8 heads, 152 us.
-template <int D>
+template <int D, bool ROPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) attn_packed_dkdv_kernel(PackedAttn p) {
   constexpr int TB = QT * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t qg[kDkvStages][2][TB];   // per stage: Q tile, then dO tile
@@ -689,6 +706,8 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
             make_float4(acc[dt][4 * jj] * mul, acc[dt][4 * jj + 1] * mul, acc[dt][4 * jj + 2] * mul, acc[dt][4 * jj + 3] * mul);
     return;
   }
+  if constexpr (ROPE)
+    if (role == 1) turn_back<D>(acc, p.rope + static_cast<int64_t>(min(my_key, blk.hi - 1)) * (D / 2), lane);
   ring_barrier();          // every wave is done with the ring, which takes the rows now
   uint16_t* out = reinterpret_cast<uint16_t*>(pick(addr(p.dv), addr(p.dk))) +
                   static_cast<int64_t>(pick(p.dv_ld, p.dk_ld)) * grp_k0 + hk * D;
@@ -699,7 +718,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
 // dK, dV = the sum of the slices' fp32 parts in order, for the blocks that were cut:
 // a workgroup per block, kv head and quarter of its rows, eight columns per thread.
 // Four slices of 32768 rows and one head of 128: 28 us for 151 MB.
-template <int D>
+template <int D, bool ROPE>
 __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
   const int hk = static_cast<int>(blockIdx.y), lane = static_cast<int>(threadIdx.x) & 63, at = static_cast<int>(blockIdx.x) / 4;
   const SeqBlock blk = p.cut_rows ? block_at(p.pk, at * 128, lane) : seq_block(p.pk, at, 128, lane);
@@ -729,6 +748,20 @@ __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
           const float4 x = *reinterpret_cast<const float4*>(src + (which * p.n_split + s) * step + 4 * h);
           v[which][h].x += x.x; v[which][h].y += x.y; v[which][h].z += x.z; v[which][h].w += x.w;
         }
+    if constexpr (ROPE) {      // dK turned back; the lane C/2 further holds the pairs' other elements
+      const bool upper = static_cast<int>(threadIdx.x) % C >= C / 2;
+      const float2* tab = p.rope + row * (D / 2) + static_cast<int>(threadIdx.x) % (C / 2) * 8;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float* x = &v[0][h].x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 cs = tab[4 * h + j];
+          const float other = __shfl_xor(x[j], C / 2, 64);
+          x[j] = x[j] * cs.x + (upper ? -other : other) * cs.y;
+        }
+      }
+    }
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       uint16_t* dst = which ? p.dv + row * p.dv_ld + col : p.dk + row * p.dk_ld + col;
@@ -747,21 +780,21 @@ int packed_hpb(int heads, int kv_heads) {
   return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
 }
 
-template <int D>
+template <int D, bool ROPE>
 hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
   if (part == 0 || part == 2) {
     p.hpb = packed_hpb(p.heads, p.kv_heads);
     p.n_slots = static_cast<int32_t>(packed_slots(p, 128 / p.hpb));
     const dim3 grid(static_cast<unsigned>(p.n_slots) * (p.heads / p.hpb) + (part == 2));    // and the workgroup that lists
     if (part == 0) hipLaunchKernelGGL(attn_packed_fwd_kernel<D>, grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL(attn_packed_dq_kernel<D>, grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((attn_packed_dq_kernel<D, ROPE>), grid, dim3(256), 0, stream, p);
   } else if (part == 1) {
     const unsigned blocks = static_cast<unsigned>(attn_packed_places(p)) * p.kv_heads;
-    hipLaunchKernelGGL(attn_packed_dkdv_kernel<D>, dim3(blocks), dim3(512), 0, stream, p);
+    hipLaunchKernelGGL((attn_packed_dkdv_kernel<D, ROPE>), dim3(blocks), dim3(512), 0, stream, p);
   } else {
     if (p.n_split == 1) return hipSuccess;
     const dim3 grid(static_cast<unsigned>(p.cut_rows ? packed_windows(p) : packed_slots(p, 128)) * 4, p.kv_heads);
-    hipLaunchKernelGGL(attn_packed_reduce_kernel<D>, grid, dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((attn_packed_reduce_kernel<D, ROPE>), grid, dim3(256), 0, stream, p);
   }
   return hipGetLastError();
 }

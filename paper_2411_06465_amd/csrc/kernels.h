@@ -272,6 +272,7 @@ struct PackedAttn {
   // their document.  cut_rows is 0 or at least 128: see packed_windows.
   int32_t n_split, cut_rows;
   int32_t list_steps;       // blocks of keys that a thread of the listing workgroup counts at most
+  const float2* rope;       // null, or rope_table's rows: dq and dk are turned back by them before they are rounded
   int32_t* items;           // attn_packed_items(pk.tokens) x 8 bytes, written by the dQ pass: its blocks of keys in order
   float* dkv_partial;       // n_split > 1: dK [n_split][tokens][kv_heads][d_h], then dV
 };
