@@ -1732,7 +1732,7 @@ LossWs plan_loss(int64_t n, int64_t h, int64_t v_t) {
 // rows: arrays of bf16 rows; words: the others, which need no more than their element's alignment (4 or 8 bytes)
 int loss_check(int64_t n, int64_t h, int64_t v_t, int64_t v0, std::initializer_list<const void*> rows,
                std::initializer_list<const void*> words, const int64_t* targets) {
-  if (n < 0 || h <= 0 || v_t <= 0 || v0 < 0) return fail(L4D_EINVAL, "bad LM-head sizes");
+  if (n < 0 || h <= 0 || v_t <= 0 || v0 < 0 || v0 > INT64_MAX - v_t) return fail(L4D_EINVAL, "bad LM-head sizes");
   if (h % 8 || h > 8192) return fail(L4D_EINVAL, "hidden must be a multiple of 8 and at most 8192");
   if (n > (int64_t)1 << 20 || v_t > (int64_t)1 << 24) return fail(L4D_EINVAL, "problem too large");   // grid sizes
   for (const void* p : rows)
