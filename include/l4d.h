@@ -513,9 +513,12 @@ int llama_layer_packed_bwd(const l4d_model* model, const l4d_parallel* par, cons
  * vocabulary: 2^31 and 2^26 tokens x columns (268 MB) or, for many tokens, 65536 and
  * 8192 columns.  The backward adds fp32 d_hidden and two or three copies of hidden.
  * Requirements: h % 8 == 0, h <= 8192; hidden, w_lm and d_hidden 16-byte aligned;
- * N <= 2^20, v_t <= 2^24; finite hidden rows also of ignored tokens (their zero
+ * N <= 2^20, v_t <= 2^24, vocab_start + v_t < 2^63; finite hidden rows also of ignored tokens (their zero
  * weights multiply them in d_w_lm); outputs that overlap neither inputs nor each other
  * (d_hidden read as hidden or w_lm: L4D_EINVAL).  N == 0 launches nothing.
+ * The tokens of one target are completed one after another: with 8192 tokens and a
+ * hidden size of 4096 a target that a tenth of them have adds 0.3 ms to the backward, one
+ * that all have 4 ms.
  * ---------------------------------------------------------------------- */
 int l4d_lm_loss_workspace_bytes(int64_t n_tokens, int64_t hidden, int64_t vocab_shard, uint64_t* fwd_bytes,
                                 uint64_t* bwd_bytes);

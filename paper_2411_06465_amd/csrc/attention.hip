@@ -1143,7 +1143,9 @@ hipError_t attn_bwd(const AttnParams& p, int part, hipStream_t stream) {
 //    heads of 128: none cut 361 us, these 351; 16384 tokens in 160, 16/4 heads of 64:
 //    172 and 138.  Limits of 1, 2.25, 4 times the even share, backward: 6 documents of
 //    8192 tokens, 32/8 heads of 128, 588, 606, 625 us; 23: 313, 301, 320; 200 of
-//    65536, 8/1 heads of 64, 285, 276, 346.
+//    65536, 8/1 heads of 64, 285, 276, 346.  Where 128 rows are the limit, backward with none
+//    cut, from 257 rows on, from 128 on: 400 documents of 16000 tokens, 22/1 heads of 64,
+//    311, 208, 195 us; 48/1 of 128, 909, 615, 589; 300 of 33000, 64/2 of 128, 1614, 1274, 1295.
 static int splits_of_all(int64_t base, int64_t want, int most) {
   int n = 1;
   while (base * n < want && n < most) n *= 2;

@@ -93,9 +93,9 @@ __device__ __forceinline__ SeqBlock query_block(const PackedAttn& p, int i, int 
 // where some row's maximum grew (a wave-wide vote).
 //
 // Long documents are bound by exponentials and other vector work beside the products,
-// at a power-limited clock: 32768 tokens in 6, 8/1 heads of 128, 625 us, 1.1 PFLOP/s,
-// matrix cores busy 51% at 1.76 GHz.  Short ones by the way to the first products, about
-// 4 us of a workgroup's 6 to 20: 8192 tokens in 23, 32/8 heads of 128, 81 us.
+// at a power-limited clock: 32768 tokens in 6, 8/1 heads of 128, 624 us, 1.1 PFLOP/s,
+// matrix cores busy 55% at 1.7 GHz.  Short ones by the way to the first products, about
+// 4 us of a workgroup's 6 to 20: 8192 tokens in 23, 32/8 heads of 128, 75 us.
 template <int D>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_fwd_kernel(PackedAttn p) {
   constexpr int TB = KT * D * 2;
@@ -339,8 +339,8 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
 // probability is large and dS enters the product in two parts (kLargeP).
 //
 // Bound as the forward is: 32768 tokens in 6 documents, 8/1 heads of 128, 886 us (1.1
-// PFLOP/s, busy 52% at 1.86 GHz); 8192 in 23, 32/8 heads, 120 us; 16384 in 160, 16/4
-// heads of 64, 43 us (48 with two workgroups per CU, here three).
+// PFLOP/s, busy 58% at 1.75 GHz); 8192 in 23, 32/8 heads, 115 us; 16384 in 160, 16/4
+// heads of 64, 41 us (48 with two workgroups per CU, here three).
 template <int D, bool ROPE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_dq_kernel(PackedAttn p) {
   constexpr int KQ = 32;                     // keys per tile
@@ -478,8 +478,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 // documents, 16/4 heads).
 //
 // Bound by the chain of a tile (scores, exponentials, handover, products; 1.0 to 1.3 us)
-// and on long documents by the clock: 32768 tokens in 6, 8/1 heads of 128, 1280 us
-// (1.0 PFLOP/s, matrix cores busy 49% at 1.83 GHz); 8192 in 23, 32/8 heads, 152 us.
+// and on long documents by the clock: 32768 tokens in 6, 8/1 heads of 128, 1287 us
+// (1.0 PFLOP/s, matrix cores busy 49% at 1.79 GHz); 8192 in 23, 32/8 heads, 137 us.
 template <int D, bool ROPE>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) attn_packed_dkdv_kernel(PackedAttn p) {
   constexpr int TB = QT * D * 2;
@@ -717,7 +717,8 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
 
 // dK, dV = the sum of the slices' fp32 parts in order, for the blocks that were cut:
 // a workgroup per block, kv head and quarter of its rows, eight columns per thread.
-// Four slices of 32768 rows and one head of 128: 28 us for 151 MB.
+// Four slices of 32768 rows and one head of 128: 29 us for 151 MB.  It runs wherever a
+// block may be cut, as only the GPU knows the documents: 5 us where few or none are.
 template <int D, bool ROPE>
 __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
   const int hk = static_cast<int>(blockIdx.y), lane = static_cast<int>(threadIdx.x) & 63, at = static_cast<int>(blockIdx.x) / 4;

@@ -776,6 +776,10 @@ __global__ void __launch_bounds__(kJoinWaves * 64) loss_join_kernel(LossJoin p) 
 // A workgroup per token and 2048 columns: d_hidden = dh + (g - hi) W[target], and
 // d_w[target] += what the parts of g leave x hidden, where the first token of a target
 // adds the rows of all of them, in order, so that the sum does not depend on timing.
+// That is a chain of one row's latency per token of a target, behind a search over the
+// targets that grows with the square of the tokens.  8192 tokens, hidden 4096, 32064
+// columns: 178 us with uniform targets, 458 where the most frequent one has 749 tokens (drawn
+// with probability 1/rank), 4.1 ms where it has all; 65536 tokens, hidden 1024: 1.9, 3.0, 31 ms.
 constexpr int kScan = 1024;          // tokens compared between two barriers
 __global__ void __launch_bounds__(256) loss_finish_grad_kernel(LossTargets p) {
   __shared__ float rest[kScan];
