@@ -19,8 +19,8 @@ class PackedAttn(C.Structure):
                [(n, C.c_int32) for n in ("heads", "kv_heads", "d_h", "hpb", "n_slots")] + [("scale", C.c_float)] + \
                [(n, C.c_int64) for n in ("q", "k", "v", "q_ld", "k_ld", "v_ld", "o", "o_ld", "lse", "dout", "do_ld",
                                          "dq", "dk", "dv", "dq_ld", "dk_ld", "dv_ld", "delta", "lse2")] + \
-               [("n_split", C.c_int32), ("cut_rows", C.c_int32), ("list_steps", C.c_int32), ("items", C.c_int64),
-                ("dkv_partial", C.c_int64)]
+               [("n_split", C.c_int32), ("cut_rows", C.c_int32), ("list_steps", C.c_int32), ("rope", C.c_int64),
+                ("items", C.c_int64), ("dkv_partial", C.c_int64)]
 
 
 def plan(starts, tokens, heads, kv):
