@@ -462,6 +462,33 @@ int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void
                     int64_t dv_ld, l4d_arena* arena, void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Attention over packed documents with a sliding window and first tokens that stay visible
+ *
+ * attn_packed_fwd / attn_packed_bwd where row i of a document (counted from its first
+ * row) sees row j <= i iff i - j < window or j < sinks: the last `window` rows up to
+ * itself, and the document's first `sinks`.  Arguments, layouts, rounding and refusals are
+ * those of the calls above; keys that no row of a block of queries sees are not read.  A
+ * window of at least packing->tokens hides nothing, and the call then is the one above, in every bit.
+ * Also L4D_EINVAL: window < 1, sinks outside 0 .. 4096, more than 2^28 rows (with a
+ * window of fewer rows).
+ * The workspace is that of attn_packed_bwd, 8 bytes per row more, and fp32 sums of dk
+ * and dv of the first tokens for every 512 rows (for more than 512 sinks, as many rows).
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int64_t window;       /* rows that a row sees, itself among them */
+  int64_t sinks;        /* first rows of a document that all its rows see */
+} l4d_window;
+
+int attn_window_fwd(const l4d_window* window, const l4d_attn* attn, const l4d_packing* packing, const void* q, int64_t q_ld,
+                    const void* k, int64_t k_ld, const void* v, int64_t v_ld, void* o, int64_t o_ld, float* lse,
+                    void* hip_stream);
+int l4d_attn_window_workspace_bytes(const l4d_window* window, const l4d_attn* attn, int64_t tokens, uint64_t* bytes);
+int attn_window_bwd(const l4d_window* window, const l4d_attn* attn, const l4d_packing* packing, const void* q, int64_t q_ld,
+                    const void* k, int64_t k_ld, const void* v, int64_t v_ld, const void* o, int64_t o_ld, const float* lse,
+                    const void* d_o, int64_t do_ld, void* dq, int64_t dq_ld, void* dk, int64_t dk_ld, void* dv,
+                    int64_t dv_ld, l4d_arena* arena, void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * The layer over packed documents
  *
  * llama_layer_fwd / llama_layer_bwd with one row of packed documents as the

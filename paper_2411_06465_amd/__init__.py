@@ -84,6 +84,10 @@ class Attn(C.Structure):
     _fields_ = [("n_heads", C.c_int64), ("n_kv_heads", C.c_int64), ("head_dim", C.c_int64), ("scale", C.c_float)]
 
 
+class Window(C.Structure):
+    _fields_ = [("window", C.c_int64), ("sinks", C.c_int64)]
+
+
 _lib = None
 
 
@@ -129,6 +133,11 @@ def lib():
             "attn_packed_fwd": ([C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64, P, P], C.c_int),
             "attn_packed_bwd": ([C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64, P, P, i64,
                                  P, i64, P, i64, P, i64, P, P], C.c_int),
+            "attn_window_fwd": ([C.POINTER(Window), C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64,
+                                 P, P], C.c_int),
+            "attn_window_bwd": ([C.POINTER(Window), C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64,
+                                 P, P, i64, P, i64, P, i64, P, i64, P, P], C.c_int),
+            "l4d_attn_window_workspace_bytes": ([C.POINTER(Window), C.POINTER(Attn), i64, C.POINTER(u64)], C.c_int),
             "llama_layer_packed_fwd": ([C.POINTER(Model), C.POINTER(Parallel), C.POINTER(PackingC), C.POINTER(Rope),
                                         C.POINTER(LayerWeights), P, C.POINTER(PeerInputs), C.POINTER(PeerOutputs), P,
                                         P, C.POINTER(P), P], C.c_int),
@@ -492,14 +501,27 @@ def _attn_shapes(q, k, packing):
     return n, a, g, d, (n, a, d), (n, g, d)
 
 
-def attn_packed_fwd(q, k, v, o, lse, packing, scale=0.0, stream=None):
-    """Causal attention within the packing's documents.  q, o [tokens][heads][d], k, v
-    [tokens][kv_heads][d] bf16; lse f32 [heads][tokens].  scale 0 = 1/sqrt(d)."""
+def _attn_fwd(entry, window, q, k, v, o, lse, packing, scale, stream):
     import torch
     n, a, g, d, qs, ks = _attn_shapes(q, k, packing)
     args = _attn_args(q, (("q", q, qs), ("k", k, ks), ("v", v, ks), ("o", o, qs)))
-    _launch(lib().attn_packed_fwd, q, stream, Attn(a, g, d, scale), _on_one_device(packing, q), *args,
+    _launch(entry, q, stream, *window, Attn(a, g, d, scale), _on_one_device(packing, q), *args,
             _flat("lse", lse, torch.float32, (a, n), q))
+
+
+def _attn_bwd(entry, window, q, k, v, o, lse, d_o, dq, dk, dv, packing, arena, scale, stream):
+    import torch
+    n, a, g, d, qs, ks = _attn_shapes(q, k, packing)
+    args = _attn_args(q, (("q", q, qs), ("k", k, ks), ("v", v, ks), ("o", o, qs), ("d_o", d_o, qs), ("dq", dq, qs),
+                          ("dk", dk, ks), ("dv", dv, ks)))
+    _launch(entry, q, stream, *window, Attn(a, g, d, scale), _on_one_device(packing, q), *args[:8],
+            _flat("lse", lse, torch.float32, (a, n), q), *args[8:], arena.h)
+
+
+def attn_packed_fwd(q, k, v, o, lse, packing, scale=0.0, stream=None):
+    """Causal attention within the packing's documents.  q, o [tokens][heads][d], k, v
+    [tokens][kv_heads][d] bf16; lse f32 [heads][tokens].  scale 0 = 1/sqrt(d)."""
+    _attn_fwd(lib().attn_packed_fwd, (), q, k, v, o, lse, packing, scale, stream)
 
 
 def l4d_attn_packed_workspace_bytes(tokens, n_heads, n_kv_heads, head_dim):
@@ -510,12 +532,29 @@ def l4d_attn_packed_workspace_bytes(tokens, n_heads, n_kv_heads, head_dim):
 
 def attn_packed_bwd(q, k, v, o, lse, d_o, dq, dk, dv, packing, arena, scale=0.0, stream=None):
     """Gradients of attn_packed_fwd, overwriting dq, dk and dv."""
-    import torch
-    n, a, g, d, qs, ks = _attn_shapes(q, k, packing)
-    args = _attn_args(q, (("q", q, qs), ("k", k, ks), ("v", v, ks), ("o", o, qs), ("d_o", d_o, qs), ("dq", dq, qs),
-                          ("dk", dk, ks), ("dv", dv, ks)))
-    _launch(lib().attn_packed_bwd, q, stream, Attn(a, g, d, scale), _on_one_device(packing, q), *args[:8],
-            _flat("lse", lse, torch.float32, (a, n), q), *args[8:], arena.h)
+    _attn_bwd(lib().attn_packed_bwd, (), q, k, v, o, lse, d_o, dq, dk, dv, packing, arena, scale, stream)
+
+
+def make_window(window, sinks=0):
+    """Rows see the `window` rows up to themselves and their document's first `sinks`."""
+    return Window(window, sinks)
+
+
+def attn_window_fwd(window, q, k, v, o, lse, packing, scale=0.0, stream=None):
+    """attn_packed_fwd within a sliding window (make_window)."""
+    _attn_fwd(lib().attn_window_fwd, (window,), q, k, v, o, lse, packing, scale, stream)
+
+
+def l4d_attn_window_workspace_bytes(window, tokens, n_heads, n_kv_heads, head_dim):
+    b = C.c_uint64()
+    _check(lib().l4d_attn_window_workspace_bytes(C.byref(window), C.byref(Attn(n_heads, n_kv_heads, head_dim, 0.0)), tokens,
+                                                 C.byref(b)))
+    return b.value
+
+
+def attn_window_bwd(window, q, k, v, o, lse, d_o, dq, dk, dv, packing, arena, scale=0.0, stream=None):
+    """Gradients of attn_window_fwd, overwriting dq, dk and dv."""
+    _attn_bwd(lib().attn_window_bwd, (window,), q, k, v, o, lse, d_o, dq, dk, dv, packing, arena, scale, stream)
 
 
 def llama_layer_packed_fwd(model, par, weights, x, y, arena, packing, rope=None, peers=None, sends=None, stream=None):

@@ -905,6 +905,7 @@ int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, co
 }  // namespace
 
 namespace {
+constexpr int kMaxSinks = 4096;
 struct AttnRows {        // one tensor of a call
   const char* name;
   const void* p;
@@ -941,23 +942,40 @@ int attn_distinct(const AttnRows* t, int n, int first_out) {
 }
 // dQ first: it also writes delta, which dK/dV reads.
 int packed_attn_backward(const PackedAttn& p, hipStream_t s) {
+  const bool w = p.window > 0;
   int rc;
-  if ((rc = launch("attn_packed_dq", s, [&] { return attn_packed_bwd(p, 2, s); }))) return rc;
-  if ((rc = launch("attn_packed_dkdv", s, [&] { return attn_packed_bwd(p, 1, s); }))) return rc;
-  if (p.n_split > 1) return launch("attn_packed_reduce", s, [&] { return attn_packed_bwd(p, 3, s); });
+  if ((rc = launch(w ? "attn_window_dq" : "attn_packed_dq", s, [&] { return attn_packed_bwd(p, 2, s); }))) return rc;
+  if ((rc = launch(w ? "attn_window_dkdv" : "attn_packed_dkdv", s, [&] { return attn_packed_bwd(p, 1, s); }))) return rc;
+  if (p.n_split > 1 &&
+      (rc = launch(w ? "attn_window_reduce" : "attn_packed_reduce", s, [&] { return attn_packed_bwd(p, 3, s); })))
+    return rc;
+  if (p.far_parts) return launch("attn_window_sinks", s, [&] { return attn_packed_bwd(p, 4, s); });
+  return L4D_OK;
+}
+// A window that no row of `tokens` rows reaches past hides nothing: the call is the one without.
+int attn_window(const l4d_window* w, int64_t tokens, PackedAttn* p) {
+  if (!w) return fail(L4D_EINVAL, "window is required");
+  if (w->window < 1) return fail(L4D_EINVAL, "the window must be at least 1");
+  if (w->sinks < 0 || w->sinks > kMaxSinks) return fail(L4D_EINVAL, "sinks must lie in 0 .. %d", kMaxSinks);
+  p->pk.tokens = (int32_t)tokens;
+  if (w->window >= tokens) return L4D_OK;
+  p->window = (int32_t)w->window;
+  p->sinks = (int32_t)w->sinks;
+  attn_window_plan(p);
   return L4D_OK;
 }
 struct PackedWs {
-  uint64_t delta, lse2, items, partial, total;
+  uint64_t delta, lse2, items, partial, sinks, total;
 };
 PackedWs plan_packed(const PackedAttn& p, int64_t tokens) {
   Carver cv;
   PackedWs w{};
   w.delta = cv.take((uint64_t)p.heads * tokens * 4);
   w.lse2 = cv.take((uint64_t)p.heads * tokens * 4);
-  w.items = cv.take((uint64_t)attn_packed_items(tokens) * 8);
+  w.items = cv.take((uint64_t)attn_packed_items(p) * (p.window ? 16 : 8));
   const int splits = attn_packed_most_splits(tokens, p.heads, p.kv_heads);
   w.partial = splits > 1 ? cv.take(2ull * splits * tokens * p.kv_heads * p.d_h * 4) : 0;
+  w.sinks = cv.take(2ull * p.far_parts * splits * p.kv_heads * p.sinks * p.d_h * 4);
   w.total = cv.used;
   return w;
 }
@@ -1614,19 +1632,30 @@ extern "C" int rope_bwd(const l4d_rope* r, int dtype, int64_t tokens, const l4d_
 extern "C" int l4d_attn_packed_workspace_bytes(const l4d_attn* at, int64_t tokens, uint64_t* bytes) {
   if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "tokens must lie in 0 .. 2^30");
   PackedAttn p{};
+  p.pk.tokens = (int32_t)tokens;
   int rc = attn_shape(at, &p);
   if (rc) return rc;
   if (bytes) *bytes = align_up(plan_packed(p, tokens).total);
   return L4D_OK;
 }
+extern "C" int l4d_attn_window_workspace_bytes(const l4d_window* w, const l4d_attn* at, int64_t tokens, uint64_t* bytes) {
+  if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "tokens must lie in 0 .. 2^30");
+  PackedAttn p{};
+  int rc;
+  if ((rc = attn_shape(at, &p)) || (rc = attn_window(w, tokens, &p))) return rc;
+  if (bytes) *bytes = align_up(plan_packed(p, tokens).total);
+  return L4D_OK;
+}
 
-extern "C" int attn_packed_fwd(const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld, const void* k,
-                               int64_t k_ld, const void* v, int64_t v_ld, void* o, int64_t o_ld, float* lse,
-                               void* stream_ptr) {
+// With windowed: attention within w.
+static int attn_forward(bool windowed, const l4d_window* w, const l4d_attn* at, const l4d_packing* pk, const void* q,
+                        int64_t q_ld, const void* k, int64_t k_ld, const void* v, int64_t v_ld, void* o, int64_t o_ld,
+                        float* lse, void* stream_ptr) {
   int rc = check_packing(pk);
   if (rc) return rc;
   PackedAttn p{};
   if ((rc = attn_shape(at, &p))) return rc;
+  if (windowed && (rc = attn_window(w, pk->tokens, &p))) return rc;
   const AttnRows t[4] = {{"q", q, q_ld, at->n_heads}, {"k", k, k_ld, at->n_kv_heads}, {"v", v, v_ld, at->n_kv_heads},
                          {"o", o, o_ld, at->n_heads}};
   if ((rc = attn_rows(t, 4, at->head_dim)) || (rc = attn_distinct(t, 4, 3))) return rc;
@@ -1641,17 +1670,29 @@ extern "C" int attn_packed_fwd(const l4d_attn* at, const l4d_packing* pk, const 
   p.q_ld = q_ld, p.k_ld = k_ld, p.v_ld = v_ld, p.o_ld = o_ld;
   p.lse = lse;
   hipStream_t s = static_cast<hipStream_t>(stream_ptr);
-  return launch("attn_packed_fwd", s, [&] { return attn_packed_fwd(p, s); });
+  return launch(p.window ? "attn_window_fwd" : "attn_packed_fwd", s, [&] { return attn_packed_fwd(p, s); });
 }
 
-extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld, const void* k,
-                               int64_t k_ld, const void* v, int64_t v_ld, const void* o, int64_t o_ld, const float* lse,
-                               const void* d_o, int64_t do_ld, void* dq, int64_t dq_ld, void* dk, int64_t dk_ld, void* dv,
-                               int64_t dv_ld, l4d_arena* A, void* stream_ptr) {
+extern "C" int attn_packed_fwd(const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld, const void* k,
+                               int64_t k_ld, const void* v, int64_t v_ld, void* o, int64_t o_ld, float* lse,
+                               void* stream_ptr) {
+  return attn_forward(false, nullptr, at, pk, q, q_ld, k, k_ld, v, v_ld, o, o_ld, lse, stream_ptr);
+}
+extern "C" int attn_window_fwd(const l4d_window* w, const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld,
+                               const void* k, int64_t k_ld, const void* v, int64_t v_ld, void* o, int64_t o_ld, float* lse,
+                               void* stream_ptr) {
+  return attn_forward(true, w, at, pk, q, q_ld, k, k_ld, v, v_ld, o, o_ld, lse, stream_ptr);
+}
+
+static int attn_backward(bool windowed, const l4d_window* w, const l4d_attn* at, const l4d_packing* pk, const void* q,
+                         int64_t q_ld, const void* k, int64_t k_ld, const void* v, int64_t v_ld, const void* o, int64_t o_ld,
+                         const float* lse, const void* d_o, int64_t do_ld, void* dq, int64_t dq_ld, void* dk, int64_t dk_ld,
+                         void* dv, int64_t dv_ld, l4d_arena* A, void* stream_ptr) {
   int rc = check_packing(pk);
   if (rc) return rc;
   PackedAttn p{};
   if ((rc = attn_shape(at, &p))) return rc;
+  if (windowed && (rc = attn_window(w, pk->tokens, &p))) return rc;
   const int64_t a = at->n_heads, g = at->n_kv_heads;
   const AttnRows t[8] = {{"q", q, q_ld, a}, {"k", k, k_ld, g}, {"v", v, v_ld, g}, {"o", o, o_ld, a},
                          {"d_o", d_o, do_ld, a}, {"dq", dq, dq_ld, a}, {"dk", dk, dk_ld, g}, {"dv", dv, dv_ld, g}};
@@ -1680,8 +1721,24 @@ extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const 
   p.lse2 = reinterpret_cast<float*>(wsb + plan.lse2);
   p.items = reinterpret_cast<int32_t*>(wsb + plan.items);
   p.dkv_partial = reinterpret_cast<float*>(wsb + plan.partial);
+  p.sink_partial = reinterpret_cast<float*>(wsb + plan.sinks);
   attn_packed_plan(&p);
   return packed_attn_backward(p, static_cast<hipStream_t>(stream_ptr));
+}
+
+extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld, const void* k,
+                               int64_t k_ld, const void* v, int64_t v_ld, const void* o, int64_t o_ld, const float* lse,
+                               const void* d_o, int64_t do_ld, void* dq, int64_t dq_ld, void* dk, int64_t dk_ld, void* dv,
+                               int64_t dv_ld, l4d_arena* A, void* stream_ptr) {
+  return attn_backward(false, nullptr, at, pk, q, q_ld, k, k_ld, v, v_ld, o, o_ld, lse, d_o, do_ld, dq, dq_ld, dk, dk_ld, dv,
+                       dv_ld, A, stream_ptr);
+}
+extern "C" int attn_window_bwd(const l4d_window* w, const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld,
+                               const void* k, int64_t k_ld, const void* v, int64_t v_ld, const void* o, int64_t o_ld,
+                               const float* lse, const void* d_o, int64_t do_ld, void* dq, int64_t dq_ld, void* dk,
+                               int64_t dk_ld, void* dv, int64_t dv_ld, l4d_arena* A, void* stream_ptr) {
+  return attn_backward(true, w, at, pk, q, q_ld, k, k_ld, v, v_ld, o, o_ld, lse, d_o, do_ld, dq, dq_ld, dk, dk_ld, dv, dv_ld,
+                       A, stream_ptr);
 }
 
 // ============================================================== loss without stored logits

@@ -26,6 +26,7 @@
 //    workgroup, or, when that leaves too few workgroups, over a slice of them
 //    with an fp32 partial per slice that a small kernel sums: no atomics, the
 //    result is deterministic.
+#include <float.h>
 #include <math.h>
 
 #include <type_traits>
@@ -1157,19 +1158,27 @@ void attn_packed_plan(PackedAttn* p) {
   p->cut_rows = 0;
   // The documents of one of the 256 threads have at most that many blocks.  Starts that are
   // not in order may make more: the list's counts then still stay below 2^31.
-  p->list_steps = static_cast<int32_t>(tokens / 128 + p->pk.n_seqs / 256 + 1);
+  p->list_steps = static_cast<int32_t>(tokens / 128 + p->pk.n_seqs / 256 + 1 + attn_far_items(*p));
   if (base < 512) {
     p->n_split = splits_of_all(base, tokens >= 2048 * n_seqs ? 1024 : 512, packed_hpb(p->heads, p->kv_heads));
     return;
   }
-  const double even = static_cast<double>(tokens) * tokens / n_seqs * p->heads / (2.0 * 128 * QT) / 256;
+  double even = static_cast<double>(tokens) * tokens / n_seqs * p->heads / (2.0 * 128 * QT) / 256;
+  if (p->window) even = std::min(even, static_cast<double>(tokens) * (p->window + 64) * p->heads / (128 * QT) / 256);
   const int64_t most = static_cast<int64_t>(std::min(std::max(64.0, even), 1e9)) / group;      // query tiles that stay whole
   p->cut_rows = static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(most * QT + 1, 128), INT32_MAX));
   p->n_split = group % 2 == 0 && tokens >= p->cut_rows ? 2 : 1;
 }
 int64_t attn_packed_places(const PackedAttn& p) {
   const int64_t most = std::min<int64_t>(packed_slots(p, 128), p.pk.tokens);     // blocks with a row
-  return p.cut_rows ? most + (p.n_split - 1) * packed_windows(p) : most * p.n_split;
+  return p.cut_rows ? most + (p.n_split - 1) * packed_windows(p) + attn_far_items(p) : (most + attn_far_items(p)) * p.n_split;
+}
+void attn_window_plan(PackedAttn* p) {
+  p->far_chunk = std::max(512, (p->sinks + 127) / 128 * 128);
+  p->far_rows = (p->sinks + 127) / 128 * 128 + std::max(p->window, 2 * p->far_chunk);
+  const bool far = p->window && p->sinks && p->pk.tokens > p->far_rows;
+  p->far_parts = far ? p->pk.tokens / p->far_chunk + 1 : 0;
+  if (!far) p->far_rows = 1 << 30;
 }
 int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads) {
   const int64_t base = (tokens + 127) / 128 * kv_heads;
@@ -1180,16 +1189,19 @@ int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads) {
 bool attn_packed_fits(const PackedAttn& p) {
   // a grid holds less than 2^32 threads; slots of the smallest query blocks (32 rows) and of the key blocks
   const int64_t q = packed_slots(p, 32) * p.heads, k = packed_slots(p, 128) * p.heads;
-  return q + 1 < (int64_t{1} << 24) && k < (int64_t{1} << 23);
+  if (p.window && p.pk.tokens > 1 << 28) return false;      // the listing workgroup's counts stay in 32 bits
+  return q + 1 < (int64_t{1} << 24) && k + attn_far_items(p) * p.heads < (int64_t{1} << 23) && p.far_parts < 1 << 22;
 }
 
-hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream) {
-  return p.d_h == 128 ? packed_launch<128, false>(p, 0, stream) : packed_launch<64, false>(p, 0, stream);
+template <int D>
+static hipError_t packed_part(PackedAttn& p, int part, hipStream_t stream) {
+  if (p.window) return packed_launch<D, false, true>(p, part, stream);
+  return p.rope && part ? packed_launch<D, true, false>(p, part, stream) : packed_launch<D, false, false>(p, part, stream);
 }
+hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream) { return attn_packed_bwd(p, 0, stream); }
 
 hipError_t attn_packed_bwd(PackedAttn p, int part, hipStream_t stream) {
-  if (p.rope) return p.d_h == 128 ? packed_launch<128, true>(p, part, stream) : packed_launch<64, true>(p, part, stream);
-  return p.d_h == 128 ? packed_launch<128, false>(p, part, stream) : packed_launch<64, false>(p, part, stream);
+  return p.d_h == 128 ? packed_part<128>(p, part, stream) : packed_part<64>(p, part, stream);
 }
 
 }  // namespace l4d

@@ -75,9 +75,44 @@ __device__ __forceinline__ void turn_back(f32x16 (&acc)[D / 32], const float2* t
 // first, where one load shows all documents (32768 tokens in 6 documents, 8/1 heads of 128:
 // forward 653 -> 625 us, dQ 933 -> 886; 8192 tokens in 23, 32/8 heads: forward 85 -> 81, dQ
 // as it was), else the documents one after another, last blocks first.
+template <bool WINDOW>
 __device__ __forceinline__ SeqBlock query_block(const PackedAttn& p, int i, int rows, int lane) {
-  return p.pk.n_seqs > 1 && p.pk.n_seqs < 64 ? ranked_block(p.pk, i, rows, lane)
-                                             : seq_block(p.pk, p.n_slots - 1 - i, rows, lane);
+  return !WINDOW && p.pk.n_seqs > 1 && p.pk.n_seqs < 64 ? ranked_block(p.pk, i, rows, lane)
+                                                        : seq_block(p.pk, p.n_slots - 1 - i, rows, lane);
+}
+
+// ------------------------------------------------------------------ sliding window, first tokens visible
+// WINDOW kernels: key j of a document is visible to query i >= j where i - j < window or
+// j is one of the document's first `sinks` rows.  A block of queries walks the tiles of the
+// first rows, then those from its first row's window on; the tiles between are never read.
+struct KeyTiles {
+  int head, skip, n;     // tiles of the first rows; tiles left out behind them; tiles to walk
+  // first key of tile t, from the document's first row on
+  template <bool WINDOW>
+  __device__ __forceinline__ int key(int t, int size) const { return (WINDOW && t >= head ? t + skip : t) * size; }
+};
+template <bool WINDOW>
+__device__ __forceinline__ KeyTiles key_tiles(const PackedAttn& p, const SeqBlock& blk, int n_keys, int size) {
+  const int all = (n_keys + size - 1) / size;
+  if constexpr (!WINDOW) return KeyTiles{0, 0, all};
+  const int head = min((p.sinks + size - 1) / size, all);
+  const int first = max(blk.row0 - blk.lo - p.window + 1, 0) / size;      // the tile of the first row's first key
+  const int skip = max(first - head, 0);
+  return KeyTiles{head, skip, all - skip};
+}
+// Whether the mask of a window cuts the tile of keys k0 .. k0 + size - 1 for one of the rows up to last_q.
+__device__ __forceinline__ bool window_cuts(const PackedAttn& p, int lo, int k0, int size, int last_q) {
+  return k0 <= last_q - p.window && k0 + size > lo + p.sinks;
+}
+
+// Rows that the queries of a block of keys cover, from its first row on: to the last row that
+// sees its last key; to far_rows behind the document's first row where the block holds first
+// tokens, whose later rows go in chunks of far_chunk rows (attn_packed_dkdv_kernel).
+template <bool WINDOW>
+__device__ __forceinline__ int block_rows(const PackedAttn& p, int lo, int hi, int row0) {
+  if constexpr (!WINDOW) return hi - row0;
+  if (row0 - lo < p.sinks) return min(hi, lo + p.far_rows) - row0;
+  return min(hi - row0, 127 + p.window);
 }
 
 // ------------------------------------------------------------------ forward
@@ -96,7 +131,7 @@ __device__ __forceinline__ SeqBlock query_block(const PackedAttn& p, int i, int 
 // at a power-limited clock: 32768 tokens in 6, 8/1 heads of 128, 624 us, 1.1 PFLOP/s,
 // matrix cores busy 55% at 1.7 GHz.  Short ones by the way to the first products, about
 // 4 us of a workgroup's 6 to 20: 8192 tokens in 23, 32/8 heads of 128, 75 us.
-template <int D>
+template <int D, bool WINDOW>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_fwd_kernel(PackedAttn p) {
   constexpr int TB = KT * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t k0[TB], v0[TB], k1[TB], v1[TB];
@@ -104,7 +139,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_hg = p.heads / p.hpb, rows = 128 / p.hpb;
   const int id = static_cast<int>(blockIdx.x), h0 = id % n_hg * p.hpb;
-  const SeqBlock blk = query_block(p, id / n_hg, rows, lane);
+  const SeqBlock blk = query_block<WINDOW>(p, id / n_hg, rows, lane);
   if (blk.row0 >= blk.hi) return;
   const int hq = h0 + wave % p.hpb, hk = h0 / (p.heads / p.kv_heads);
   const int wave_q0 = blk.row0 + wave / p.hpb * 32;
@@ -115,17 +150,19 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   const LaneAddr la = lane_addr<D>(lane);
 
   const float c = p.scale * kLog2e;
-  float m_run = -INFINITY, l_run = 0.f;
+  // a window may hide a whole tile from a row: its maximum then stays finite, and exp2(-inf - m_run) 0
+  float m_run = WINDOW ? -FLT_MAX : -INFINITY, l_run = 0.f;
   f32x16 o[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = f32x16{};
 
   const TileCopy<D, KT> copy_k(p.k_ld, wave, lane), copy_v(p.v_ld, wave, lane);
   const uint32_t ka0 = lds_addr(k0), ka1 = lds_addr(k1), va0 = lds_addr(v0), va1 = lds_addr(v1);
-  const int n_tiles = (n_keys + KT - 1) / KT;
+  const KeyTiles tiles = key_tiles<WINDOW>(p, blk, n_keys, KT);
+  const int n_tiles = tiles.n;
   const auto copy_tile = [&](const TileCopy<D, KT>& copy, const uint16_t* base, int64_t ld, int t, uint32_t lds)
       __attribute__((always_inline)) {
-    const int64_t row = blk.lo + t * KT;
+    const int64_t row = blk.lo + tiles.key<WINDOW>(t, KT);
     if (t < n_tiles) copy(lds, base + row * ld + hk * D, blk.hi - static_cast<int>(row));
   };
   // the first tiles' copies, and under them the queries
@@ -153,7 +190,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   // exponentials.  After the last tile sn comes from stale LDS and is never used.
   const auto step = [&](int t, const uint8_t* vt, const uint8_t* kt_next, f32x16 (&s)[2], float mx, f32x16 (&sn)[2],
                         float& mxn) __attribute__((always_inline)) {
-    const int kpos0 = blk.lo + t * KT;
+    const int kpos0 = blk.lo + tiles.key<WINDOW>(t, KT);
     if (kpos0 + KT - 1 > wave_q0) {                   // the tile reaches past the wave's first row
       const int lim = my_q - kpos0 - rbase;           // last visible key, relative to the lane's first
 #pragma unroll
@@ -161,6 +198,17 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (t2 * 32 + 8 * (i >> 2) + (i & 3) > lim) s[t2][i] = -INFINITY;
+      mx = row_max(s);
+    }
+    if (WINDOW && window_cuts(p, blk.lo, kpos0, KT, wave_q0 + 31)) {
+      const int out = my_q - p.window - kpos0 - rbase, sink = blk.lo + p.sinks - kpos0 - rbase;   // hidden: sink <= key <= out
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = t2 * 32 + 8 * (i >> 2) + (i & 3);
+          if (key >= sink && key <= out) s[t2][i] = -INFINITY;
+        }
       mx = row_max(s);
     }
     mx = half_max(mx) * c;
@@ -277,12 +325,16 @@ __device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
 // in 160, 16/4 heads of 64.  The list hides behind the other workgroups' dQ.  Its order
 // within a step varies, the sums do not; steps of 1/16 scatter a document's neighbours,
 // which read the same rows (1305 -> 1280 us on the long documents).
+//
+// With a window the entries are {first row, sign bit: second slice; first query row; row
+// behind the last one; row behind the first tokens, sign bit: sums in parts}, and behind the
+// blocks of a document's first tokens come the chunks of the rows far from them.
 constexpr int kOrderBins = 2048;
+template <bool WINDOW>
 __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int room = p.pk.tokens + packed_windows(p);
+  const int room = static_cast<int>(attn_packed_items(p) - 1);
   const int group = p.heads / p.kv_heads;
-  int2* items = reinterpret_cast<int2*>(p.items) + 1;
   for (int i = tid; i < kOrderBins; i += 256) bin[i] = 0;
   __syncthreads();
   // a document per thread: a document of n blocks takes the pass n^2 tiles, this loop n steps
@@ -290,14 +342,26 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
     int left = p.list_steps;             // no more blocks than that, whatever starts holds
     for (int i = tid; i < p.pk.n_seqs; i += 256) {
       const int hi = seq_start(p.pk, i + 1);
-      for (int row0 = seq_start(p.pk, i); row0 < hi && left > 0; row0 += 128, --left) {
-        const int n_rows = hi - row0, slices = packed_slices(p, n_rows);
+      const int lo = seq_start(p.pk, i);
+      const auto add = [&](int row0, int q0, int n_rows, int slices, int n) __attribute__((always_inline)) {
         const float work = static_cast<float>((n_rows + QT - 1) / QT) * (group / slices);
-        visit(row0, hi, static_cast<int>(__float_as_uint(work) >> 17) - (127 << 6), p.cut_rows ? slices : 1);
+        visit(lo, hi, row0, q0, n_rows, static_cast<int>(__float_as_uint(work) >> 17) - (127 << 6), n);
+      };
+      for (int row0 = lo; row0 < hi && left > 0; row0 += 128, --left) {
+        const int n_rows = block_rows<WINDOW>(p, lo, hi, row0), slices = packed_slices(p, n_rows);
+        add(row0, row0, n_rows, slices, p.cut_rows ? slices : 1);
       }
+      if constexpr (WINDOW)
+        for (int q0 = lo + p.far_rows; q0 < hi;) {
+          const int end = min(hi, (q0 / p.far_chunk + 1) * p.far_chunk);
+          for (int row0 = lo; row0 < lo + p.sinks && left > 0; row0 += 128, --left)
+            add(row0, q0, end - q0, p.cut_rows ? 1 : p.n_split, 1);
+          if (left <= 0) break;
+          q0 = end;
+        }
     }
   };
-  each([&](int, int, int k, int n) { atomicAdd(&bin[k], n); });
+  each([&](int, int, int, int, int, int k, int n) { atomicAdd(&bin[k], n); });
   __syncthreads();
   if (wave == 0) {                       // entries in fuller bins, for every bin
     constexpr int M = kOrderBins / 64;
@@ -321,9 +385,16 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
     }
   }
   __syncthreads();
-  each([&](int row0, int hi, int k, int n) {
+  each([&](int lo, int hi, int row0, int q0, int n_rows, int k, int n) {
     const int at = atomicAdd(&bin[k], n);
-    for (int j = 0; j < n && at + j < room; ++j) items[at + j] = make_int2(row0 | (j ? INT32_MIN : 0), hi);
+    for (int j = 0; j < n && at + j < room; ++j) {
+      const int first = row0 | (j ? INT32_MIN : 0);
+      if constexpr (WINDOW)
+        reinterpret_cast<int4*>(p.items)[1 + at + j] = make_int4(
+            first, q0, q0 + n_rows, (lo + p.sinks) | (row0 - lo < p.sinks && hi - lo > p.far_rows ? INT32_MIN : 0));
+      else
+        reinterpret_cast<int2*>(p.items)[1 + at + j] = make_int2(first, hi);
+    }
   });
 }
 
@@ -341,7 +412,7 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
 // Bound as the forward is: 32768 tokens in 6 documents, 8/1 heads of 128, 886 us (1.1
 // PFLOP/s, busy 58% at 1.75 GHz); 8192 in 23, 32/8 heads, 115 us; 16384 in 160, 16/4
 // heads of 64, 41 us (48 with two workgroups per CU, here three).
-template <int D, bool ROPE>
+template <int D, bool ROPE, bool WINDOW>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_dq_kernel(PackedAttn p) {
   constexpr int KQ = 32;                     // keys per tile
   constexpr int TB = KQ * D * 2;
@@ -350,9 +421,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_hg = p.heads / p.hpb, rows = 128 / p.hpb;
   static_assert(sizeof(kbuf) >= kOrderBins * sizeof(int), "the bins lie in the K tiles");
-  if (blockIdx.x == 0) return packed_order(p, reinterpret_cast<int*>(kbuf));
+  if (blockIdx.x == 0) return packed_order<WINDOW>(p, reinterpret_cast<int*>(kbuf));
   const int id = static_cast<int>(blockIdx.x) - 1, h0 = id % n_hg * p.hpb;
-  const SeqBlock blk = query_block(p, id / n_hg, rows, lane);
+  const SeqBlock blk = query_block<WINDOW>(p, id / n_hg, rows, lane);
   if (blk.row0 >= blk.hi) return;
   const int hq = h0 + wave % p.hpb, hk = h0 / (p.heads / p.kv_heads);
   const int wave_q0 = blk.row0 + wave / p.hpb * 32;
@@ -363,9 +434,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   const LaneAddr la = lane_addr<D>(lane);
 
   const TileCopy<D, KQ> copy_k(p.k_ld, wave, lane), copy_v(p.v_ld, wave, lane);
-  const int n_tiles = (n_keys + KQ - 1) / KQ;
+  const KeyTiles tiles = key_tiles<WINDOW>(p, blk, n_keys, KQ);
+  const int n_tiles = tiles.n;
   const auto issue = [&](int t, int b) __attribute__((always_inline)) {
-    const int64_t r0 = blk.lo + t * KQ;
+    const int64_t r0 = blk.lo + tiles.key<WINDOW>(t, KQ);
     const int valid = blk.hi - static_cast<int>(r0);
     copy_k(lds_addr(kbuf[b]), p.k + r0 * p.k_ld + hk * D, valid);
     copy_v(lds_addr(vbuf[b]), p.v + r0 * p.v_ld + hk * D, valid);
@@ -414,11 +486,20 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     __builtin_amdgcn_sched_barrier(0);
     f32x16 sc = f32x16{}, dp = f32x16{};
     scores2<D, kLookDq>(kbuf[b], 0, qf, sc, vbuf[b], 0, dof, dp, la);
-    if (blk.lo + t * KQ + KQ - 1 > wave_q0) {               // the tile reaches past the wave's first row
-      const int lim = my_q - (blk.lo + t * KQ) - rbase;
+    const int kpos0 = blk.lo + tiles.key<WINDOW>(t, KQ);
+    if (kpos0 + KQ - 1 > wave_q0) {                         // the tile reaches past the wave's first row
+      const int lim = my_q - kpos0 - rbase;
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (8 * (i >> 2) + (i & 3) > lim) sc[i] = -INFINITY;
+    }
+    if (WINDOW && window_cuts(p, blk.lo, kpos0, KQ, wave_q0 + 31)) {
+      const int out = my_q - p.window - kpos0 - rbase, sink = blk.lo + p.sinks - kpos0 - rbase;   // hidden: sink <= key <= out
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = 8 * (i >> 2) + (i & 3);
+        if (key >= sink && key <= out) sc[i] = -INFINITY;
+      }
     }
     float p_max = 0.f, sum = 0.f;
 #pragma unroll
@@ -480,7 +561,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 // Bound by the chain of a tile (scores, exponentials, handover, products; 1.0 to 1.3 us)
 // and on long documents by the clock: 32768 tokens in 6, 8/1 heads of 128, 1287 us
 // (1.0 PFLOP/s, matrix cores busy 49% at 1.79 GHz); 8192 in 23, 32/8 heads, 137 us.
-template <int D, bool ROPE>
+template <int D, bool ROPE, bool WINDOW>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) attn_packed_dkdv_kernel(PackedAttn p) {
   constexpr int TB = QT * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t qg[kDkvStages][2][TB];   // per stage: Q tile, then dO tile
@@ -495,15 +576,23 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
   // rows it then has in its L2.
   const int id = static_cast<int>(blockIdx.x), cut = p.cut_rows ? 1 : p.n_split, at = id / (p.kv_heads * cut);
   const int n_items = p.items[0];
-  const int2 item = reinterpret_cast<const int2*>(p.items)[1 + at];
+  int4 item;                             // see packed_order
+  if constexpr (WINDOW) {
+    item = reinterpret_cast<const int4*>(p.items)[1 + at];
+  } else {
+    const int2 x = reinterpret_cast<const int2*>(p.items)[1 + at];
+    item = make_int4(x.x, x.x & INT32_MAX, x.y, 0);
+  }
   if (at >= n_items) return;
   const int hk = id % (p.kv_heads * cut) / cut, split = p.cut_rows ? item.x < 0 : id % cut;
-  const struct { int row0, hi; } blk{item.x & INT32_MAX, item.y};
-  const int n_rows = blk.hi - blk.row0, n_qt = (n_rows + QT - 1) / QT;
-  const int slices = packed_slices(p, n_rows);
+  const struct { int row0, q0, hi; } blk{item.x & INT32_MAX, WINDOW ? item.y : item.x & INT32_MAX, item.z};
+  const int n_rows = blk.hi - blk.q0, n_qt = (n_rows + QT - 1) / QT;
+  const bool far = WINDOW && blk.q0 != blk.row0;      // rows far from first tokens: their sums go in a part
+  const int slices = far ? (p.cut_rows ? 1 : p.n_split) : packed_slices(p, n_rows);
   const int hps = group / slices, head0 = hk * group + split * hps;
   const int grp_k0 = blk.row0 + grp * 32;
   const int my_key = grp_k0 + (lane & 31);
+  const int sink_end = item.w & INT32_MAX;
   const bool key_ok = my_key < blk.hi;
   const int rbase = 4 * (lane >> 5);
   const LaneAddr la = lane_addr<D>(lane);
@@ -524,8 +613,8 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
   const TileCopy<D, QT> copy(ld, grp, lane);
   const uint32_t qg_addr = lds_addr(qg) + role * TB, st_addr = lds_addr(st) + (role * QT + grp * (QT / 4)) * 4;
   // the next tile to copy: its first row, its head's statistics from the block's first row on, its query tile, tiles left after it
-  uint64_t src = pick(addr(p.q), addr(p.dout)) + (blk.row0 * ld + head0 * D) * 2;
-  uint64_t row = pick(addr(p.lse2), addr(p.delta)) + (static_cast<int64_t>(head0) * p.pk.tokens + blk.row0) * 4;
+  uint64_t src = pick(addr(p.q), addr(p.dout)) + (blk.q0 * ld + head0 * D) * 2;
+  uint64_t row = pick(addr(p.lse2), addr(p.delta)) + (static_cast<int64_t>(head0) * p.pk.tokens + blk.q0) * 4;
   const int64_t tile_step = QT * ld * 2, head_step = D * 2 - (n_qt - 1) * tile_step;
   int copy_qt = 0, copy_left = hps * n_qt - 1;
   // Copies that tile into stage b, kCopies per wave, and moves on; past the last
@@ -567,7 +656,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
   };
   // role 0: P = exp(S - lse) of tile qt from its scores in s; bf16 into x, fp32 into handover hb
   auto probs = [&](int qt, const float4 (&ls4)[4], float4 (*hb)[2][64]) __attribute__((always_inline)) {
-    const int q0 = blk.row0 + qt * QT;
+    const int q0 = blk.q0 + qt * QT;
 #pragma unroll
     for (int jj = 0; jj < 4; ++jj) {
       const float4 ls = ls4[jj];
@@ -575,9 +664,11 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
 #pragma unroll
       for (int u = 0; u < 4; ++u) s[4 * jj + u] = fast_exp2(fmaf(s[4 * jj + u], c, -lsv[u]));
     }
-    if (q0 < grp_k0 + 31 || q0 + QT > blk.hi) {      // the tile straddles the diagonal, or the document ends in it
+    // the tile straddles the diagonal, the document ends in it, or the first key's window does
+    if (q0 < grp_k0 + 31 || q0 + QT > blk.hi || (WINDOW && q0 + QT > grp_k0 + p.window)) {
       // visible query rows r (relative to the lane's first row): lo <= r <= hi
-      const int lo = (key_ok ? my_key - q0 : QT) - rbase, hi = blk.hi - 1 - q0 - rbase;
+      const int last = WINDOW && my_key >= sink_end ? min(blk.hi, my_key + p.window) : blk.hi;
+      const int lo = (key_ok ? my_key - q0 : QT) - rbase, hi = last - 1 - q0 - rbase;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int r = 8 * (i >> 2) + (i & 3);
@@ -692,6 +783,23 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
   wait_copies<0>();      // no copy may land after the end
 
   const float mul = role == 1 ? p.scale : 1.f;
+  if constexpr (WINDOW) {
+    if (item.w < 0) {        // first tokens of a document with rows far from them: joined by attn_sink_reduce_kernel
+      const int lo = sink_end - p.sinks, part = far ? blk.q0 / p.far_chunk : (lo + p.far_rows) / p.far_chunk - 1;
+      const int64_t half = static_cast<int64_t>(p.far_parts) * p.n_split * p.kv_heads * p.sinks * D;
+      if (my_key < sink_end) {
+        float* out = p.sink_partial + (role == 1 ? 0 : half) +
+                     (((static_cast<int64_t>(part) * p.n_split + split) * p.kv_heads + hk) * p.sinks + my_key - lo) * D;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int jj = 0; jj < 4; ++jj)
+            *reinterpret_cast<float4*>(out + dt * 32 + 8 * jj + rbase) =
+                make_float4(acc[dt][4 * jj] * mul, acc[dt][4 * jj + 1] * mul, acc[dt][4 * jj + 2] * mul, acc[dt][4 * jj + 3] * mul);
+      }
+      if (far) return;
+    }
+  }
   if (slices > 1) {
     if (!key_ok) return;
     // lane owns key my_key; register i of tile dt is d = 32 dt + acc_row(i)
@@ -719,12 +827,12 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
 // a workgroup per block, kv head and quarter of its rows, eight columns per thread.
 // Four slices of 32768 rows and one head of 128: 29 us for 151 MB.  It runs wherever a
 // block may be cut, as only the GPU knows the documents: 5 us where few or none are.
-template <int D, bool ROPE>
+template <int D, bool ROPE, bool WINDOW>
 __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
   const int hk = static_cast<int>(blockIdx.y), lane = static_cast<int>(threadIdx.x) & 63, at = static_cast<int>(blockIdx.x) / 4;
   const SeqBlock blk = p.cut_rows ? block_at(p.pk, at * 128, lane) : seq_block(p.pk, at, 128, lane);
   if (blk.row0 >= blk.hi) return;
-  const int n_rows = blk.hi - blk.row0, slices = packed_slices(p, n_rows);
+  const int n_rows = blk.hi - blk.row0, slices = packed_slices(p, block_rows<WINDOW>(p, blk.lo, blk.hi, blk.row0));
   if (slices == 1) return;
   const int64_t step = static_cast<int64_t>(p.pk.tokens) * p.kv_heads * D;
   constexpr int C = D / 8, R = 256 / C;                  // rows at a time
@@ -772,6 +880,43 @@ __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
   }
 }
 
+// dK, dV of first tokens whose document has rows far from them: the sum of their block's own
+// part and of those of the far rows, in order, over what attn_packed_dkdv_kernel or
+// attn_packed_reduce_kernel stored.  A workgroup per part that may be a document's first and
+// kv head; a wave per first token and tensor, columns over its lanes.
+template <int D>
+__global__ void __launch_bounds__(256) attn_sink_reduce_kernel(PackedAttn p) {
+  const int lane = static_cast<int>(threadIdx.x) & 63, hk = static_cast<int>(blockIdx.y);
+  const int part0 = static_cast<int>(blockIdx.x), base = (part0 + 1) * p.far_chunk;
+  // the document whose first far row lies in chunk part0 + 1
+  const SeqRows s = seq_of_row(p.pk, base + p.far_chunk - 1 - p.far_rows, lane);
+  if (s.i < 0 || s.lo + p.far_rows < base || s.hi <= s.lo + p.far_rows) return;
+  const int last = (s.hi - 1) / p.far_chunk;
+  const int64_t step = static_cast<int64_t>(p.kv_heads) * p.sinks * D;       // from one slice to the next
+  const int64_t half = static_cast<int64_t>(p.far_parts) * p.n_split * step;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int i = static_cast<int>(blockIdx.z) * 4 + wave; i < 2 * p.sinks; i += 4 * gridDim.z) {
+    const int which = i & 1, row = i >> 1;
+    const float* src = p.sink_partial + which * half + (static_cast<int64_t>(part0) * p.n_split * p.kv_heads + hk) * p.sinks * D +
+                       static_cast<int64_t>(row) * D;
+    const int own = packed_slices(p, block_rows<true>(p, s.lo, s.hi, s.lo + row / 128 * 128));
+    float v[D / 64] = {};
+    for (int c = 0; c < own; ++c)
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) v[u] += src[c * step + lane * (D / 64) + u];
+    const int far = p.cut_rows ? 1 : p.n_split;
+    for (int part = part0 + 1; part <= last; ++part) {
+      src += p.n_split * step;
+      for (int c = 0; c < far; ++c)
+#pragma unroll
+        for (int u = 0; u < D / 64; ++u) v[u] += src[c * step + lane * (D / 64) + u];
+    }
+    uint16_t* dst = (which ? p.dv + (s.lo + row) * p.dv_ld : p.dk + (s.lo + row) * p.dk_ld) + hk * D + lane * (D / 64);
+    if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst) = pack2(v[0], v[1]);
+    else *dst = f2bf(v[0]);
+  }
+}
+
 // Blocks of `rows` rows over every packing of `tokens` rows.
 int64_t packed_slots(const PackedAttn& p, int rows) { return p.pk.tokens / rows + static_cast<int64_t>(p.pk.n_seqs); }
 
@@ -781,21 +926,24 @@ int packed_hpb(int heads, int kv_heads) {
   return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
 }
 
-template <int D, bool ROPE>
+template <int D, bool ROPE, bool WINDOW>
 hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
   if (part == 0 || part == 2) {
     p.hpb = packed_hpb(p.heads, p.kv_heads);
     p.n_slots = static_cast<int32_t>(packed_slots(p, 128 / p.hpb));
     const dim3 grid(static_cast<unsigned>(p.n_slots) * (p.heads / p.hpb) + (part == 2));    // and the workgroup that lists
-    if (part == 0) hipLaunchKernelGGL(attn_packed_fwd_kernel<D>, grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((attn_packed_dq_kernel<D, ROPE>), grid, dim3(256), 0, stream, p);
+    if (part == 0) hipLaunchKernelGGL((attn_packed_fwd_kernel<D, WINDOW>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((attn_packed_dq_kernel<D, ROPE, WINDOW>), grid, dim3(256), 0, stream, p);
   } else if (part == 1) {
     const unsigned blocks = static_cast<unsigned>(attn_packed_places(p)) * p.kv_heads;
-    hipLaunchKernelGGL((attn_packed_dkdv_kernel<D, ROPE>), dim3(blocks), dim3(512), 0, stream, p);
-  } else {
+    hipLaunchKernelGGL((attn_packed_dkdv_kernel<D, ROPE, WINDOW>), dim3(blocks), dim3(512), 0, stream, p);
+  } else if (part == 3) {
     if (p.n_split == 1) return hipSuccess;
     const dim3 grid(static_cast<unsigned>(p.cut_rows ? packed_windows(p) : packed_slots(p, 128)) * 4, p.kv_heads);
-    hipLaunchKernelGGL((attn_packed_reduce_kernel<D, ROPE>), grid, dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((attn_packed_reduce_kernel<D, ROPE, WINDOW>), grid, dim3(256), 0, stream, p);
+  } else if constexpr (WINDOW) {
+    const dim3 grid(static_cast<unsigned>(p.far_parts - 1), p.kv_heads, std::min((2 * p.sinks + 3) / 4, 8));
+    hipLaunchKernelGGL(attn_sink_reduce_kernel<D>, grid, dim3(256), 0, stream, p);
   }
   return hipGetLastError();
 }
