@@ -427,6 +427,73 @@ int rope_bwd(const l4d_rope* rope, int dtype, int64_t tokens, const l4d_packing*
              const l4d_rope_heads* dq, const l4d_rope_heads* dk, void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Rotary positions with several axes
+ *
+ * rope_fwd / rope_bwd where a token has one position per axis (time, height and width of
+ * images and video) and every pair turns by the position of one of them.
+ *   n_axes: 1 .. 4;  pairs[i]: pairs of axis i, each at least 1, their sum rot_dim/2;
+ *   order    L4D_AXES_SECTIONS: the first pairs[0] pairs belong to axis 0, the next
+ *            pairs[1] to axis 1, and so on;
+ *            L4D_AXES_CYCLED: pair j belongs to axis i = j mod n_axes while j < n_axes
+ *            pairs[i], else to axis 0 (i + n_axes (pairs[i] - 1) < rot_dim/2 for i > 0);
+ *   frequencies  L4D_AXES_SHARED: pair j turns with f_j of the whole head, whatever its axis;
+ *            L4D_AXES_OWN: the m-th pair of an axis (from 0) with f_m of rot_dim = 2 pairs[i].
+ *   positions: int64 [n_axes][tokens] device array of any sign, required.
+ * All else, packing, scalings, in-place and refusals, as in rope_fwd.
+ * ---------------------------------------------------------------------- */
+enum { L4D_AXES_SECTIONS = 0, L4D_AXES_CYCLED = 1 };
+enum { L4D_AXES_SHARED = 0, L4D_AXES_OWN = 1 };
+
+typedef struct {
+  int64_t n_axes;
+  int64_t pairs[4];
+  int32_t order, frequencies;
+} l4d_rope_axes;
+
+int rope_axes_fwd(const l4d_rope* rope, const l4d_rope_axes* axes, int dtype, int64_t tokens, const l4d_packing* packing,
+                  const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, void* hip_stream);
+int rope_axes_bwd(const l4d_rope* rope, const l4d_rope_axes* axes, int dtype, int64_t tokens, const l4d_packing* packing,
+                  const int64_t* positions, const l4d_rope_heads* dq, const l4d_rope_heads* dk, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Norms of query and key heads, with the rotation in the same pass
+ *
+ *   n = x g / sqrt(mean(x^2) + eps) over the head_dim elements of every head,
+ *   y = A R(pos) n, the rotation of rope_fwd (axes NULL) or rope_axes_fwd.
+ * The backward takes x again (nothing is kept) and dy, the gradient of y:
+ *   dn = A R(pos)^T dy,  r = (mean(x^2) + eps)^(-1/2),  d_gain += sum of dn x r over rows and heads,
+ *   dx = r (dn g - x r^2 mean(dn g x)).
+ * Everything between is fp32, outputs are rounded once; the sums of d_gain have a fixed order.
+ *   x, y, dy, dx: up to two tensors [tokens][heads][head_dim] as in rope_fwd (k may be NULL);
+ *   gain: [head_dim], of the call's dtype;  d_gain: f32 [head_dim] (+=);
+ *   axes: NULL or the axes of positions, as above;  packing, positions: as in rope_fwd.  Rows
+ *   of no document add nothing to d_gain, and their outputs are left as they were.
+ *   An output may be an input of its own tensor (same address and stride: y on x, dx on dy
+ *   or x); other arrays that share an element with an output are refused.
+ * The backward needs l4d_qk_norm_workspace_bytes of arena.
+ * Also L4D_EINVAL: an odd head_dim, eps below 1e-30 or not finite, a NULL or misaligned gain.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  const void *x, *gain;
+  void* y;
+  int64_t heads, x_ld, y_ld;
+} l4d_norm_heads;
+
+typedef struct {
+  const void *x, *gain, *dy;
+  void* dx;
+  float* d_gain;
+  int64_t heads, x_ld, dy_ld, dx_ld;
+} l4d_norm_heads_grad;
+
+int qk_norm_rope_fwd(const l4d_rope* rope, const l4d_rope_axes* axes, int dtype, int64_t tokens, const l4d_packing* packing,
+                     const int64_t* positions, float eps, const l4d_norm_heads* q, const l4d_norm_heads* k, void* hip_stream);
+int l4d_qk_norm_workspace_bytes(int64_t tokens, int64_t head_dim, uint64_t* bytes);
+int qk_norm_rope_bwd(const l4d_rope* rope, const l4d_rope_axes* axes, int dtype, int64_t tokens, const l4d_packing* packing,
+                     const int64_t* positions, float eps, const l4d_norm_heads_grad* q, const l4d_norm_heads_grad* k,
+                     l4d_arena* arena, void* hip_stream);
+
+/* ------------------------------------------------------------------------
  * Causal attention over packed documents, grouped query heads
  *
  *   o_i = sum_j p_ij v_j,  p_i. = softmax of scale q_i . k_j over the rows j <= i of
@@ -509,6 +576,32 @@ int llama_layer_packed_bwd(const l4d_model* model, const l4d_parallel* par, cons
                            const l4d_rope* rope, const l4d_layer_weights* w, const l4d_peer_inputs* peers,
                            const l4d_peer_outputs* sends, l4d_stash* stash, const void* dy, void* dx,
                            const l4d_layer_grads* dw, l4d_arena* arena, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Dropout in front of the residual sum, without a stored mask
+ *
+ *   y = residual + keep x / (1 - p)  (residual NULL: keep x / (1 - p));
+ *   dx = keep dy / (1 - p), the gradient of x (that of residual is dy itself).
+ * Element (i, j) has the place e = (first_row + i) cols + j in the whole array, of which a
+ * sequence-parallel rank holds the rows from first_row on: all ranks draw from one mask, and
+ * so does a call over any part of the rows.  It is kept where word e % 4 of Philox4x32-10
+ * (Salmon et al., SC 2011) at the 128-bit counter (e / 4, offset) under the 64-bit key `seed`
+ * is at least p 2^32 (rounded to a whole number).  Nothing of the mask is kept: the backward
+ * forms it again from the same rng, p and first_row.
+ *   rng: int64 [2] device array: seed, offset.  Read on the GPU, so a captured step may
+ *   change it between replays; calls that must not share a mask take another offset.
+ *   dtype: L4D_BF16 or L4D_F32, of x, residual, y, dy, dx: [rows][cols], row strides in elements.
+ * fp32 arithmetic, one rounding.  A dropped element's x or dy is not used, whatever it holds.
+ * y may be x or residual, dx may be dy (same address and stride).
+ * L4D_EINVAL: p below 0 or not below 1 (in 32 bits), rows outside 0 .. 2^31, cols outside
+ * 0 .. 2^24, more than 2^34 elements, first_row outside 0 .. 2^38, an ld below cols or above
+ * 2^31, NULL or misaligned arrays, an output that shares elements with another array in any other way.
+ * ---------------------------------------------------------------------- */
+int dropout_add_fwd(int dtype, int64_t rows, int64_t cols, const void* x, int64_t x_ld, const void* residual,
+                    int64_t residual_ld, void* y, int64_t y_ld, double p, const int64_t* rng, int64_t first_row,
+                    void* hip_stream);
+int dropout_add_bwd(int dtype, int64_t rows, int64_t cols, const void* dy, int64_t dy_ld, void* dx, int64_t dx_ld, double p,
+                    const int64_t* rng, int64_t first_row, void* hip_stream);
 
 /* ------------------------------------------------------------------------
  * LM-head cross-entropy without stored logits

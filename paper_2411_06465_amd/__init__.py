@@ -84,6 +84,19 @@ class Attn(C.Structure):
     _fields_ = [("n_heads", C.c_int64), ("n_kv_heads", C.c_int64), ("head_dim", C.c_int64), ("scale", C.c_float)]
 
 
+class RopeAxes(C.Structure):
+    _fields_ = [("n_axes", C.c_int64), ("pairs", C.c_int64 * 4), ("order", C.c_int32), ("frequencies", C.c_int32)]
+
+
+class NormHeads(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "gain", "y")] + [(n, C.c_int64) for n in ("heads", "x_ld", "y_ld")]
+
+
+class NormHeadsGrad(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "gain", "dy", "dx", "d_gain")] + \
+               [(n, C.c_int64) for n in ("heads", "x_ld", "dy_ld", "dx_ld")]
+
+
 class Window(C.Structure):
     _fields_ = [("window", C.c_int64), ("sinks", C.c_int64)]
 
@@ -130,6 +143,17 @@ def lib():
                           C.POINTER(RopeHeads), P], C.c_int),
             "rope_bwd": ([C.POINTER(Rope), C.c_int, i64, C.POINTER(PackingC), P, C.POINTER(RopeHeads),
                           C.POINTER(RopeHeads), P], C.c_int),
+            "rope_axes_fwd": ([C.POINTER(Rope), C.POINTER(RopeAxes), C.c_int, i64, C.POINTER(PackingC), P,
+                               C.POINTER(RopeHeads), C.POINTER(RopeHeads), P], C.c_int),
+            "rope_axes_bwd": ([C.POINTER(Rope), C.POINTER(RopeAxes), C.c_int, i64, C.POINTER(PackingC), P,
+                               C.POINTER(RopeHeads), C.POINTER(RopeHeads), P], C.c_int),
+            "qk_norm_rope_fwd": ([C.POINTER(Rope), C.POINTER(RopeAxes), C.c_int, i64, C.POINTER(PackingC), P, f32,
+                                  C.POINTER(NormHeads), C.POINTER(NormHeads), P], C.c_int),
+            "qk_norm_rope_bwd": ([C.POINTER(Rope), C.POINTER(RopeAxes), C.c_int, i64, C.POINTER(PackingC), P, f32,
+                                  C.POINTER(NormHeadsGrad), C.POINTER(NormHeadsGrad), P, P], C.c_int),
+            "l4d_qk_norm_workspace_bytes": ([i64, i64, C.POINTER(u64)], C.c_int),
+            "dropout_add_fwd": ([C.c_int, i64, i64, P, i64, P, i64, P, i64, C.c_double, P, i64, P], C.c_int),
+            "dropout_add_bwd": ([C.c_int, i64, i64, P, i64, P, i64, C.c_double, P, i64, P], C.c_int),
             "attn_packed_fwd": ([C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64, P, P], C.c_int),
             "attn_packed_bwd": ([C.POINTER(Attn), C.POINTER(PackingC), P, i64, P, i64, P, i64, P, i64, P, P, i64,
                                  P, i64, P, i64, P, i64, P, P], C.c_int),
@@ -463,6 +487,13 @@ def _rope_io(name, x, y, dtype, tokens, d, like):
     return RopeHeads(x.data_ptr(), x.data_ptr() if y is None else y.data_ptr(), shape[1], x_ld, y_ld)
 
 
+def _float_type(name, t):
+    import torch
+    if t.dtype != torch.bfloat16 and t.dtype != torch.float32:
+        raise TypeError(f"{name} must be bfloat16 or float32, not {t.dtype}")
+    return 0 if t.dtype == torch.bfloat16 else 1
+
+
 def _rope(entry, rope, q, q_out, k, k_out, positions, packing, stream):
     import torch
     dtype, tokens = q.dtype, q.shape[0]
@@ -483,6 +514,90 @@ def rope_fwd(rope, q, q_out=None, k=None, k_out=None, positions=None, packing=No
 def rope_bwd(rope, dq, dq_out=None, dk=None, dk_out=None, positions=None, packing=None, stream=None):
     """The gradient with respect to rope_fwd's inputs from that of its outputs."""
     _rope(lib().rope_bwd, rope, dq, dq_out, dk, dk_out, positions, packing, stream)
+
+
+AXES_ORDERS = {"sections": 0, "cycled": 1}
+AXES_FREQUENCIES = {"shared": 0, "own": 1}
+
+
+def make_rope_axes(pairs, order="sections", frequencies="shared"):
+    """Rotary positions with several axes: pairs[i] of a head's rotated pairs turn by the position on axis i."""
+    if not 1 <= len(pairs) <= 4:
+        raise ValueError("one to four axes")
+    return RopeAxes(len(pairs), (C.c_int64 * 4)(*pairs), AXES_ORDERS[order], AXES_FREQUENCIES[frequencies])
+
+
+def _positions(axes, positions, tokens, like):
+    import torch
+    if axes is None:
+        return _flat("positions", positions, torch.int64, (tokens,), like)
+    if positions is None:
+        raise ValueError("axes need positions, [n_axes][tokens]")
+    return _flat("positions", positions, torch.int64, (axes.n_axes, tokens), like)
+
+
+def _rope_axes(entry, rope, axes, q, positions, q_out, k, k_out, packing, stream):
+    dtype, tokens, f32 = q.dtype, q.shape[0], _float_type("q", q)
+    io = _rope_io("q", q, q_out, dtype, tokens, rope.head_dim, q)
+    io_k = None if k is None else _rope_io("k", k, k_out, dtype, tokens, rope.head_dim, q)
+    _launch(entry, q, stream, rope, axes, f32, tokens, None if packing is None else _on_one_device(packing, q),
+            _positions(axes, positions, tokens, q), io, io_k)
+
+
+def rope_axes_fwd(rope, axes, q, positions, q_out=None, k=None, k_out=None, packing=None, stream=None):
+    """rope_fwd with positions [n_axes][tokens] (make_rope_axes)."""
+    _rope_axes(lib().rope_axes_fwd, rope, axes, q, positions, q_out, k, k_out, packing, stream)
+
+
+def rope_axes_bwd(rope, axes, dq, positions, dq_out=None, dk=None, dk_out=None, packing=None, stream=None):
+    """The gradient with respect to rope_axes_fwd's inputs from that of its outputs."""
+    _rope_axes(lib().rope_axes_bwd, rope, axes, dq, positions, dq_out, dk, dk_out, packing, stream)
+
+
+def _norm_gain(name, gain, dtype, d, like):
+    if gain is None:
+        raise ValueError(f"{name} is required")
+    return _flat(name, gain, dtype, (d,), like)
+
+
+def qk_norm_rope_fwd(rope, q, q_gain, q_out=None, k=None, k_gain=None, k_out=None, eps=1e-6, positions=None, axes=None,
+                     packing=None, stream=None):
+    """RMS norm of every head of q (and k), [tokens][heads][head_dim], times its gain, rotated, into q_out (k_out); in
+    place without an output.  positions as in rope_fwd, or [n_axes][tokens] with axes."""
+    dtype, tokens, d, f32 = q.dtype, q.shape[0], rope.head_dim, _float_type("q", q)
+    io = []
+    for name, x, gain, y in (("q", q, q_gain, q_out), ("k", k, k_gain, k_out)):
+        if x is not None:
+            h = _rope_io(name, x, y, dtype, tokens, d, q)
+            io.append(NormHeads(h.x, _norm_gain(name + "_gain", gain, dtype, d, q), h.y, h.heads, h.x_ld, h.y_ld))
+    _launch(lib().qk_norm_rope_fwd, q, stream, rope, axes, f32, tokens,
+            None if packing is None else _on_one_device(packing, q), _positions(axes, positions, tokens, q), eps, io[0],
+            io[1] if len(io) > 1 else None)
+
+
+def l4d_qk_norm_workspace_bytes(tokens, head_dim):
+    """Arena bytes of qk_norm_rope_bwd."""
+    b = C.c_uint64()
+    _check(lib().l4d_qk_norm_workspace_bytes(tokens, head_dim, C.byref(b)))
+    return b.value
+
+
+def qk_norm_rope_bwd(rope, q, q_gain, dq_out, dq, d_q_gain, arena, k=None, k_gain=None, dk_out=None, dk=None, d_k_gain=None,
+                     eps=1e-6, positions=None, axes=None, packing=None, stream=None):
+    """Gradients of qk_norm_rope_fwd from those of its outputs (dq_out, dk_out): dq and dk overwritten, the gains'
+    gradients (f32) added to."""
+    import torch
+    dtype, tokens, d, f32 = q.dtype, q.shape[0], rope.head_dim, _float_type("q", q)
+    io = []
+    for name, x, gain, dy, dx, dg in (("q", q, q_gain, dq_out, dq, d_q_gain), ("k", k, k_gain, dk_out, dk, d_k_gain)):
+        if x is not None:
+            h = _rope_io(name, x, dx, dtype, tokens, d, q)
+            io.append(NormHeadsGrad(h.x, _norm_gain(name + "_gain", gain, dtype, d, q), dy.data_ptr(), h.y,
+                                    _norm_gain("d_" + name + "_gain", dg, torch.float32, d, q), h.heads, h.x_ld,
+                                    _rows("d" + name + "_out", dy, dtype, x.shape, q), h.y_ld))
+    _launch(lib().qk_norm_rope_bwd, q, stream, rope, axes, f32, tokens,
+            None if packing is None else _on_one_device(packing, q), _positions(axes, positions, tokens, q), eps, io[0],
+            io[1] if len(io) > 1 else None, arena.h)
 
 
 def _attn_args(q, tensors):
@@ -571,6 +686,46 @@ def llama_layer_packed_bwd(model, par, weights, stash, dy, dx, grads, arena, pac
     _launch(lib().llama_layer_packed_bwd, dy, stream, model, par, _on_one_device(packing, dy), rope, _weights(weights),
             _peers(peers), _sends(sends), stash.h, dy.data_ptr(), dx.data_ptr(), g, arena.h)
     stash.h = None
+
+
+# ------------------------------------------------------------------ dropout and residual
+
+def _matrix(name, t, dtype, shape, like):
+    """Row stride of a [rows][cols] tensor with contiguous rows."""
+    _want(name, t, dtype, shape, like)
+    (n, cols), (ld, one) = shape, t.stride()
+    if cols > 1 and one != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    if n <= 1:
+        return cols
+    if ld < cols:
+        raise ValueError(f"the rows of {name} overlap")
+    return ld
+
+
+def _dropout_args(x, rng):
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x must be [rows][cols]")
+    f32 = _float_type("x", x)
+    return f32, x.dtype, x.shape, _flat("rng", rng, torch.int64, (2,), x)
+
+
+def dropout_add_fwd(x, residual, y, rng, p, first_row=0, stream=None):
+    """y = residual + x / (1 - p) where the mask of rng (int64 [2] on the GPU: seed, offset) keeps x, residual elsewhere
+    (residual None: 0).  x, residual, y: [rows][cols], rows first_row .. of the whole array."""
+    f32, dtype, shape, words = _dropout_args(x, rng)
+    r_ld = 0 if residual is None else _matrix("residual", residual, dtype, shape, x)
+    _launch(lib().dropout_add_fwd, x, stream, f32, *shape, x.data_ptr(), _matrix("x", x, dtype, shape, x),
+            None if residual is None else residual.data_ptr(), r_ld, y.data_ptr(), _matrix("y", y, dtype, shape, x), p, words,
+            first_row)
+
+
+def dropout_add_bwd(dy, dx, rng, p, first_row=0, stream=None):
+    """The gradient of dropout_add_fwd's x from that of its y (which is the residual's own)."""
+    f32, dtype, shape, words = _dropout_args(dy, rng)
+    _launch(lib().dropout_add_bwd, dy, stream, f32, *shape, dy.data_ptr(), _matrix("dy", dy, dtype, shape, dy),
+            dx.data_ptr(), _matrix("dx", dx, dtype, shape, dy), p, words, first_row)
 
 
 # ------------------------------------------------------------------ loss without stored logits

@@ -855,17 +855,72 @@ bool rows_meet(const RowRange& a, const RowRange& b) {
   return off < a.width || off + b.width > a.ld;
 }
 
-int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk,
-              const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, int inverse, void* stream_ptr) {
-  if (!r || !q) return fail(L4D_EINVAL, "rope and q are required");
+// f_j / 2 pi and the axis of every pair.
+int rope_axes(const l4d_rope* r, const l4d_rope_axes* x, RopeRotate* a) {
+  int rc = rope_turns(r, a->turns);
+  if (rc || !x) return rc;
+  const int64_t n = x->n_axes, pairs = r->rot_dim / 2;
+  if (n < 1 || n > 4) return fail(L4D_EINVAL, "rope axes: n_axes must lie in 1 .. 4");
+  if (x->order != L4D_AXES_SECTIONS && x->order != L4D_AXES_CYCLED) return fail(L4D_EINVAL, "rope axes: unknown order");
+  if (x->frequencies != L4D_AXES_SHARED && x->frequencies != L4D_AXES_OWN)
+    return fail(L4D_EINVAL, "rope axes: unknown frequencies");
+  int64_t sum = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    if (x->pairs[i] < 1 || x->pairs[i] > pairs) return fail(L4D_EINVAL, "rope axes: an axis without pairs, or with more than rot_dim/2");
+    sum += x->pairs[i];
+  }
+  if (sum != pairs) return fail(L4D_EINVAL, "rope axes: the pairs must add up to rot_dim/2");
+  for (int64_t i = 1; x->order == L4D_AXES_CYCLED && i < n; ++i)
+    if (i + n * (x->pairs[i] - 1) >= pairs) return fail(L4D_EINVAL, "rope axes: too many pairs of an axis to be dealt in turn");
+  double own[4][kMaxRopePairs];
+  for (int64_t i = 0; x->frequencies == L4D_AXES_OWN && i < n; ++i) {
+    l4d_rope one = *r;
+    one.rot_dim = 2 * x->pairs[i];
+    if ((rc = rope_turns(&one, own[i]))) return rc;
+  }
+  int64_t used[4] = {};
+  for (int64_t j = 0, section = 0; j < pairs; ++j) {
+    int64_t at = j % n;
+    if (x->order == L4D_AXES_CYCLED) at = j < n * x->pairs[at] ? at : 0;
+    else at = section += used[section] == x->pairs[section];
+    a->axis[j] = (uint8_t)at;
+    if (x->frequencies == L4D_AXES_OWN) a->turns[j] = own[at][used[at]];
+    ++used[at];
+  }
+  a->n_axes = (int32_t)n;
+  return L4D_OK;
+}
+
+// The checks and parameters that calls over heads share, tensors apart.
+int rope_setup(const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t tokens, const l4d_packing* pk,
+               const int64_t* positions, RopeRotate* a) {
+  if (!r) return fail(L4D_EINVAL, "rope is required");
   if (dtype != L4D_BF16 && dtype != L4D_F32) return fail(L4D_EINVAL, "rope: unknown dtype");
   if (tokens < 0 || tokens > kMaxRopeRows) return fail(L4D_EINVAL, "rope: tokens must lie in 0 .. 2^25");
   int rc;
   if (pk && (rc = check_packing(pk))) return rc;
   if (pk && pk->tokens != tokens) return fail(L4D_EINVAL, "rope: the packing is of another number of tokens");
   if (reinterpret_cast<uintptr_t>(positions) % 8) return fail(L4D_EINVAL, "rope: positions must be 8-byte aligned");
+  if (axes && !positions) return fail(L4D_EINVAL, "rope axes: positions are required");
+  if ((rc = rope_axes(r, axes, a))) return rc;
+  a->pk = pk ? device_packing(pk) : Packing{nullptr, -1, (int32_t)tokens};
+  a->positions = positions;
+  a->tokens = (int32_t)tokens;
+  a->d_h = (int32_t)r->head_dim;
+  a->rot = (int32_t)r->rot_dim;
+  a->f32 = dtype == L4D_F32;
+  a->interleaved = r->layout == L4D_ROPE_INTERLEAVED;
+  a->amplitude = (float)r->amplitude;
+  return L4D_OK;
+}
+
+int rope_call(const char* name, const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t tokens,
+              const l4d_packing* pk, const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, int inverse,
+              void* stream_ptr) {
+  if (!r || !q) return fail(L4D_EINVAL, "rope and q are required");
   RopeRotate a{};
-  if ((rc = rope_turns(r, a.turns))) return rc;
+  int rc = rope_setup(r, axes, dtype, tokens, pk, positions, &a);
+  if (rc) return rc;
   const int64_t size = dtype == L4D_F32 ? 4 : 2;
   const l4d_rope_heads* in[2] = {q, k};
   RowRange from[2], to[2];
@@ -890,17 +945,121 @@ int rope_call(const char* name, const l4d_rope* r, int dtype, int64_t tokens, co
     a.t[a.n_tensors++] = RopeHeads{t->x, t->y, t->x_ld, t->y_ld, (int32_t)t->heads};
   }
   if (tokens == 0 || (pk && pk->n_seqs == 0)) return L4D_OK;
-  a.pk = pk ? device_packing(pk) : Packing{nullptr, -1, (int32_t)tokens};
-  a.positions = positions;
-  a.tokens = (int32_t)tokens;
-  a.d_h = (int32_t)r->head_dim;
-  a.rot = (int32_t)r->rot_dim;
-  a.f32 = dtype == L4D_F32;
-  a.interleaved = r->layout == L4D_ROPE_INTERLEAVED;
   a.inverse = inverse;
-  a.amplitude = (float)r->amplitude;
   hipStream_t s = static_cast<hipStream_t>(stream_ptr);
   return launch(name, s, [&] { return rope_rotate(a, s); });
+}
+
+// ------------------------------------------------------------ norm and rotation of heads
+
+// One tensor of a call: its arrays, the last one the output; g and d_g of head_dim elements.
+struct NormTensor {
+  const void *x, *dy;
+  void* out;
+  const void* gain;
+  float* d_gain;
+  int64_t heads, x_ld, dy_ld, out_ld;
+};
+int norm_call(const char* name, const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t tokens, const l4d_packing* pk,
+              const int64_t* positions, float eps, const NormTensor* in, int n, bool backward, l4d_arena* A, void* stream_ptr) {
+  QkNorm p{};
+  int rc = rope_setup(r, axes, dtype, tokens, pk, positions, &p.r);
+  if (rc) return rc;
+  if (r->head_dim % 2) return fail(L4D_EINVAL, "qk_norm: head_dim must be even");
+  if (!(eps >= 1e-30f) || !std::isfinite(eps)) return fail(L4D_EINVAL, "qk_norm: eps must be finite and at least 1e-30");
+  if (tokens == 0) return L4D_OK;                    // an empty array may have no address
+  const uint64_t size = dtype == L4D_F32 ? 4 : 2, d = (uint64_t)r->head_dim, rows = (uint64_t)tokens;
+  struct Array { RowRange at; int tensor; };
+  Array ins[6], outs[4];
+  int n_in = 0, n_out = 0;
+  for (int i = 0; i < n; ++i) {
+    const NormTensor& t = in[i];
+    if (!t.x || !t.out || !t.gain || (backward && (!t.dy || !t.d_gain))) return fail(L4D_EINVAL, "qk_norm: an array is NULL");
+    if (t.heads < 1 || t.heads > 8192) return fail(L4D_EINVAL, "qk_norm: heads must lie in 1 .. 8192");
+    const int64_t cols = t.heads * r->head_dim, most = (int64_t)1 << 31;
+    if (t.x_ld < cols || t.out_ld < cols || t.x_ld > most || t.out_ld > most || (backward && (t.dy_ld < cols || t.dy_ld > most)))
+      return fail(L4D_EINVAL, "qk_norm: a row stride is shorter than the heads, or above 2^31");
+    const auto off = [&](const void* x, uint64_t by) { return reinterpret_cast<uintptr_t>(x) % by != 0; };
+    if (off(t.x, size) || off(t.out, size) || off(t.gain, size) || (backward && (off(t.dy, size) || off(t.d_gain, 4))))
+      return fail(L4D_EINVAL, "qk_norm: an array is misaligned");
+    const auto range = [&](const void* x, int64_t ld) {
+      return RowRange{reinterpret_cast<uintptr_t>(x), cols * size, ld * size, rows};
+    };
+    ins[n_in++] = {range(t.x, t.x_ld), i};
+    ins[n_in++] = {RowRange{reinterpret_cast<uintptr_t>(t.gain), d * size, d * size, 1}, -1};
+    if (backward) {
+      ins[n_in++] = {range(t.dy, t.dy_ld), i};
+      outs[n_out++] = {RowRange{reinterpret_cast<uintptr_t>(t.d_gain), d * 4, d * 4, 1}, -1};
+    }
+    outs[n_out++] = {range(t.out, t.out_ld), i};
+    p.r.t[i] = RopeHeads{t.x, t.out, t.x_ld, t.out_ld, (int32_t)t.heads};
+    p.gain[i] = t.gain;
+    p.dy[i] = t.dy;
+    p.dy_ld[i] = t.dy_ld;
+    p.d_gain[i] = t.d_gain;
+  }
+  // An output may lie exactly on an input of its own tensor; nothing else it writes may be read or written twice.
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < n_in; ++j) {
+      const RowRange &a = outs[i].at, &b = ins[j].at;
+      if (outs[i].tensor >= 0 && outs[i].tensor == ins[j].tensor && a.p == b.p && a.ld == b.ld) continue;
+      if (rows_meet(a, b)) return fail(L4D_EINVAL, "qk_norm: an output overlaps an input");
+    }
+    for (int j = 0; j < i; ++j)
+      if (rows_meet(outs[i].at, outs[j].at)) return fail(L4D_EINVAL, "qk_norm: two outputs overlap");
+  }
+  if (backward && !A) return fail(L4D_EINVAL, "arena is required");
+  if (pk && pk->n_seqs == 0) return L4D_OK;
+  p.r.n_tensors = n;
+  p.eps = eps;
+  p.backward = backward;
+  Workspace ws;
+  if (backward) {
+    if ((rc = take_ws(A, align_up((uint64_t)qk_norm_parts(tokens) * 2 * d * 4), ws))) return rc;
+    p.partial = reinterpret_cast<float*>(A->base + ws.off);
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
+  return launch(name, s, [&] { return qk_norm_rope(p, s); });
+}
+
+// ------------------------------------------------------------ dropout and residual
+
+int dropout_call(const char* name, int dtype, int64_t rows, int64_t cols, const void* x, int64_t x_ld, const void* res,
+                 int64_t r_ld, void* y, int64_t y_ld, double p, const int64_t* rng, int64_t first_row, void* stream_ptr) {
+  if (dtype != L4D_BF16 && dtype != L4D_F32) return fail(L4D_EINVAL, "dropout: unknown dtype");
+  if (rows < 0 || rows > (int64_t)1 << 31 || cols < 0 || cols > (int64_t)1 << 24 || rows * cols > (int64_t)1 << 34)
+    return fail(L4D_EINVAL, "dropout: rows must lie in 0 .. 2^31, cols in 0 .. 2^24, their product in 0 .. 2^34");
+  if (first_row < 0 || first_row > (int64_t)1 << 38) return fail(L4D_EINVAL, "dropout: first_row must lie in 0 .. 2^38");
+  if (!(p >= 0.0) || std::nearbyint(p * 4294967296.0) > 4294967295.0)
+    return fail(L4D_EINVAL, "dropout: p must lie in [0, 1)");
+  if (rows == 0 || cols == 0) return L4D_OK;         // an empty array may have no address
+  if (!x || !y || !rng) return fail(L4D_EINVAL, "dropout: an array is NULL");
+  if (reinterpret_cast<uintptr_t>(rng) % 8) return fail(L4D_EINVAL, "dropout: rng must be 8-byte aligned");
+  const uint64_t size = dtype == L4D_F32 ? 4 : 2;
+  const void* arrays[3] = {x, y, res};
+  const int64_t lds[3] = {x_ld, y_ld, r_ld};
+  RowRange at[3];
+  for (int i = 0; i < (res ? 3 : 2); ++i) {
+    if (reinterpret_cast<uintptr_t>(arrays[i]) % size) return fail(L4D_EINVAL, "dropout: an array is misaligned");
+    if (lds[i] < cols || lds[i] > (int64_t)1 << 31)
+      return fail(L4D_EINVAL, "dropout: a row stride is shorter than the columns, or above 2^31");
+    at[i] = RowRange{reinterpret_cast<uintptr_t>(arrays[i]), cols * size, lds[i] * size, (uint64_t)rows};
+  }
+  const RowRange words{reinterpret_cast<uintptr_t>(rng), 16, 16, 1};
+  if (rows_meet(at[1], words)) return fail(L4D_EINVAL, "dropout: the output overlaps rng");
+  for (int i = 0; i < (res ? 3 : 2); i += 2)
+    if (!(at[1].p == at[i].p && at[1].ld == at[i].ld) && rows_meet(at[1], at[i]))
+      return fail(L4D_EINVAL, "dropout: input and output overlap");
+  DropoutAdd a{};
+  a.x = x, a.residual = res, a.y = y;
+  a.rows = rows, a.cols = cols, a.x_ld = x_ld, a.r_ld = r_ld, a.y_ld = y_ld;
+  a.rng = rng;
+  a.first = (uint64_t)first_row * (uint64_t)cols;
+  a.threshold = (uint32_t)std::nearbyint(p * 4294967296.0);
+  a.scale = (float)(1.0 / (1.0 - p));
+  a.f32 = dtype == L4D_F32;
+  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
+  return launch(name, s, [&] { return dropout_add(a, s); });
 }
 }  // namespace
 
@@ -1619,12 +1778,65 @@ extern "C" int lm_head_bwd(const l4d_model* m, const l4d_parallel* p, const void
 
 extern "C" int rope_fwd(const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk, const int64_t* positions,
                         const l4d_rope_heads* q, const l4d_rope_heads* k, void* stream_ptr) {
-  return rope_call("rope_fwd", r, dtype, tokens, pk, positions, q, k, 0, stream_ptr);
+  return rope_call("rope_fwd", r, nullptr, dtype, tokens, pk, positions, q, k, 0, stream_ptr);
 }
 
 extern "C" int rope_bwd(const l4d_rope* r, int dtype, int64_t tokens, const l4d_packing* pk, const int64_t* positions,
                         const l4d_rope_heads* q, const l4d_rope_heads* k, void* stream_ptr) {
-  return rope_call("rope_bwd", r, dtype, tokens, pk, positions, q, k, 1, stream_ptr);
+  return rope_call("rope_bwd", r, nullptr, dtype, tokens, pk, positions, q, k, 1, stream_ptr);
+}
+
+extern "C" int rope_axes_fwd(const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t tokens, const l4d_packing* pk,
+                             const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, void* stream_ptr) {
+  if (!axes) return fail(L4D_EINVAL, "axes is required");
+  return rope_call("rope_axes_fwd", r, axes, dtype, tokens, pk, positions, q, k, 0, stream_ptr);
+}
+extern "C" int rope_axes_bwd(const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t tokens, const l4d_packing* pk,
+                             const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, void* stream_ptr) {
+  if (!axes) return fail(L4D_EINVAL, "axes is required");
+  return rope_call("rope_axes_bwd", r, axes, dtype, tokens, pk, positions, q, k, 1, stream_ptr);
+}
+
+// ------------------------------------------------------------ norm and rotation of heads
+
+extern "C" int qk_norm_rope_fwd(const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t tokens,
+                                const l4d_packing* pk, const int64_t* positions, float eps, const l4d_norm_heads* q,
+                                const l4d_norm_heads* k, void* stream_ptr) {
+  if (!q) return fail(L4D_EINVAL, "q is required");
+  NormTensor t[2];
+  int n = 0;
+  for (const l4d_norm_heads* h : {q, k})
+    if (h) t[n++] = NormTensor{h->x, nullptr, h->y, h->gain, nullptr, h->heads, h->x_ld, 0, h->y_ld};
+  return norm_call("qk_norm_rope_fwd", r, axes, dtype, tokens, pk, positions, eps, t, n, false, nullptr, stream_ptr);
+}
+extern "C" int l4d_qk_norm_workspace_bytes(int64_t tokens, int64_t head_dim, uint64_t* bytes) {
+  if (tokens < 0 || tokens > kMaxRopeRows) return fail(L4D_EINVAL, "rope: tokens must lie in 0 .. 2^25");
+  if (head_dim < 2 || head_dim > 2 * kMaxRopePairs) return fail(L4D_EINVAL, "rope: head_dim must lie in 2 .. 512");
+  if (bytes) *bytes = align_up((uint64_t)qk_norm_parts(tokens) * 2 * head_dim * 4);
+  return L4D_OK;
+}
+extern "C" int qk_norm_rope_bwd(const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t tokens,
+                                const l4d_packing* pk, const int64_t* positions, float eps, const l4d_norm_heads_grad* q,
+                                const l4d_norm_heads_grad* k, l4d_arena* A, void* stream_ptr) {
+  if (!q) return fail(L4D_EINVAL, "q is required");
+  NormTensor t[2];
+  int n = 0;
+  for (const l4d_norm_heads_grad* h : {q, k})
+    if (h) t[n++] = NormTensor{h->x, h->dy, h->dx, h->gain, h->d_gain, h->heads, h->x_ld, h->dy_ld, h->dx_ld};
+  return norm_call("qk_norm_rope_bwd", r, axes, dtype, tokens, pk, positions, eps, t, n, true, A, stream_ptr);
+}
+
+// ------------------------------------------------------------ dropout and residual
+
+extern "C" int dropout_add_fwd(int dtype, int64_t rows, int64_t cols, const void* x, int64_t x_ld, const void* residual,
+                               int64_t residual_ld, void* y, int64_t y_ld, double p, const int64_t* rng, int64_t first_row,
+                               void* stream_ptr) {
+  return dropout_call("dropout_add_fwd", dtype, rows, cols, x, x_ld, residual, residual_ld, y, y_ld, p, rng, first_row,
+                      stream_ptr);
+}
+extern "C" int dropout_add_bwd(int dtype, int64_t rows, int64_t cols, const void* dy, int64_t dy_ld, void* dx, int64_t dx_ld,
+                               double p, const int64_t* rng, int64_t first_row, void* stream_ptr) {
+  return dropout_call("dropout_add_bwd", dtype, rows, cols, dy, dy_ld, nullptr, 0, dx, dx_ld, p, rng, first_row, stream_ptr);
 }
 
 // ------------------------------------------------------------ packed attention

@@ -313,7 +313,7 @@ struct RopeHeads {          // one tensor [tokens][heads][d_h] (element strides)
 };
 struct RopeRotate {
   Packing pk;
-  const int64_t* positions; // null: the distance from the document's first row
+  const int64_t* positions; // null: the distance from the document's first row; with axes [n_axes][tokens]
   RopeHeads t[2];
   int32_t n_tensors, tokens;
   int32_t d_h, rot;
@@ -324,11 +324,45 @@ struct RopeRotate {
   int32_t units[2], first_rest[2];   // units per head of each tensor; those from first_rest on are copied
   uint32_t magic[2];             // ceil(2^32 / units)
   double turns[kMaxRopePairs];   // f_j / 2 pi
+  int32_t n_axes;                // 0: one position for all pairs
+  uint8_t axis[kMaxRopePairs];   // the axis whose position turns pair j
 };
 hipError_t rope_rotate(const RopeRotate& p, hipStream_t stream);
 // tab[row][j] = A (cos, sin) of pair j at the row's distance from its document's start
 // (0 for rows of no document): the table of the layer's QKV epilogue.
 hipError_t rope_table(const RopeRotate& p, float2* tab, hipStream_t stream);
+// Norm of every head (t[i].x) and its rotation into t[i].y; backward: dx into t[i].y from x and
+// dy, and the gains' gradients added to d_gain.
+constexpr int kQkNormWaves = 8, kQkNormParts = 512;
+struct QkNorm {
+  RopeRotate r;
+  const void* gain[2];       // [d_h] of the tensors' type
+  float eps;
+  int32_t backward;
+  const void* dy[2];
+  int64_t dy_ld[2];
+  float* d_gain[2];          // [d_h], +=
+  float* partial;            // [qk_norm_parts(tokens)][2][d_h]
+  // set by qk_norm_rope
+  int32_t group;             // lanes per head
+  float inv_d;
+};
+int32_t qk_norm_parts(int64_t tokens);
+hipError_t qk_norm_rope(const QkNorm& p, hipStream_t stream);
+
+// y = residual + keep x scale (no residual: keep x scale), see dropout_kernel.
+struct DropoutAdd {
+  const void *x, *residual;
+  void* y;
+  int64_t rows, cols, x_ld, r_ld, y_ld;
+  const int64_t* rng;        // seed, offset
+  uint64_t first;            // place of element (0, 0) in the whole array
+  uint32_t threshold;        // kept: words of at least this
+  float scale;
+  int32_t f32;
+};
+hipError_t dropout_add(const DropoutAdd& p, hipStream_t stream);
+
 // Zeroes the first `cols` columns (a multiple of 8) of the rows of x (row stride ld)
 // that belong to no document.
 hipError_t clear_outside(const Packing& pk, uint16_t* x, int64_t ld, int64_t cols, hipStream_t stream);

@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(256) clear_outside_kernel(Packing pk, uint16_t
   }
 }
 
-template <typename T, int V, bool INTER>
+template <typename T, int V, bool INTER, bool AXES>
 __global__ void __launch_bounds__(256) rope_rotate_kernel(RopeRotate p) {
   __shared__ __attribute__((aligned(16))) float2 table[4][kMaxRopePairs];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -170,10 +170,11 @@ __global__ void __launch_bounds__(256) rope_rotate_kernel(RopeRotate p) {
     if (row >= s.hi) return;
     pos = row - s.lo;
   }
-  if (p.positions) pos = p.positions[row];
+  if (!AXES && p.positions) pos = p.positions[row];
   const int pairs = p.rot / 2;
   float2* tab = table[wave];
   for (int j = lane; j < pairs; j += 64) {
+    if (AXES) pos = p.positions[static_cast<int64_t>(p.axis[j]) * p.tokens + row];
     float2 cs = rope_angle(p, pos, j);
     if (p.inverse) cs.y = -cs.y;
     tab[j] = cs;
@@ -1152,12 +1153,12 @@ hipError_t embed_bwd(const int64_t* ids, uint64_t* keys, RowSrc dy, int64_t v0, 
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool AXES>
 static hipError_t rope_launch(const RopeRotate& p, bool vec, dim3 grid, hipStream_t stream) {
-  if (vec && p.interleaved) hipLaunchKernelGGL((rope_rotate_kernel<T, 8, true>), grid, dim3(256), 0, stream, p);
-  else if (vec) hipLaunchKernelGGL((rope_rotate_kernel<T, 8, false>), grid, dim3(256), 0, stream, p);
-  else if (p.interleaved) hipLaunchKernelGGL((rope_rotate_kernel<T, 1, true>), grid, dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((rope_rotate_kernel<T, 1, false>), grid, dim3(256), 0, stream, p);
+  if (vec && p.interleaved) hipLaunchKernelGGL((rope_rotate_kernel<T, 8, true, AXES>), grid, dim3(256), 0, stream, p);
+  else if (vec) hipLaunchKernelGGL((rope_rotate_kernel<T, 8, false, AXES>), grid, dim3(256), 0, stream, p);
+  else if (p.interleaved) hipLaunchKernelGGL((rope_rotate_kernel<T, 1, true, AXES>), grid, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((rope_rotate_kernel<T, 1, false, AXES>), grid, dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 hipError_t rope_rotate(const RopeRotate& params, hipStream_t stream) {
@@ -1183,7 +1184,8 @@ hipError_t rope_rotate(const RopeRotate& params, hipStream_t stream) {
   p.parts = 1;
   while (static_cast<int64_t>(p.tokens) * p.parts * 2 <= 8192 && most > 64 * p.parts) p.parts *= 2;
   const dim3 grid(static_cast<unsigned>((p.tokens + 3) / 4), static_cast<unsigned>(p.parts));
-  return p.f32 ? rope_launch<float>(p, vec, grid, stream) : rope_launch<uint16_t>(p, vec, grid, stream);
+  if (p.n_axes) return p.f32 ? rope_launch<float, true>(p, vec, grid, stream) : rope_launch<uint16_t, true>(p, vec, grid, stream);
+  return p.f32 ? rope_launch<float, false>(p, vec, grid, stream) : rope_launch<uint16_t, false>(p, vec, grid, stream);
 }
 
 hipError_t rope_table(const RopeRotate& p, float2* tab, hipStream_t stream) {
@@ -1211,5 +1213,7 @@ hipError_t loss_finish_grad(const LossTargets& p, hipStream_t stream) {
   hipLaunchKernelGGL(loss_finish_grad_kernel, dim3(static_cast<unsigned>(p.n), (p.h + 2047) / 2048), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
+
+#include "heads.h"
 
 }  // namespace l4d

@@ -1,0 +1,374 @@
+"""Norms of query and key heads with the rotation in the same pass, and rotary positions with
+several axes, against plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+import paper_2411_06465_amd as L
+from packed_common import F, U, inside, rope_frequencies, rope_plain, starts_of
+
+pytestmark = pytest.mark.gpu
+BF16, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+BASE = 500000.0
+
+
+def step_of(dtype):
+    return U if dtype == BF16 else F
+
+
+def axes_frequencies(pairs, order, own, rot, **scaling):
+    """(axis, frequency) of every pair."""
+    n, out, used = len(pairs), [], [0] * len(pairs)
+    shared = rope_frequencies(rot, BASE, **scaling)
+    mine = [rope_frequencies(2 * m, BASE, **scaling) for m in pairs]
+    owner = [a for a, m in enumerate(pairs) for _ in range(m)]
+    for j in range(rot // 2):
+        a = owner[j] if order == "sections" else (j % n if j // n < pairs[j % n] else 0)
+        out.append((a, mine[a][used[a]] if own else shared[j]))
+        used[a] += 1
+    assert used == list(pairs)
+    return out
+
+
+def turn(x, table, pos, rot, layout, amplitude=1.0, inverse=False):
+    """Rotation of x [n][heads][d] (float64), pair j by pos[axis][row] times its frequency -> (y, bound).
+
+    Both sides form angles in 64 bits.  A frequency base^(-m) comes from exponentials and powers of
+    arguments up to log(base) < 14, whose rounding (2^-53 of the argument, twice) is that many times
+    2^-53 of the result: with the products around it at most 40 x 2^-53 of the angle between the
+    two.  Far positions (2^40) make that 5e-3 of a radian: it is part of the bound."""
+    y, bound = torch.empty_like(x), torch.zeros_like(x)
+    y.copy_(x)
+    for a in sorted({a for a, _ in table}):
+        # every axis turns all pairs; its own are taken
+        one, e = rope_plain(x, pos[a], rot, layout, [f for _, f in table], amplitude, inverse)
+        for j, (b, _) in enumerate(table):
+            if a == b:
+                i0, i1 = (j, j + rot // 2) if layout == "half" else (2 * j, 2 * j + 1)
+                far = 40 * 2.0 ** -53 * (pos[a].to(F64).abs() * table[j][1])[:, None]
+                far = amplitude * far * (x[..., i0].abs() + x[..., i1].abs())
+                for i in (i0, i1):
+                    y[..., i], bound[..., i] = one[..., i], e[..., i] + far
+    return y, bound
+
+
+def pair_sum(e, rot, layout):
+    """|e| of a pair's two elements, for both of them; 0 behind the rotated part's own."""
+    out = e.clone()
+    half = rot // 2
+    i0, i1 = (slice(0, half), slice(half, rot)) if layout == "half" else (slice(0, rot, 2), slice(1, rot, 2))
+    out[..., i0] = out[..., i1] = e[..., i0] + e[..., i1]
+    return out
+
+
+def norm_plain(x, gain, table, pos, rot, layout, eps, dy=None, amplitude=1.0):
+    """x, dy [n][heads][d], gain [d] float64 -> results and bounds of an fp32 computation before its rounding."""
+    n, heads, d = x.shape
+    r = (x.square().mean(-1, keepdim=True) + eps).rsqrt()
+    e_r = ((d + 4) / 2 + 2) * F                                      # relative: the sum, its root
+    y, e_turn = turn(x * r * gain, table, pos, rot, layout, amplitude)
+    e_n = (e_r + 3 * F) * (x * r * gain).abs()
+    out = dict(y=y, _y=e_turn + max(1.0, amplitude) * pair_sum(e_n, rot, layout))
+    if dy is None:
+        return out
+    dn, e_dn = turn(dy, table, pos, rot, layout, amplitude, True)
+    t = dn * gain * x
+    c = r ** 3 * t.mean(-1, keepdim=True)
+    e_c = r ** 3 / d * ((e_dn * (gain * x).abs()).sum(-1, keepdim=True) + (d + 4) * F * t.abs().sum(-1, keepdim=True))
+    e_c = e_c + (3 * e_r + 6 * F) * c.abs()
+    out["dx"] = r * gain * dn - c * x
+    out["_dx"] = r * gain.abs() * e_dn + e_c * x.abs() + (e_r + 6 * F) * ((r * gain * dn).abs() + (c * x).abs())
+    g = dn * x * r
+    out["dg"] = g.sum((0, 1))
+    out["_dg"] = (e_dn * (x * r).abs() + (e_r + 3 * F + n * heads * F) * g.abs()).sum((0, 1)) + F * out["dg"].abs()
+    return out
+
+
+def rows_inside(starts, n):
+    rows = torch.zeros(n, dtype=torch.bool)
+    rows[starts[0]:max(starts[0], starts[-1])] = True
+    return rows
+
+
+def document_positions(starts, n):
+    pos = torch.zeros(n, dtype=torch.int64)
+    for lo, hi in zip(starts[:-1], starts[1:]):
+        pos[lo:hi] = torch.arange(hi - lo)
+    return pos
+
+
+def make(n, heads, kv, d, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+
+    def t(*shape, mean=0.0, std=1.0):
+        return (mean + std * torch.randn(shape, generator=g)).to(dtype)
+
+    return dict(q=t(n, heads, d), k=t(n, kv, d), dq=t(n, heads, d), dk=t(n, kv, d), gq=t(d, mean=1.0, std=0.2),
+                gk=t(d, mean=1.0, std=0.2), axes=torch.randint(-5000, 1 << 40, (4, n), generator=g))
+
+
+def arena(n, d):
+    size = L.l4d_qk_norm_workspace_bytes(n, d) + 256
+    return L.Arena.on(torch.full((size,), 0xff, dtype=torch.uint8, device="cuda"))
+
+
+NORMS = [  # lens, first, tail, heads, kv heads, d, rot, layout, dtype, pairs of axes
+    ([1], 0, 0, 1, 1, 128, 128, "half", BF16, None),
+    ([3, 0, 5], 2, 4, 4, 2, 64, 64, "half", BF16, None),
+    ([40, 33], 0, 7, 32, 8, 128, 128, "half", BF16, None),
+    ([40, 33], 0, 7, 9, 3, 128, 64, "interleaved", BF16, None),
+    ([50], 3, 0, 5, 5, 64, 32, "half", F32, None),
+    ([21, 30], 0, 0, 7, 1, 128, 128, "interleaved", F32, (20, 24, 20)),
+    ([70], 0, 1, 6, 2, 256, 256, "half", BF16, (1, 127)),
+    ([20], 0, 1, 3, 2, 512, 512, "half", F32, None),
+    ([20], 0, 1, 3, 2, 512, 16, "interleaved", BF16, None),
+    ([60], 1, 1, 4, 2, 80, 80, "half", BF16, None),              # a head of five lanes among eight
+    ([60], 1, 1, 4, 2, 96, 32, "half", F32, (8, 8)),
+    ([60], 1, 1, 3, 1, 16, 16, "interleaved", BF16, None),       # one lane a head
+    ([60], 0, 1, 3, 1, 50, 26, "half", BF16, None),              # no whole vectors
+    ([60], 0, 1, 3, 1, 510, 510, "half", F32, (100, 100, 55)),
+    ([7, 9], 0, 1, 2, 1, 2, 2, "interleaved", F32, None),
+    ([5000], 10, 20, 2, 1, 64, 64, "half", BF16, None),          # more rows than waves of the backward
+]
+
+
+@pytest.mark.parametrize("lens,first,tail,heads,kv,d,rot,layout,dtype,pairs", NORMS)
+def test_norm_matches_the_plain_form(lens, first, tail, heads, kv, d, rot, layout, dtype, pairs):
+    starts, eps = starts_of(lens, first), 1e-6
+    n = starts[-1] + tail
+    x = make(n, heads, kv, d, dtype, n + d)
+    inside_rows = rows_inside(starts, n)
+    for t in ("q", "k", "dq", "dk"):
+        x[t][~inside_rows] = math.nan                # rows of no document: nothing of them may be used
+    pk = L.make_packing(torch.tensor(starts, device="cuda"), n)
+    rope = L.make_rope(d, rot, layout, BASE)
+    axes, pos, given = None, document_positions(starts, n)[None], None
+    table = [(0, f) for f in rope_frequencies(rot, BASE)]
+    if pairs:
+        axes, pos = L.make_rope_axes(pairs), x["axes"][:len(pairs)].contiguous()
+        given, table = pos.cuda(), axes_frequencies(pairs, "sections", False, rot)
+    c = {t: v.cuda() for t, v in x.items()}
+    y = {t: torch.full_like(c[t], 7.0) for t in ("q", "k")}
+    dx = {t: torch.full_like(c[t], 7.0) for t in ("q", "k")}
+    dg = {t: torch.full((d,), 3.0, device="cuda") for t in ("q", "k")}
+    where = dict(eps=eps, positions=given, axes=axes, packing=pk)
+    L.qk_norm_rope_fwd(rope, c["q"], c["gq"], y["q"], c["k"], c["gk"], y["k"], **where)
+    L.qk_norm_rope_bwd(rope, c["q"], c["gq"], c["dq"], dx["q"], dg["q"], arena(n, d), c["k"], c["gk"], c["dk"], dx["k"],
+                       dg["k"], **where)
+    at = inside_rows
+    for t, g in (("q", "gq"), ("k", "gk")):
+        want = norm_plain(x[t][at].double(), x[g].double(), table, pos[:, at], rot, layout, eps, x["d" + t][at].double())
+        s = step_of(dtype)
+        inside(t, y[t].cpu()[at], want["y"], (1 + s) * want["_y"] + s * want["y"].abs())
+        inside("d" + t, dx[t].cpu()[at], want["dx"], (1 + s) * want["_dx"] + s * want["dx"].abs())
+        inside("gain " + t, dg[t].cpu(), 3.0 + want["dg"], want["_dg"] + 4 * F * (3.0 + want["dg"].abs()))
+        assert bool((y[t].cpu()[~at] == 7.0).all()) and bool((dx[t].cpu()[~at] == 7.0).all())
+
+
+def test_norm_of_one_tensor_without_a_packing_given_positions():
+    n, d = 37, 128
+    x = make(n, 6, 1, d, BF16, 3)
+    pos = x["axes"][0].contiguous()
+    c = {t: v.cuda() for t, v in x.items()}
+    rope = L.make_rope(d, 64, "half", BASE, "linear", factor=4.0, amplitude=1.25)
+    y, dx, dg = torch.zeros_like(c["q"]), torch.zeros_like(c["q"]), torch.zeros(d, device="cuda")
+    L.qk_norm_rope_fwd(rope, c["q"], c["gq"], y, eps=1e-3, positions=pos.cuda())
+    L.qk_norm_rope_bwd(rope, c["q"], c["gq"], c["dq"], dx, dg, arena(n, d), eps=1e-3, positions=pos.cuda())
+    table = [(0, f) for f in rope_frequencies(64, BASE, "linear", 4.0)]
+    want = norm_plain(x["q"].double(), x["gq"].double(), table, pos[None], 64, "half", 1e-3, x["dq"].double(), 1.25)
+    inside("y", y.cpu(), want["y"], (1 + U) * want["_y"] + U * want["y"].abs())
+    inside("dx", dx.cpu(), want["dx"], (1 + U) * want["_dx"] + U * want["dx"].abs())
+    inside("dg", dg.cpu(), want["dg"], want["_dg"])
+
+
+def test_norm_gradients_against_differences():
+    """Directional differences of sum(y dy) of the 64-bit form, in x and in the gain."""
+    n, heads, d, eps, h = 19, 3, 64, 1e-5, 1e-6
+    x = make(n, heads, 1, d, F32, 8)
+    table, pos = [(0, f) for f in rope_frequencies(d, BASE)], torch.arange(n)[None]
+    c = {t: v.cuda() for t, v in x.items()}
+    dx, dg = torch.zeros_like(c["q"]), torch.zeros(d, device="cuda")
+    L.qk_norm_rope_bwd(L.make_rope(d, base=BASE), c["q"], c["gq"], c["dq"], dx, dg, arena(n, d), eps=eps)
+    for name, got in (("q", dx), ("gq", dg)):
+        way = torch.randn(x[name].shape, generator=torch.Generator().manual_seed(1), dtype=F64)
+        val = []
+        for s in (h, -h):
+            y = {t: x[t].double() for t in ("q", "gq")}
+            y[name] = y[name] + s * way
+            val.append(float((norm_plain(y["q"], y["gq"], table, pos, d, "half", eps)["y"] * x["dq"].double()).sum()))
+        slope = (val[0] - val[1]) / (2 * h)
+        mine = float((got.cpu().double() * way).sum())
+        # fp32 gradients: (d + 10) F relative; the difference: h^2 and 1e-16/h of the sum's size
+        assert abs(mine - slope) <= 1e-5 * float((got.cpu().double().abs() * way.abs()).sum()), (name, mine, slope)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_in_place_and_in_columns_of_a_fused_array(dtype):
+    """q and k as columns of [rows][(a + 2 g) d], the outputs in their place."""
+    n, a, g, d = 75, 6, 2, 64
+    gen = torch.Generator().manual_seed(1)
+    qkv, dqkv = ((torch.randn((n, (a + 2 * g) * d), generator=gen)).to(dtype).cuda() for _ in range(2))
+    gain = [torch.randn((d,), generator=gen).to(dtype).cuda() for _ in range(2)]
+    rope, pk = L.make_rope(d), L.make_packing(torch.tensor([0, 30, 70], device="cuda"), n)
+
+    def cols(t):
+        return [t[:, i * d:j * d].unflatten(1, (j - i, d)) for i, j in ((0, a), (a, a + g))]
+
+    apart = [t.contiguous() for t in cols(qkv)]
+    y = [torch.empty_like(t).copy_(t) for t in apart]
+    L.qk_norm_rope_fwd(rope, apart[0], gain[0], y[0], apart[1], gain[1], y[1], packing=pk)
+    dy = [t.contiguous() for t in cols(dqkv)]
+    dx, dg = [t.clone() for t in dy], [torch.zeros(d, device="cuda") for _ in range(2)]
+    L.qk_norm_rope_bwd(rope, apart[0], gain[0], dy[0], dx[0], dg[0], arena(n, d), apart[1], gain[1], dy[1], dx[1], dg[1],
+                       packing=pk)
+    here, q, k = dqkv.clone(), *cols(qkv)
+    dgh = [torch.zeros(d, device="cuda") for _ in range(2)]
+    hq, hk = cols(here)
+    L.qk_norm_rope_bwd(rope, q, gain[0], hq, hq, dgh[0], arena(n, d), k, gain[1], hk, hk, dgh[1], packing=pk)
+    fused = qkv.clone()
+    q, k = cols(fused)
+    L.qk_norm_rope_fwd(rope, q, gain[0], None, k, gain[1], None, packing=pk)
+    for i in range(2):
+        assert torch.equal(cols(fused)[i], y[i]) and torch.equal(cols(here)[i], dx[i]) and torch.equal(dgh[i], dg[i])
+    assert torch.equal(fused[:, (a + g) * d:], qkv[:, (a + g) * d:])
+
+
+def test_norm_of_vectors_and_of_single_elements_agree():
+    """An array that starts off a 16-byte border takes the path of single elements."""
+    n, a, d = 33, 5, 128
+    gen = torch.Generator().manual_seed(1)
+    x, dy = (torch.randn((n, a, d), generator=gen).cuda() for _ in range(2))
+    gain = torch.randn(d, generator=gen).cuda()
+    rope = L.make_rope(d)
+    out = []
+    for shift in (0, 1):
+        def off(t):
+            flat = torch.zeros(t.numel() + shift, device="cuda")[shift:].view(t.shape)
+            return flat.copy_(t)
+        y, dx, dg = off(torch.zeros_like(x)), off(torch.zeros_like(x)), torch.zeros(d, device="cuda")
+        L.qk_norm_rope_fwd(rope, off(x), gain, y)
+        L.qk_norm_rope_bwd(rope, off(x), gain, off(dy), dx, dg, arena(n, d))
+        out.append((y, dx, dg))
+    for p, q in zip(*out):
+        # the sums over a head run in another order: (d + 10) F of the largest terms
+        assert float((p - q).abs().max()) <= 2 * (d + 10) * F * float(p.abs().max())
+
+
+def test_norm_of_extreme_rows():
+    """A row of zeros, one of infinities, one of the largest numbers: no other row changes."""
+    n, a, d = 20, 4, 128
+    x = make(n, a, 1, d, BF16, 5)["q"].cuda()
+    gain = torch.ones(d, dtype=BF16, device="cuda")
+    rope = L.make_rope(d)
+    y, z = torch.zeros_like(x), torch.zeros_like(x)
+    L.qk_norm_rope_fwd(rope, x, gain, y)
+    for row, v in ((3, 0.0), (5, math.inf), (7, math.nan), (9, torch.finfo(BF16).max)):
+        x[row] = v
+    L.qk_norm_rope_fwd(rope, x, gain, z)
+    keep = [i for i in range(n) if i not in (3, 5, 7, 9)]
+    assert torch.equal(y[keep], z[keep]) and bool((z[3] == 0).all())
+
+
+AXES = [  # lens, tail, heads, kv heads, d, layout, dtype, pairs, order, own frequencies
+    ([40, 33], 7, 32, 8, 128, "half", BF16, (16, 24, 24), "sections", False),
+    ([40, 33], 7, 4, 1, 128, "half", BF16, (24, 20, 20), "cycled", False),
+    ([60], 0, 3, 3, 64, "interleaved", F32, (16, 16), "sections", True),
+    ([60], 2, 3, 3, 64, "half", F32, (10, 8, 8, 6), "cycled", True),
+    ([60], 2, 3, 1, 80, "half", BF16, (40,), "cycled", False),
+    ([60], 2, 3, 1, 100, "interleaved", BF16, (1, 2, 3, 4), "sections", True),      # part of a head, no whole vectors
+    ([60], 2, 2, 1, 64, "half", F32, (2, 1, 1), "cycled", False),
+    ([1], 0, 1, 1, 512, "half", BF16, (128, 64, 64), "sections", False),
+]
+
+
+@pytest.mark.parametrize("inverse", [False, True])
+@pytest.mark.parametrize("lens,tail,heads,kv,d,layout,dtype,pairs,order,own", AXES)
+def test_axes_match_the_plain_form(lens, tail, heads, kv, d, layout, dtype, pairs, order, own, inverse):
+    starts, rot = starts_of(lens, 2), 2 * sum(pairs)
+    n = starts[-1] + tail
+    x = make(n, heads, kv, d, dtype, n + d)
+    pos = x["axes"][:len(pairs)].contiguous()
+    scaling = dict(scaling="bands", factor=8.0, low=1.0, high=4.0, original=8192)
+    rope = L.make_rope(d, rot, layout, BASE, **scaling)
+    axes = L.make_rope_axes(pairs, order, "own" if own else "shared")
+    pk = L.make_packing(torch.tensor(starts, device="cuda"), n)
+    q, k = (torch.full_like(x[t], 7.0).cuda() for t in ("q", "k"))
+    call = L.rope_axes_bwd if inverse else L.rope_axes_fwd
+    call(rope, axes, x["q"].cuda(), pos.cuda(), q, x["k"].cuda(), k, packing=pk)
+    table = axes_frequencies(pairs, order, own, rot, **scaling)
+    at = rows_inside(starts, n)
+    for got, t in ((q, "q"), (k, "k")):
+        want, e = turn(x[t][at].double(), table, pos[:, at], rot, layout, 1.0, inverse)
+        s = step_of(dtype)
+        inside(t, got.cpu()[at], want, (1 + s) * e + s * want.abs())
+        assert bool((got.cpu()[~at] == 7.0).all())
+
+
+def test_equal_positions_on_every_axis_are_one_position():
+    n, d = 50, 128
+    x = make(n, 8, 2, d, BF16, 6)
+    pos = x["axes"][0].contiguous().cuda()
+    rope = L.make_rope(d, base=BASE)
+    want, got = x["q"].cuda(), x["q"].cuda()
+    L.rope_fwd(rope, want, positions=pos)
+    L.rope_axes_fwd(rope, L.make_rope_axes((22, 21, 21), "cycled"), got, pos.repeat(3, 1).contiguous())
+    assert torch.equal(want, got)
+
+
+def test_captured_and_replayed_with_an_eager_call_between():
+    n, a, g, d = 200, 8, 2, 128
+    x = {t: v.cuda() for t, v in make(n, a, g, d, BF16, 4).items()}
+    pos = x["axes"][:3].contiguous() % 1000
+    starts = torch.tensor([0, 90, 180], device="cuda")
+    rope, axes, pk = L.make_rope(d), L.make_rope_axes((24, 20, 20)), L.make_packing(starts, n)
+
+    def call(y, dx, dg, ar):
+        where = dict(positions=pos, axes=axes, packing=pk)
+        L.qk_norm_rope_fwd(rope, x["q"], x["gq"], y[0], x["k"], x["gk"], y[1], **where)
+        for t in dg:
+            t.zero_()
+        L.qk_norm_rope_bwd(rope, x["q"], x["gq"], x["dq"], dx[0], dg[0], ar, x["k"], x["gk"], x["dk"], dx[1], dg[1], **where)
+
+    def arrays():
+        return ([torch.zeros_like(x[t]) for t in ("q", "k")], [torch.zeros_like(x[t]) for t in ("q", "k")],
+                [torch.zeros(d, device="cuda") for _ in range(2)])
+
+    mine, ar = arrays(), arena(n, d)
+    call(*mine, ar)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call(*mine, ar)
+    for i in range(3):
+        x["q"].add_(1.0)
+        pos.add_(17)
+        starts.copy_(torch.tensor([i, 50 + 40 * i, 190]))
+        for group in mine:
+            for t in group:
+                t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = arrays()
+        call(*want, arena(n, d))
+        for p, q in zip(mine, want):
+            for u, v in zip(p, q):
+                assert torch.equal(u, v), i
+
+
+def test_rows_behind_2_to_32_elements():
+    """A row stride that puts the last rows behind 2^32 elements."""
+    n, a, d, ld = 600, 2, 64, 1 << 23
+    if torch.cuda.mem_get_info()[0] < 14 << 30:
+        pytest.skip("needs 11 GB")
+    x = {t: v.cuda() for t, v in make(n, a, 1, d, BF16, 4).items()}
+    big = torch.zeros((n - 1) * ld + a * d, dtype=BF16, device="cuda").as_strided((n, a, d), (ld, d, 1))
+    big.copy_(x["q"])
+    rope, dg = L.make_rope(d), [torch.zeros(d, device="cuda") for _ in range(2)]
+    y, dx = torch.zeros_like(x["q"]), torch.zeros_like(x["q"])
+    L.qk_norm_rope_bwd(rope, x["q"], x["gq"], x["dq"], dx, dg[0], arena(n, d))
+    dxb = torch.zeros_like(dx)
+    L.qk_norm_rope_bwd(rope, big, x["gq"], x["dq"], dxb, dg[1], arena(n, d))
+    L.qk_norm_rope_fwd(rope, x["q"], x["gq"], y)
+    L.qk_norm_rope_fwd(rope, big, x["gq"])
+    assert torch.equal(big, y) and torch.equal(dx, dxb) and torch.equal(*dg)
