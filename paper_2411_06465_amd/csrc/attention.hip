@@ -1152,6 +1152,31 @@ static int splits_of_all(int64_t base, int64_t want, int most) {
   while (base * n < want && n < most) n *= 2;
   return n;
 }
+// Rows that the queries of a block of keys cover at most.
+static int64_t window_rows(const PackedAttn& p) {
+  const int64_t tokens = p.pk.tokens;
+  if (!p.window) return tokens;
+  return std::min<int64_t>(tokens, std::max(127 + p.window, p.sinks ? p.far_rows : 0));
+}
+// With a window the blocks are about equally long, so that what counts is how many rounds
+// they make, each as long as a block's tiles (0.9 us each), against the sums of the slices.
+// 32768 tokens in 2 documents, window 4096, 8/1 heads of 128, forward and backward in 1, 2, 4
+// slices: 2187, 2216, 2222 us; 128 tokens in 3, window 16, 4/2 heads of 64, in 1 and 2: 28.0, 31.3.
+static int window_splits(const PackedAttn& p) {
+  const int64_t tokens = p.pk.tokens, n_seqs = std::max(p.pk.n_seqs, 1), group = p.heads / p.kv_heads;
+  const int64_t at_once = p.d_h == 128 ? 256 : 512;
+  // in whole blocks: those whose window the document's end cuts are half as long on average
+  const double blocks = (tokens / 128.0 - n_seqs * std::min<double>(p.window, tokens / n_seqs) / 256) * p.kv_heads;
+  const double tiles = std::min<double>(p.window + 128, static_cast<double>(tokens) / n_seqs + QT) / QT * group;
+  int best = 1;
+  double least = 1e30;
+  for (int n = 1; n <= packed_hpb(p.heads, p.kv_heads); n *= 2) {
+    const double sums = n > 1 ? 6.0 + 16e-6 * n * tokens * p.kv_heads * p.d_h / 4.8 : 0.0;
+    const double us = std::ceil(blocks * n / at_once) * (0.9 * tiles / n + 5.0) + sums;
+    if (us < least) least = us, best = n;
+  }
+  return best;
+}
 void attn_packed_plan(PackedAttn* p) {
   const int64_t tokens = p->pk.tokens, n_seqs = std::max(p->pk.n_seqs, 1), group = p->heads / p->kv_heads;
   const int64_t base = std::min(tokens / 128 + n_seqs, tokens) * p->kv_heads;      // at most that many blocks
@@ -1159,6 +1184,10 @@ void attn_packed_plan(PackedAttn* p) {
   // The documents of one of the 256 threads have at most that many blocks.  Starts that are
   // not in order may make more: the list's counts then still stay below 2^31.
   p->list_steps = static_cast<int32_t>(tokens / 128 + p->pk.n_seqs / 256 + 1 + attn_far_items(*p));
+  if (p->window && base < 512) {
+    p->n_split = window_splits(*p);
+    return;
+  }
   if (base < 512) {
     p->n_split = splits_of_all(base, tokens >= 2048 * n_seqs ? 1024 : 512, packed_hpb(p->heads, p->kv_heads));
     return;
@@ -1167,15 +1196,23 @@ void attn_packed_plan(PackedAttn* p) {
   if (p->window) even = std::min(even, static_cast<double>(tokens) * (p->window + 64) * p->heads / (128 * QT) / 256);
   const int64_t most = static_cast<int64_t>(std::min(std::max(64.0, even), 1e9)) / group;      // query tiles that stay whole
   p->cut_rows = static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(most * QT + 1, 128), INT32_MAX));
-  p->n_split = group % 2 == 0 && tokens >= p->cut_rows ? 2 : 1;
+  p->n_split = group % 2 == 0 && window_rows(*p) >= p->cut_rows ? 2 : 1;
 }
 int64_t attn_packed_places(const PackedAttn& p) {
   const int64_t most = std::min<int64_t>(packed_slots(p, 128), p.pk.tokens);     // blocks with a row
   return p.cut_rows ? most + (p.n_split - 1) * packed_windows(p) + attn_far_items(p) : (most + attn_far_items(p)) * p.n_split;
 }
 void attn_window_plan(PackedAttn* p) {
-  p->far_chunk = std::max(512, (p->sinks + 127) / 128 * 128);
-  p->far_rows = (p->sinks + 127) / 128 * 128 + std::max(p->window, 2 * p->far_chunk);
+  // Chunks of 256 rows: a far chunk of 512 rows is a tenth to a half of a block's tiles, and starts
+  // last (16384 tokens, window 1024, 16/4 heads of 64, 512 blocks on 512 places: dK/dV 231 us
+  // with chunks of 512, 198 of 256, 201 of 128; 32768 tokens, window 4096, 8/1 heads of 128: 1018,
+  // 1020, 1025, the sums of the parts 7, 9, 14).  Not more than half a short window, whose
+  // blocks would wait for the first one (window 128 of 100 documents: 94 us with 512, 67 with
+  // 128); more for many first tokens, whose parts have as many rows.
+  const int blocks = (p->sinks + 127) / 128 * 128;
+  const int chunk = std::min((std::max(p->window / 2, 4 * p->sinks) + 127) / 128 * 128, p->sinks > 64 ? 512 : 256);
+  p->far_chunk = std::max(chunk, blocks);
+  p->far_rows = blocks + std::max(p->window, 2 * p->far_chunk - blocks);
   const bool far = p->window && p->sinks && p->pk.tokens > p->far_rows;
   p->far_parts = far ? p->pk.tokens / p->far_chunk + 1 : 0;
   if (!far) p->far_rows = 1 << 30;

@@ -883,36 +883,48 @@ __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
 // dK, dV of first tokens whose document has rows far from them: the sum of their block's own
 // part and of those of the far rows, in order, over what attn_packed_dkdv_kernel or
 // attn_packed_reduce_kernel stored.  A workgroup per part that may be a document's first and
-// kv head; a wave per first token and tensor, columns over its lanes.
+// kv head, a wave per first token and tensor, sixteen loads in flight (one load after another:
+// 51 us for 48 parts of four slices).
 template <int D>
 __global__ void __launch_bounds__(256) attn_sink_reduce_kernel(PackedAttn p) {
+  constexpr int N = D / 64, L = 16;      // columns per lane; loads in flight
   const int lane = static_cast<int>(threadIdx.x) & 63, hk = static_cast<int>(blockIdx.y);
   const int part0 = static_cast<int>(blockIdx.x), base = (part0 + 1) * p.far_chunk;
   // the document whose first far row lies in chunk part0 + 1
   const SeqRows s = seq_of_row(p.pk, base + p.far_chunk - 1 - p.far_rows, lane);
   if (s.i < 0 || s.lo + p.far_rows < base || s.hi <= s.lo + p.far_rows) return;
-  const int last = (s.hi - 1) / p.far_chunk;
+  const int parts = (s.hi - 1) / p.far_chunk - part0;
   const int64_t step = static_cast<int64_t>(p.kv_heads) * p.sinks * D;       // from one slice to the next
   const int64_t half = static_cast<int64_t>(p.far_parts) * p.n_split * step;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int i = static_cast<int>(blockIdx.z) * 4 + wave; i < 2 * p.sinks; i += 4 * gridDim.z) {
+  for (int i = static_cast<int>(blockIdx.z) * 4 + wave; i < 2 * p.sinks; i += 4 * static_cast<int>(gridDim.z)) {
     const int which = i & 1, row = i >> 1;
     const float* src = p.sink_partial + which * half + (static_cast<int64_t>(part0) * p.n_split * p.kv_heads + hk) * p.sinks * D +
-                       static_cast<int64_t>(row) * D;
+                       static_cast<int64_t>(row) * D + lane * N;
+    // the own part's slices, then those of every far part
     const int own = packed_slices(p, block_rows<true>(p, s.lo, s.hi, s.lo + row / 128 * 128));
-    float v[D / 64] = {};
-    for (int c = 0; c < own; ++c)
+    const int n = p.cut_rows ? parts : parts * p.n_split;
+    const int64_t far_step = p.cut_rows ? p.n_split * step : step;
+    float v[N];
 #pragma unroll
-      for (int u = 0; u < D / 64; ++u) v[u] += src[c * step + lane * (D / 64) + u];
-    const int far = p.cut_rows ? 1 : p.n_split;
-    for (int part = part0 + 1; part <= last; ++part) {
-      src += p.n_split * step;
-      for (int c = 0; c < far; ++c)
+    for (int u = 0; u < N; ++u) v[u] = src[u];
+    for (int c = 1; c < own; ++c)
 #pragma unroll
-        for (int u = 0; u < D / 64; ++u) v[u] += src[c * step + lane * (D / 64) + u];
+      for (int u = 0; u < N; ++u) v[u] += src[c * step + u];
+    src += p.n_split * step;
+    for (int left = n; left > 0; left -= L, src += L * far_step) {
+      float x[L][N];
+#pragma unroll
+      for (int j = 0; j < L; ++j)        // loads without a condition: they stay in flight together
+#pragma unroll
+        for (int u = 0; u < N; ++u) x[j][u] = src[min(j, left - 1) * far_step + u];
+#pragma unroll
+      for (int j = 0; j < L; ++j)
+#pragma unroll
+        for (int u = 0; u < N; ++u) v[u] += j < left ? x[j][u] : 0.f;
     }
-    uint16_t* dst = (which ? p.dv + (s.lo + row) * p.dv_ld : p.dk + (s.lo + row) * p.dk_ld) + hk * D + lane * (D / 64);
-    if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst) = pack2(v[0], v[1]);
+    uint16_t* dst = (which ? p.dv + (s.lo + row) * p.dv_ld : p.dk + (s.lo + row) * p.dk_ld) + hk * D + lane * N;
+    if constexpr (N == 2) *reinterpret_cast<uint32_t*>(dst) = pack2(v[0], v[1]);
     else *dst = f2bf(v[0]);
   }
 }
@@ -942,7 +954,7 @@ hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
     const dim3 grid(static_cast<unsigned>(p.cut_rows ? packed_windows(p) : packed_slots(p, 128)) * 4, p.kv_heads);
     hipLaunchKernelGGL((attn_packed_reduce_kernel<D, ROPE, WINDOW>), grid, dim3(256), 0, stream, p);
   } else if constexpr (WINDOW) {
-    const dim3 grid(static_cast<unsigned>(p.far_parts - 1), p.kv_heads, std::min((2 * p.sinks + 3) / 4, 8));
+    const dim3 grid(static_cast<unsigned>(p.far_parts - 1), p.kv_heads, std::min((p.sinks + 1) / 2, 16));
     hipLaunchKernelGGL(attn_sink_reduce_kernel<D>, grid, dim3(256), 0, stream, p);
   }
   return hipGetLastError();

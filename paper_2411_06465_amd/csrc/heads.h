@@ -79,7 +79,7 @@ __device__ __forceinline__ bool row_angles(const RopeRotate& r, int row, int lan
 }
 
 template <typename T, int V>
-constexpr int kNormFlight = V == 1 ? 1 : sizeof(T) == 2 ? 4 : 2;      // heads in flight per lane
+constexpr int kNormFlight = V == 1 ? 1 : 4;      // heads in flight per lane
 
 template <typename T, int V, int K, bool INTER>
 __global__ void __launch_bounds__(256) qk_norm_fwd_kernel(QkNorm p) {
@@ -156,24 +156,28 @@ __global__ void __launch_bounds__(256) qk_norm_fwd_kernel(QkNorm p) {
   }
 }
 
-// The backward's waves walk rows in steps of the grid, each lane with its own part of dg; a
-// workgroup's sum goes to its row of `partial`, and qk_norm_gain_kernel adds these up: the
-// order is fixed.
+// The backward's waves walk the rows of one tensor in steps of the grid, each lane with its
+// own part of dg; a workgroup's sum goes to its row of `partial`, and qk_norm_gain_kernel adds
+// these up: the order is fixed.
 template <typename T, int V, int K, bool INTER>
-__global__ void __launch_bounds__(kQkNormWaves * 64) qk_norm_bwd_kernel(QkNorm p) {
-  constexpr int F = V == 1 ? 1 : sizeof(T) == 2 ? 2 : 1, E = 2 * V;
+__global__ void __launch_bounds__(kQkNormWaves * 64) __attribute__((amdgpu_waves_per_eu(4, 4))) qk_norm_bwd_kernel(QkNorm p) {
+  constexpr int F = sizeof(T) == 4 && V > 1 ? 2 : 1, E = 2 * V;
   extern __shared__ __attribute__((aligned(16))) float2 shared_lds[];       // angles of every wave, then its sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const HeadLane<T, V, K, INTER> at(p.r.d_h, p.r.rot, lane % p.group, p.group);
-  const int d = p.r.d_h, hps = 64 / p.group, mine = lane / p.group;
+  const int d = p.r.d_h, hps = 64 / p.group, mine = lane / p.group, t = blockIdx.y;
+  const RopeHeads& h = p.r.t[t];
   float2* table = shared_lds + wave * (p.r.rot / 2);
-  float dg[2][K][E];
+  float g[K][E], dg[K][E];
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int k = 0; k < K; ++k) {
+    RopeVec<T, V> lo, hi;
+    lo.load(static_cast<const T*>(p.gain[t]) + at.a[k]);
+    hi.load(static_cast<const T*>(p.gain[t]) + at.b[k]);
+    at.get(k, lo, hi, g[k]);
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int i = 0; i < E; ++i) dg[t][k][i] = 0.f;
+    for (int i = 0; i < E; ++i) dg[k][i] = 0.f;
+  }
   for (int64_t row = static_cast<int64_t>(blockIdx.x) * kQkNormWaves + wave; row < p.r.tokens;
        row += static_cast<int64_t>(gridDim.x) * kQkNormWaves) {
     if (!row_angles(p.r, static_cast<int>(row), lane, table)) continue;
@@ -182,74 +186,60 @@ __global__ void __launch_bounds__(kQkNormWaves * 64) qk_norm_bwd_kernel(QkNorm p
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int i = 0; i < V; ++i) cs[k][i] = at.pair[k] < 0 ? make_float2(1.f, 0.f) : table[at.pair[k] + i];
+    const T* x = static_cast<const T*>(h.x) + row * h.x_ld;
+    const T* dy = static_cast<const T*>(p.dy[t]) + row * p.dy_ld[t];
+    T* dx = static_cast<T*>(h.y) + row * h.y_ld;
+    for (int h0 = 0; h0 < h.heads; h0 += F * hps) {
+      RopeVec<T, V> xa[F][K], xb[F][K], ya[F][K], yb[F][K];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (t >= p.r.n_tensors) break;
-      const RopeHeads& h = p.r.t[t];
-      const T* x = static_cast<const T*>(h.x) + row * h.x_ld;
-      const T* dy = static_cast<const T*>(p.dy[t]) + row * p.dy_ld[t];
-      T* dx = static_cast<T*>(h.y) + row * h.y_ld;
-      const T* gain = static_cast<const T*>(p.gain[t]);
-      float g[K][E];
+      for (int f = 0; f < F; ++f) {
+        const int head = min(h0 + f * hps + mine, h.heads - 1);
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        RopeVec<T, V> lo, hi;
-        lo.load(gain + at.a[k]);
-        hi.load(gain + at.b[k]);
-        at.get(k, lo, hi, g[k]);
+        for (int k = 0; k < K; ++k) {
+          xa[f][k].load(x + head * d + at.a[k]);
+          xb[f][k].load(x + head * d + at.b[k]);
+          ya[f][k].load(dy + head * d + at.a[k]);
+          yb[f][k].load(dy + head * d + at.b[k]);
+        }
       }
-      for (int h0 = 0; h0 < h.heads; h0 += F * hps) {
-        RopeVec<T, V> xa[F][K], xb[F][K], ya[F][K], yb[F][K];
 #pragma unroll
-        for (int f = 0; f < F; ++f) {
-          const int head = min(h0 + f * hps + mine, h.heads - 1);
+      for (int f = 0; f < F; ++f) {
+        if (h0 + f * hps >= h.heads) break;
+        const int head = h0 + f * hps + mine;
+        const bool ok = head < h.heads;
+        float v[K][E], dn[K][E], s1 = 0.f, s2 = 0.f;
 #pragma unroll
-          for (int k = 0; k < K; ++k) {
-            xa[f][k].load(x + head * d + at.a[k]);
-            xb[f][k].load(x + head * d + at.b[k]);
-            ya[f][k].load(dy + head * d + at.a[k]);
-            yb[f][k].load(dy + head * d + at.b[k]);
+        for (int k = 0; k < K; ++k) {
+          float o[E];
+          at.get(k, xa[f][k], xb[f][k], v[k]);
+          at.get(k, ya[f][k], yb[f][k], o);
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float y0 = o[at.first(i)], y1 = o[at.second(i)];
+            dn[k][at.first(i)] = y0 * cs[k][i].x + y1 * cs[k][i].y;
+            dn[k][at.second(i)] = y1 * cs[k][i].x - y0 * cs[k][i].y;
+          }
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            s1 = fmaf(v[k][i], v[k][i], s1);
+            s2 = fmaf(dn[k][i] * g[k][i], v[k][i], s2);
           }
         }
+        const float rstd = rsqrtf(group_sum(s1, p.group) * p.inv_d + p.eps);
+        const float c = group_sum(s2, p.group) * p.inv_d * rstd * rstd * rstd;
 #pragma unroll
-        for (int f = 0; f < F; ++f) {
-          if (h0 + f * hps >= h.heads) break;
-          const int head = h0 + f * hps + mine;
-          const bool ok = head < h.heads;
-          float v[K][E], dn[K][E], s1 = 0.f, s2 = 0.f;
+        for (int k = 0; k < K; ++k) {
+          float out[E];
 #pragma unroll
-          for (int k = 0; k < K; ++k) {
-            float o[E];
-            at.get(k, xa[f][k], xb[f][k], v[k]);
-            at.get(k, ya[f][k], yb[f][k], o);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-              const float y0 = o[at.first(i)], y1 = o[at.second(i)];
-              dn[k][at.first(i)] = y0 * cs[k][i].x + y1 * cs[k][i].y;
-              dn[k][at.second(i)] = y1 * cs[k][i].x - y0 * cs[k][i].y;
-            }
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-              s1 = fmaf(v[k][i], v[k][i], s1);
-              s2 = fmaf(dn[k][i] * g[k][i], v[k][i], s2);
-            }
+          for (int i = 0; i < E; ++i) {
+            out[i] = rstd * g[k][i] * dn[k][i] - c * v[k][i];
+            dg[k][i] += ok ? dn[k][i] * v[k][i] * rstd : 0.f;
           }
-          const float rstd = rsqrtf(group_sum(s1, p.group) * p.inv_d + p.eps);
-          const float c = group_sum(s2, p.group) * p.inv_d * rstd * rstd * rstd, add = ok ? rstd : 0.f;
-#pragma unroll
-          for (int k = 0; k < K; ++k) {
-            float out[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-              out[i] = rstd * g[k][i] * dn[k][i] - c * v[k][i];
-              if (ok) dg[t][k][i] = fmaf(dn[k][i], v[k][i] * add, dg[t][k][i]);
-            }
-            if (ok && at.live[k]) {
-              xa[f][k].set(out);
-              xb[f][k].set(out + V);
-              xa[f][k].store(dx + head * d + at.a[k]);
-              xb[f][k].store(dx + head * d + at.b[k]);
-            }
+          if (ok && at.live[k]) {
+            xa[f][k].set(out);
+            xb[f][k].set(out + V);
+            xa[f][k].store(dx + head * d + at.a[k]);
+            xb[f][k].store(dx + head * d + at.b[k]);
           }
         }
       }
@@ -259,21 +249,19 @@ __global__ void __launch_bounds__(kQkNormWaves * 64) qk_norm_bwd_kernel(QkNorm p
   __syncthreads();
   float* sums = reinterpret_cast<float*>(shared_lds);
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        float v = dg[t][k][i];
-        for (int o = p.group; o < 64; o *= 2) v += __shfl_xor(v, o, 64);
-        if (mine == 0 && at.live[k]) sums[(wave * 2 + t) * d + (i < V ? at.a[k] + i : at.b[k] + i - V)] = v;
-      }
+    for (int i = 0; i < E; ++i) {
+      float v = dg[k][i];
+      for (int o = p.group; o < 64; o *= 2) v += __shfl_xor(v, o, 64);
+      if (mine == 0 && at.live[k]) sums[wave * d + (i < V ? at.a[k] + i : at.b[k] + i - V)] = v;
+    }
   __syncthreads();
-  for (int e = threadIdx.x; e < 2 * d; e += kQkNormWaves * 64) {
+  for (int e = threadIdx.x; e < d; e += kQkNormWaves * 64) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kQkNormWaves; ++w) v += sums[w * 2 * d + e];
-    p.partial[static_cast<int64_t>(blockIdx.x) * 2 * d + e] = v;
+    for (int w = 0; w < kQkNormWaves; ++w) v += sums[w * d + e];
+    p.partial[(static_cast<int64_t>(blockIdx.x) * 2 + t) * d + e] = v;
   }
 }
 
@@ -377,7 +365,7 @@ __global__ void __launch_bounds__(256) dropout_any_kernel(DropoutAdd p) {
 template <typename T, int V, int K>
 hipError_t norm_launch(const QkNorm& p, dim3 grid, hipStream_t stream) {
   if (p.backward) {
-    const size_t lds = kQkNormWaves * std::max<size_t>(p.r.rot / 2 * sizeof(float2), 2 * p.r.d_h * sizeof(float));
+    const size_t lds = kQkNormWaves * std::max<size_t>(p.r.rot / 2 * sizeof(float2), p.r.d_h * sizeof(float));
     if (p.r.interleaved) hipLaunchKernelGGL((qk_norm_bwd_kernel<T, V, K, true>), grid, dim3(kQkNormWaves * 64), lds, stream, p);
     else hipLaunchKernelGGL((qk_norm_bwd_kernel<T, V, K, false>), grid, dim3(kQkNormWaves * 64), lds, stream, p);
     const dim3 sums((p.r.d_h + 63) / 64, p.r.n_tensors);
@@ -410,8 +398,9 @@ int32_t qk_norm_parts(int64_t tokens) {
 hipError_t qk_norm_rope(const QkNorm& params, hipStream_t stream) {
   QkNorm p = params;
   const int size = p.r.f32 ? 4 : 2;
-  // whole units of 8 pairs, of which a head has at most 32
-  bool vec = p.r.rot % 16 == 0 && p.r.d_h % 16 == 0;
+  // whole units of two 16-byte vectors, of which a head has at most 64
+  const int unit = 32 / size;
+  bool vec = p.r.rot % unit == 0 && p.r.d_h % unit == 0;
   for (int t = 0; t < p.r.n_tensors; ++t) {
     const RopeHeads& h = p.r.t[t];
     vec = vec && aligned16(h.x, h.x_ld, size) && aligned16(h.y, h.y_ld, size) && aligned16(p.gain[t], 8, size) &&
@@ -420,18 +409,18 @@ hipError_t qk_norm_rope(const QkNorm& params, hipStream_t stream) {
   p.inv_d = 1.f / static_cast<float>(p.r.d_h);
   p.group = 64;
   if (vec)
-    for (p.group = 1; p.group < p.r.d_h / 16;) p.group *= 2;
+    for (p.group = 1; p.group < p.r.d_h / unit;) p.group *= 2;
   p.r.parts = 1;
-  dim3 grid(static_cast<unsigned>(qk_norm_parts(p.r.tokens)));
+  dim3 grid(static_cast<unsigned>(qk_norm_parts(p.r.tokens)), static_cast<unsigned>(p.r.n_tensors));
   if (!p.backward) {
-    const int at_once = (vec ? (p.r.f32 ? kNormFlight<float, 8> : kNormFlight<uint16_t, 8>) : 1) * (64 / p.group);
+    const int at_once = (vec ? kNormFlight<uint16_t, 8> : 1) * (64 / p.group);
     int most = p.r.t[0].heads;
     if (p.r.n_tensors > 1) most = std::max(most, p.r.t[1].heads);
     // waves per row: as rope_rotate
     while (static_cast<int64_t>(p.r.tokens) * p.r.parts * 2 <= 8192 && most > at_once * p.r.parts) p.r.parts *= 2;
     grid = dim3(static_cast<unsigned>((p.r.tokens + 3) / 4), static_cast<unsigned>(p.r.parts));
   }
-  if (p.r.f32) return vec ? norm_launch<float, 8, 1>(p, grid, stream) : norm_launch<float, 1, 4>(p, grid, stream);
+  if (p.r.f32) return vec ? norm_launch<float, 4, 1>(p, grid, stream) : norm_launch<float, 1, 4>(p, grid, stream);
   return vec ? norm_launch<uint16_t, 8, 1>(p, grid, stream) : norm_launch<uint16_t, 1, 4>(p, grid, stream);
 }
 

@@ -278,8 +278,8 @@ struct PackedAttn {
   // A row sees the `window` rows up to itself and its document's first `sinks`; window 0: no
   // window.  dK/dV, set by attn_window_plan: the queries more than far_rows behind a
   // document's start meet its first rows in chunks of far_chunk rows of the whole array.
-  // Documents share no chunk there, as far_rows > far_chunk, and the chunk before a
-  // document's first one takes its first rows' own part: far_rows >= 2 far_chunk + 128.
+  // Documents share no chunk there, and the chunk before a document's first one is no other
+  // document's and takes its first rows' own part: far_rows >= 2 far_chunk.
   int32_t window, sinks;
   int32_t far_rows, far_chunk, far_parts;   // far_parts: chunks, 0: no document has far rows
   float* sink_partial;      // far_parts > 0: dK [far_parts][n_split][kv_heads][sinks][d_h], then dV
