@@ -560,19 +560,29 @@ def _norm_gain(name, gain, dtype, d, like):
     return _flat(name, gain, dtype, (d,), like)
 
 
+def _norm_rows(name, x, dtype, tokens, d, like):
+    """(shape, row stride) of a tensor of heads."""
+    shape = x.shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != d:
+        raise ValueError(f"{name} must be [{tokens}][heads][{d}], not {tuple(shape)}")
+    return shape, _rows(name, x, dtype, shape, like)
+
+
 def qk_norm_rope_fwd(rope, q, q_gain, q_out=None, k=None, k_gain=None, k_out=None, eps=1e-6, positions=None, axes=None,
                      packing=None, stream=None):
     """RMS norm of every head of q (and k), [tokens][heads][head_dim], times its gain, rotated, into q_out (k_out); in
     place without an output.  positions as in rope_fwd, or [n_axes][tokens] with axes."""
     dtype, tokens, d, f32 = q.dtype, q.shape[0], rope.head_dim, _float_type("q", q)
-    io = []
-    for name, x, gain, y in (("q", q, q_gain, q_out), ("k", k, k_gain, k_out)):
-        if x is not None:
-            h = _rope_io(name, x, y, dtype, tokens, d, q)
-            io.append(NormHeads(h.x, _norm_gain(name + "_gain", gain, dtype, d, q), h.y, h.heads, h.x_ld, h.y_ld))
+    shape, ld = _norm_rows("q", q, dtype, tokens, d, q)
+    y, y_ld = (q, ld) if q_out is None else (q_out, _rows("q_out", q_out, dtype, shape, q))
+    io = NormHeads(q.data_ptr(), _norm_gain("q_gain", q_gain, dtype, d, q), y.data_ptr(), shape[1], ld, y_ld)
+    io_k = None
+    if k is not None:
+        shape, ld = _norm_rows("k", k, dtype, tokens, d, q)
+        y, y_ld = (k, ld) if k_out is None else (k_out, _rows("k_out", k_out, dtype, shape, q))
+        io_k = NormHeads(k.data_ptr(), _norm_gain("k_gain", k_gain, dtype, d, q), y.data_ptr(), shape[1], ld, y_ld)
     _launch(lib().qk_norm_rope_fwd, q, stream, rope, axes, f32, tokens,
-            None if packing is None else _on_one_device(packing, q), _positions(axes, positions, tokens, q), eps, io[0],
-            io[1] if len(io) > 1 else None)
+            None if packing is None else _on_one_device(packing, q), _positions(axes, positions, tokens, q), eps, io, io_k)
 
 
 def l4d_qk_norm_workspace_bytes(tokens, head_dim):
@@ -588,16 +598,18 @@ def qk_norm_rope_bwd(rope, q, q_gain, dq_out, dq, d_q_gain, arena, k=None, k_gai
     gradients (f32) added to."""
     import torch
     dtype, tokens, d, f32 = q.dtype, q.shape[0], rope.head_dim, _float_type("q", q)
-    io = []
-    for name, x, gain, dy, dx, dg in (("q", q, q_gain, dq_out, dq, d_q_gain), ("k", k, k_gain, dk_out, dk, d_k_gain)):
-        if x is not None:
-            h = _rope_io(name, x, dx, dtype, tokens, d, q)
-            io.append(NormHeadsGrad(h.x, _norm_gain(name + "_gain", gain, dtype, d, q), dy.data_ptr(), h.y,
-                                    _norm_gain("d_" + name + "_gain", dg, torch.float32, d, q), h.heads, h.x_ld,
-                                    _rows("d" + name + "_out", dy, dtype, x.shape, q), h.y_ld))
+
+    def heads(name, x, gain, dy, dx, dg):
+        shape, ld = _norm_rows(name, x, dtype, tokens, d, q)
+        dy_ld, dx_ld = _rows(f"d{name}_out", dy, dtype, shape, q), _rows(f"d{name}", dx, dtype, shape, q)
+        return NormHeadsGrad(x.data_ptr(), _norm_gain(f"{name}_gain", gain, dtype, d, q), dy.data_ptr(), dx.data_ptr(),
+                             _norm_gain(f"d_{name}_gain", dg, torch.float32, d, q), shape[1], ld, dy_ld, dx_ld)
+
+    io = heads("q", q, q_gain, dq_out, dq, d_q_gain)
+    io_k = None if k is None else heads("k", k, k_gain, dk_out, dk, d_k_gain)
     _launch(lib().qk_norm_rope_bwd, q, stream, rope, axes, f32, tokens,
-            None if packing is None else _on_one_device(packing, q), _positions(axes, positions, tokens, q), eps, io[0],
-            io[1] if len(io) > 1 else None, arena.h)
+            None if packing is None else _on_one_device(packing, q), _positions(axes, positions, tokens, q), eps, io, io_k,
+            arena.h)
 
 
 def _attn_args(q, tensors):

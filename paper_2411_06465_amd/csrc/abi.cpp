@@ -1101,18 +1101,22 @@ int attn_distinct(const AttnRows* t, int n, int first_out) {
 }
 // dQ first: it also writes delta, which dK/dV reads.
 int packed_attn_backward(const PackedAttn& p, hipStream_t s) {
-  const bool w = p.window > 0;
   int rc;
-  if ((rc = launch(w ? "attn_window_dq" : "attn_packed_dq", s, [&] { return attn_packed_bwd(p, 2, s); }))) return rc;
-  if ((rc = launch(w ? "attn_window_dkdv" : "attn_packed_dkdv", s, [&] { return attn_packed_bwd(p, 1, s); }))) return rc;
-  if (p.n_split > 1 &&
-      (rc = launch(w ? "attn_window_reduce" : "attn_packed_reduce", s, [&] { return attn_packed_bwd(p, 3, s); })))
-    return rc;
-  if (p.far_parts) return launch("attn_window_sinks", s, [&] { return attn_packed_bwd(p, 4, s); });
+  if ((rc = launch("attn_packed_dq", s, [&] { return attn_packed_bwd(p, 2, s); }))) return rc;
+  if ((rc = launch("attn_packed_dkdv", s, [&] { return attn_packed_bwd(p, 1, s); }))) return rc;
+  if (p.n_split > 1) return launch("attn_packed_reduce", s, [&] { return attn_packed_bwd(p, 3, s); });
+  return L4D_OK;
+}
+int window_attn_backward(const WindowAttn& p, hipStream_t s) {
+  int rc;
+  if ((rc = launch("attn_window_dq", s, [&] { return attn_window_bwd(p, 2, s); }))) return rc;
+  if ((rc = launch("attn_window_dkdv", s, [&] { return attn_window_bwd(p, 1, s); }))) return rc;
+  if (p.n_split > 1 && (rc = launch("attn_window_reduce", s, [&] { return attn_window_bwd(p, 3, s); }))) return rc;
+  if (p.far_parts) return launch("attn_window_sinks", s, [&] { return attn_window_bwd(p, 4, s); });
   return L4D_OK;
 }
 // A window that no row of `tokens` rows reaches past hides nothing: the call is the one without.
-int attn_window(const l4d_window* w, int64_t tokens, PackedAttn* p) {
+int attn_window(const l4d_window* w, int64_t tokens, WindowAttn* p) {
   if (!w) return fail(L4D_EINVAL, "window is required");
   if (w->window < 1) return fail(L4D_EINVAL, "the window must be at least 1");
   if (w->sinks < 0 || w->sinks > kMaxSinks) return fail(L4D_EINVAL, "sinks must lie in 0 .. %d", kMaxSinks);
@@ -1120,18 +1124,18 @@ int attn_window(const l4d_window* w, int64_t tokens, PackedAttn* p) {
   if (w->window >= tokens) return L4D_OK;
   p->window = (int32_t)w->window;
   p->sinks = (int32_t)w->sinks;
-  attn_window_plan(p);
+  attn_window_chunks(p);
   return L4D_OK;
 }
 struct PackedWs {
   uint64_t delta, lse2, items, partial, sinks, total;
 };
-PackedWs plan_packed(const PackedAttn& p, int64_t tokens) {
+PackedWs plan_packed(const WindowAttn& p, int64_t tokens) {
   Carver cv;
   PackedWs w{};
   w.delta = cv.take((uint64_t)p.heads * tokens * 4);
   w.lse2 = cv.take((uint64_t)p.heads * tokens * 4);
-  w.items = cv.take((uint64_t)attn_packed_items(p) * (p.window ? 16 : 8));
+  w.items = cv.take(p.window ? (uint64_t)attn_window_items(p) * 16 : (uint64_t)attn_packed_items(tokens) * 8);
   const int splits = attn_packed_most_splits(tokens, p.heads, p.kv_heads);
   w.partial = splits > 1 ? cv.take(2ull * splits * tokens * p.kv_heads * p.d_h * 4) : 0;
   w.sinks = cv.take(2ull * p.far_parts * splits * p.kv_heads * p.sinks * p.d_h * 4);
@@ -1843,8 +1847,7 @@ extern "C" int dropout_add_bwd(int dtype, int64_t rows, int64_t cols, const void
 
 extern "C" int l4d_attn_packed_workspace_bytes(const l4d_attn* at, int64_t tokens, uint64_t* bytes) {
   if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "tokens must lie in 0 .. 2^30");
-  PackedAttn p{};
-  p.pk.tokens = (int32_t)tokens;
+  WindowAttn p{};
   int rc = attn_shape(at, &p);
   if (rc) return rc;
   if (bytes) *bytes = align_up(plan_packed(p, tokens).total);
@@ -1852,7 +1855,7 @@ extern "C" int l4d_attn_packed_workspace_bytes(const l4d_attn* at, int64_t token
 }
 extern "C" int l4d_attn_window_workspace_bytes(const l4d_window* w, const l4d_attn* at, int64_t tokens, uint64_t* bytes) {
   if (tokens < 0 || tokens > (int64_t)1 << 30) return fail(L4D_EINVAL, "tokens must lie in 0 .. 2^30");
-  PackedAttn p{};
+  WindowAttn p{};
   int rc;
   if ((rc = attn_shape(at, &p)) || (rc = attn_window(w, tokens, &p))) return rc;
   if (bytes) *bytes = align_up(plan_packed(p, tokens).total);
@@ -1865,7 +1868,7 @@ static int attn_forward(bool windowed, const l4d_window* w, const l4d_attn* at, 
                         float* lse, void* stream_ptr) {
   int rc = check_packing(pk);
   if (rc) return rc;
-  PackedAttn p{};
+  WindowAttn p{};
   if ((rc = attn_shape(at, &p))) return rc;
   if (windowed && (rc = attn_window(w, pk->tokens, &p))) return rc;
   const AttnRows t[4] = {{"q", q, q_ld, at->n_heads}, {"k", k, k_ld, at->n_kv_heads}, {"v", v, v_ld, at->n_kv_heads},
@@ -1873,7 +1876,7 @@ static int attn_forward(bool windowed, const l4d_window* w, const l4d_attn* at, 
   if ((rc = attn_rows(t, 4, at->head_dim)) || (rc = attn_distinct(t, 4, 3))) return rc;
   if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return fail(L4D_EINVAL, "lse is required, 4-byte aligned");
   p.pk = device_packing(pk);
-  if (!attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
+  if (p.window ? !attn_window_fits(p) : !attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
   if (pk->tokens == 0 || pk->n_seqs == 0) return L4D_OK;
   p.q = static_cast<const uint16_t*>(q);
   p.k = static_cast<const uint16_t*>(k);
@@ -1882,7 +1885,8 @@ static int attn_forward(bool windowed, const l4d_window* w, const l4d_attn* at, 
   p.q_ld = q_ld, p.k_ld = k_ld, p.v_ld = v_ld, p.o_ld = o_ld;
   p.lse = lse;
   hipStream_t s = static_cast<hipStream_t>(stream_ptr);
-  return launch(p.window ? "attn_window_fwd" : "attn_packed_fwd", s, [&] { return attn_packed_fwd(p, s); });
+  if (p.window) return launch("attn_window_fwd", s, [&] { return attn_window_fwd(p, s); });
+  return launch("attn_packed_fwd", s, [&] { return attn_packed_fwd(p, s); });
 }
 
 extern "C" int attn_packed_fwd(const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld, const void* k,
@@ -1902,7 +1906,7 @@ static int attn_backward(bool windowed, const l4d_window* w, const l4d_attn* at,
                          void* dv, int64_t dv_ld, l4d_arena* A, void* stream_ptr) {
   int rc = check_packing(pk);
   if (rc) return rc;
-  PackedAttn p{};
+  WindowAttn p{};
   if ((rc = attn_shape(at, &p))) return rc;
   if (windowed && (rc = attn_window(w, pk->tokens, &p))) return rc;
   const int64_t a = at->n_heads, g = at->n_kv_heads;
@@ -1912,7 +1916,7 @@ static int attn_backward(bool windowed, const l4d_window* w, const l4d_attn* at,
   if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return fail(L4D_EINVAL, "lse is required, 4-byte aligned");
   if (!A) return fail(L4D_EINVAL, "arena is required");
   p.pk = device_packing(pk);
-  if (!attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
+  if (p.window ? !attn_window_fits(p) : !attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
   if (pk->tokens == 0 || pk->n_seqs == 0) return L4D_OK;
   const PackedWs plan = plan_packed(p, pk->tokens);
   Workspace ws;
@@ -1934,8 +1938,13 @@ static int attn_backward(bool windowed, const l4d_window* w, const l4d_attn* at,
   p.items = reinterpret_cast<int32_t*>(wsb + plan.items);
   p.dkv_partial = reinterpret_cast<float*>(wsb + plan.partial);
   p.sink_partial = reinterpret_cast<float*>(wsb + plan.sinks);
+  hipStream_t s = static_cast<hipStream_t>(stream_ptr);
+  if (p.window) {
+    attn_window_plan(&p);
+    return window_attn_backward(p, s);
+  }
   attn_packed_plan(&p);
-  return packed_attn_backward(p, static_cast<hipStream_t>(stream_ptr));
+  return packed_attn_backward(p, s);
 }
 
 extern "C" int attn_packed_bwd(const l4d_attn* at, const l4d_packing* pk, const void* q, int64_t q_ld, const void* k,

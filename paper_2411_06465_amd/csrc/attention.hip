@@ -1152,17 +1152,74 @@ static int splits_of_all(int64_t base, int64_t want, int most) {
   while (base * n < want && n < most) n *= 2;
   return n;
 }
+void attn_packed_plan(PackedAttn* p) {
+  const int64_t tokens = p->pk.tokens, n_seqs = std::max(p->pk.n_seqs, 1), group = p->heads / p->kv_heads;
+  const int64_t base = std::min(tokens / 128 + n_seqs, tokens) * p->kv_heads;      // at most that many blocks
+  p->cut_rows = 0;
+  // The documents of one of the 256 threads have at most that many blocks.  Starts that are
+  // not in order may make more: the list's counts then still stay below 2^31.
+  p->list_steps = static_cast<int32_t>(tokens / 128 + p->pk.n_seqs / 256 + 1);
+  if (base < 512) {
+    p->n_split = splits_of_all(base, tokens >= 2048 * n_seqs ? 1024 : 512, packed_hpb(p->heads, p->kv_heads));
+    return;
+  }
+  const double even = static_cast<double>(tokens) * tokens / n_seqs * p->heads / (2.0 * 128 * QT) / 256;
+  const int64_t most = static_cast<int64_t>(std::min(std::max(64.0, even), 1e9)) / group;      // query tiles that stay whole
+  p->cut_rows = static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(most * QT + 1, 128), INT32_MAX));
+  p->n_split = group % 2 == 0 && tokens >= p->cut_rows ? 2 : 1;
+}
+int64_t attn_packed_places(const PackedAttn& p) {
+  const int64_t most = std::min<int64_t>(packed_slots(p, 128), p.pk.tokens);     // blocks with a row
+  return p.cut_rows ? most + (p.n_split - 1) * packed_windows(p) : most * p.n_split;
+}
+int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads) {
+  const int64_t base = (tokens + 127) / 128 * kv_heads;
+  return base < 512 ? splits_of_all(base, 1024, packed_hpb(static_cast<int>(heads), static_cast<int>(kv_heads)))
+                    : (heads / kv_heads % 2 == 0 ? 2 : 1);
+}
+
+bool attn_packed_fits(const PackedAttn& p) {
+  // a grid holds less than 2^32 threads; slots of the smallest query blocks (32 rows) and of the key blocks
+  const int64_t q = packed_slots(p, 32) * p.heads, k = packed_slots(p, 128) * p.heads;
+  return q + 1 < (int64_t{1} << 24) && k < (int64_t{1} << 23);
+}
+
+template <bool WINDOW>
+static hipError_t packed_part(AttnArgs<WINDOW>& p, int part, hipStream_t stream) {
+  if constexpr (!WINDOW)     // only the layer's attention turns its gradients back
+    if (p.rope) return p.d_h == 128 ? packed_launch<128, true, false>(p, part, stream) : packed_launch<64, true, false>(p, part, stream);
+  return p.d_h == 128 ? packed_launch<128, false, WINDOW>(p, part, stream) : packed_launch<64, false, WINDOW>(p, part, stream);
+}
+hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream) { return packed_part<false>(p, 0, stream); }
+hipError_t attn_packed_bwd(PackedAttn p, int part, hipStream_t stream) { return packed_part<false>(p, part, stream); }
+
+// ------------------------------------------------------------------ with a window
+
+void attn_window_chunks(WindowAttn* p) {
+  // Chunks of 256 rows: a far chunk of 512 rows is a tenth to a half of a block's tiles, and starts
+  // last (16384 tokens, window 1024, 16/4 heads of 64, 512 blocks on 512 places: dK/dV 231 us
+  // with chunks of 512, 198 of 256, 201 of 128; 32768 tokens, window 4096, 8/1 heads of 128: 1018,
+  // 1020, 1025, the sums of the parts 7, 9, 14).  Not more than half a short window, whose
+  // blocks would wait for the first one (window 128 of 100 documents: 94 us with 512, 67 with
+  // 128); more for many first tokens, whose parts have as many rows.
+  const int blocks = (p->sinks + 127) / 128 * 128;
+  const int chunk = std::min((std::max(p->window / 2, 4 * p->sinks) + 127) / 128 * 128, p->sinks > 64 ? 512 : 256);
+  p->far_chunk = std::max(chunk, blocks);
+  p->far_rows = blocks + std::max(p->window, 2 * p->far_chunk - blocks);
+  const bool far = p->sinks && p->pk.tokens > p->far_rows;
+  p->far_parts = far ? p->pk.tokens / p->far_chunk + 1 : 0;
+  if (!far) p->far_rows = 1 << 30;
+}
 // Rows that the queries of a block of keys cover at most.
-static int64_t window_rows(const PackedAttn& p) {
+static int64_t window_rows(const WindowAttn& p) {
   const int64_t tokens = p.pk.tokens;
-  if (!p.window) return tokens;
   return std::min<int64_t>(tokens, std::max(127 + p.window, p.sinks ? p.far_rows : 0));
 }
 // With a window the blocks are about equally long, so that what counts is how many rounds
 // they make, each as long as a block's tiles (0.9 us each), against the sums of the slices.
 // 32768 tokens in 2 documents, window 4096, 8/1 heads of 128, forward and backward in 1, 2, 4
 // slices: 2187, 2216, 2222 us; 128 tokens in 3, window 16, 4/2 heads of 64, in 1 and 2: 28.0, 31.3.
-static int window_splits(const PackedAttn& p) {
+static int window_splits(const WindowAttn& p) {
   const int64_t tokens = p.pk.tokens, n_seqs = std::max(p.pk.n_seqs, 1), group = p.heads / p.kv_heads;
   const int64_t at_once = p.d_h == 128 ? 256 : 512;
   // in whole blocks: those whose window the document's end cuts are half as long on average
@@ -1177,68 +1234,29 @@ static int window_splits(const PackedAttn& p) {
   }
   return best;
 }
-void attn_packed_plan(PackedAttn* p) {
+void attn_window_plan(WindowAttn* p) {
   const int64_t tokens = p->pk.tokens, n_seqs = std::max(p->pk.n_seqs, 1), group = p->heads / p->kv_heads;
-  const int64_t base = std::min(tokens / 128 + n_seqs, tokens) * p->kv_heads;      // at most that many blocks
   p->cut_rows = 0;
-  // The documents of one of the 256 threads have at most that many blocks.  Starts that are
-  // not in order may make more: the list's counts then still stay below 2^31.
   p->list_steps = static_cast<int32_t>(tokens / 128 + p->pk.n_seqs / 256 + 1 + attn_far_items(*p));
-  if (p->window && base < 512) {
+  if (std::min(tokens / 128 + n_seqs, tokens) * p->kv_heads < 512) {
     p->n_split = window_splits(*p);
     return;
   }
-  if (base < 512) {
-    p->n_split = splits_of_all(base, tokens >= 2048 * n_seqs ? 1024 : 512, packed_hpb(p->heads, p->kv_heads));
-    return;
-  }
-  double even = static_cast<double>(tokens) * tokens / n_seqs * p->heads / (2.0 * 128 * QT) / 256;
-  if (p->window) even = std::min(even, static_cast<double>(tokens) * (p->window + 64) * p->heads / (128 * QT) / 256);
-  const int64_t most = static_cast<int64_t>(std::min(std::max(64.0, even), 1e9)) / group;      // query tiles that stay whole
+  // as attn_packed_plan: the blocks with more tiles than a CU would get on average are cut by two
+  const double even = static_cast<double>(tokens) / 128 * std::min(tokens / (2.0 * n_seqs), p->window + 64.0) * p->heads / QT / 256;
+  const int64_t most = static_cast<int64_t>(std::min(std::max(64.0, even), 1e9)) / group;
   p->cut_rows = static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(most * QT + 1, 128), INT32_MAX));
   p->n_split = group % 2 == 0 && window_rows(*p) >= p->cut_rows ? 2 : 1;
 }
-int64_t attn_packed_places(const PackedAttn& p) {
-  const int64_t most = std::min<int64_t>(packed_slots(p, 128), p.pk.tokens);     // blocks with a row
-  return p.cut_rows ? most + (p.n_split - 1) * packed_windows(p) + attn_far_items(p) : (most + attn_far_items(p)) * p.n_split;
+int64_t attn_window_places(const WindowAttn& p) {
+  return attn_packed_places(p) + attn_far_items(p) * (p.cut_rows ? 1 : p.n_split);
 }
-void attn_window_plan(PackedAttn* p) {
-  // Chunks of 256 rows: a far chunk of 512 rows is a tenth to a half of a block's tiles, and starts
-  // last (16384 tokens, window 1024, 16/4 heads of 64, 512 blocks on 512 places: dK/dV 231 us
-  // with chunks of 512, 198 of 256, 201 of 128; 32768 tokens, window 4096, 8/1 heads of 128: 1018,
-  // 1020, 1025, the sums of the parts 7, 9, 14).  Not more than half a short window, whose
-  // blocks would wait for the first one (window 128 of 100 documents: 94 us with 512, 67 with
-  // 128); more for many first tokens, whose parts have as many rows.
-  const int blocks = (p->sinks + 127) / 128 * 128;
-  const int chunk = std::min((std::max(p->window / 2, 4 * p->sinks) + 127) / 128 * 128, p->sinks > 64 ? 512 : 256);
-  p->far_chunk = std::max(chunk, blocks);
-  p->far_rows = blocks + std::max(p->window, 2 * p->far_chunk - blocks);
-  const bool far = p->window && p->sinks && p->pk.tokens > p->far_rows;
-  p->far_parts = far ? p->pk.tokens / p->far_chunk + 1 : 0;
-  if (!far) p->far_rows = 1 << 30;
+bool attn_window_fits(const WindowAttn& p) {
+  const int64_t k = (packed_slots(p, 128) + attn_far_items(p)) * p.heads;
+  // up to 2^28 rows the listing workgroup's counts stay in 32 bits
+  return attn_packed_fits(p) && p.pk.tokens <= 1 << 28 && k < (int64_t{1} << 23) && p.far_parts < 1 << 22;
 }
-int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads) {
-  const int64_t base = (tokens + 127) / 128 * kv_heads;
-  return base < 512 ? splits_of_all(base, 1024, packed_hpb(static_cast<int>(heads), static_cast<int>(kv_heads)))
-                    : (heads / kv_heads % 2 == 0 ? 2 : 1);
-}
-
-bool attn_packed_fits(const PackedAttn& p) {
-  // a grid holds less than 2^32 threads; slots of the smallest query blocks (32 rows) and of the key blocks
-  const int64_t q = packed_slots(p, 32) * p.heads, k = packed_slots(p, 128) * p.heads;
-  if (p.window && p.pk.tokens > 1 << 28) return false;      // the listing workgroup's counts stay in 32 bits
-  return q + 1 < (int64_t{1} << 24) && k + attn_far_items(p) * p.heads < (int64_t{1} << 23) && p.far_parts < 1 << 22;
-}
-
-template <int D>
-static hipError_t packed_part(PackedAttn& p, int part, hipStream_t stream) {
-  if (p.window) return packed_launch<D, false, true>(p, part, stream);
-  return p.rope && part ? packed_launch<D, true, false>(p, part, stream) : packed_launch<D, false, false>(p, part, stream);
-}
-hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream) { return attn_packed_bwd(p, 0, stream); }
-
-hipError_t attn_packed_bwd(PackedAttn p, int part, hipStream_t stream) {
-  return p.d_h == 128 ? packed_part<128>(p, part, stream) : packed_part<64>(p, part, stream);
-}
+hipError_t attn_window_fwd(WindowAttn p, hipStream_t stream) { return packed_part<true>(p, 0, stream); }
+hipError_t attn_window_bwd(WindowAttn p, int part, hipStream_t stream) { return packed_part<true>(p, part, stream); }
 
 }  // namespace l4d

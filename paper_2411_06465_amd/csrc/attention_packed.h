@@ -9,6 +9,9 @@
 // holds (an infinity or NaN in V, say, which a zero probability would not hide)
 // can reach another.
 
+template <bool WINDOW>
+using AttnArgs = std::conditional_t<WINDOW, WindowAttn, PackedAttn>;
+
 // Tiles with a probability above this keep a second bf16 part of P (dV) and dS (dQ,
 // dK) in the backward's products (a wave-wide vote): there single elements decide a
 // gradient.  Relative error of dQ, dK, dV on short documents 1.8, 1.7, 1.7e-3, on
@@ -76,7 +79,7 @@ __device__ __forceinline__ void turn_back(f32x16 (&acc)[D / 32], const float2* t
 // forward 653 -> 625 us, dQ 933 -> 886; 8192 tokens in 23, 32/8 heads: forward 85 -> 81, dQ
 // as it was), else the documents one after another, last blocks first.
 template <bool WINDOW>
-__device__ __forceinline__ SeqBlock query_block(const PackedAttn& p, int i, int rows, int lane) {
+__device__ __forceinline__ SeqBlock query_block(const AttnArgs<WINDOW>& p, int i, int rows, int lane) {
   return !WINDOW && p.pk.n_seqs > 1 && p.pk.n_seqs < 64 ? ranked_block(p.pk, i, rows, lane)
                                                         : seq_block(p.pk, p.n_slots - 1 - i, rows, lane);
 }
@@ -92,16 +95,19 @@ struct KeyTiles {
   __device__ __forceinline__ int key(int t, int size) const { return (WINDOW && t >= head ? t + skip : t) * size; }
 };
 template <bool WINDOW>
-__device__ __forceinline__ KeyTiles key_tiles(const PackedAttn& p, const SeqBlock& blk, int n_keys, int size) {
+__device__ __forceinline__ KeyTiles key_tiles(const AttnArgs<WINDOW>& p, const SeqBlock& blk, int n_keys, int size) {
   const int all = (n_keys + size - 1) / size;
-  if constexpr (!WINDOW) return KeyTiles{0, 0, all};
-  const int head = min((p.sinks + size - 1) / size, all);
-  const int first = max(blk.row0 - blk.lo - p.window + 1, 0) / size;      // the tile of the first row's first key
-  const int skip = max(first - head, 0);
-  return KeyTiles{head, skip, all - skip};
+  if constexpr (WINDOW) {
+    const int head = min((p.sinks + size - 1) / size, all);
+    const int first = max(blk.row0 - blk.lo - p.window + 1, 0) / size;      // the tile of the first row's first key
+    const int skip = max(first - head, 0);
+    return KeyTiles{head, skip, all - skip};
+  } else {
+    return KeyTiles{0, 0, all};
+  }
 }
 // Whether the mask of a window cuts the tile of keys k0 .. k0 + size - 1 for one of the rows up to last_q.
-__device__ __forceinline__ bool window_cuts(const PackedAttn& p, int lo, int k0, int size, int last_q) {
+__device__ __forceinline__ bool window_cuts(const WindowAttn& p, int lo, int k0, int size, int last_q) {
   return k0 <= last_q - p.window && k0 + size > lo + p.sinks;
 }
 
@@ -109,10 +115,13 @@ __device__ __forceinline__ bool window_cuts(const PackedAttn& p, int lo, int k0,
 // sees its last key; to far_rows behind the document's first row where the block holds first
 // tokens, whose later rows go in chunks of far_chunk rows (attn_packed_dkdv_kernel).
 template <bool WINDOW>
-__device__ __forceinline__ int block_rows(const PackedAttn& p, int lo, int hi, int row0) {
-  if constexpr (!WINDOW) return hi - row0;
-  if (row0 - lo < p.sinks) return min(hi, lo + p.far_rows) - row0;
-  return min(hi - row0, 127 + p.window);
+__device__ __forceinline__ int block_rows(const AttnArgs<WINDOW>& p, int lo, int hi, int row0) {
+  if constexpr (WINDOW) {
+    if (row0 - lo < p.sinks) return min(hi, lo + p.far_rows) - row0;
+    return min(hi - row0, 127 + p.window);
+  } else {
+    return hi - row0;
+  }
 }
 
 // ------------------------------------------------------------------ forward
@@ -132,7 +141,7 @@ __device__ __forceinline__ int block_rows(const PackedAttn& p, int lo, int hi, i
 // matrix cores busy 55% at 1.7 GHz.  Short ones by the way to the first products, about
 // 4 us of a workgroup's 6 to 20: 8192 tokens in 23, 32/8 heads of 128, 75 us.
 template <int D, bool WINDOW>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_fwd_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_fwd_kernel(AttnArgs<WINDOW> p) {
   constexpr int TB = KT * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t k0[TB], v0[TB], k1[TB], v1[TB];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -200,7 +209,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
           if (t2 * 32 + 8 * (i >> 2) + (i & 3) > lim) s[t2][i] = -INFINITY;
       mx = row_max(s);
     }
-    if (WINDOW && window_cuts(p, blk.lo, kpos0, KT, wave_q0 + 31)) {
+    if constexpr (WINDOW) if (window_cuts(p, blk.lo, kpos0, KT, wave_q0 + 31)) {
       const int out = my_q - p.window - kpos0 - rbase, sink = blk.lo + p.sinks - kpos0 - rbase;   // hidden: sink <= key <= out
 #pragma unroll
       for (int t2 = 0; t2 < 2; ++t2)
@@ -331,9 +340,10 @@ __device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
 // blocks of a document's first tokens come the chunks of the rows far from them.
 constexpr int kOrderBins = 2048;
 template <bool WINDOW>
-__device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
+__device__ __forceinline__ void packed_order(const AttnArgs<WINDOW>& p, int* bin) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int room = static_cast<int>(attn_packed_items(p) - 1);
+  int room = p.pk.tokens + packed_windows(p);
+  if constexpr (WINDOW) room = static_cast<int>(attn_window_items(p) - 1);
   const int group = p.heads / p.kv_heads;
   for (int i = tid; i < kOrderBins; i += 256) bin[i] = 0;
   __syncthreads();
@@ -413,7 +423,7 @@ __device__ __forceinline__ void packed_order(const PackedAttn& p, int* bin) {
 // PFLOP/s, busy 58% at 1.75 GHz); 8192 in 23, 32/8 heads, 115 us; 16384 in 160, 16/4
 // heads of 64, 41 us (48 with two workgroups per CU, here three).
 template <int D, bool ROPE, bool WINDOW>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_dq_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2, D == 64 ? 3 : 2))) attn_packed_dq_kernel(AttnArgs<WINDOW> p) {
   constexpr int KQ = 32;                     // keys per tile
   constexpr int TB = KQ * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t kbuf[2][TB], vbuf[2][TB];
@@ -493,7 +503,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
       for (int i = 0; i < 16; ++i)
         if (8 * (i >> 2) + (i & 3) > lim) sc[i] = -INFINITY;
     }
-    if (WINDOW && window_cuts(p, blk.lo, kpos0, KQ, wave_q0 + 31)) {
+    if constexpr (WINDOW) if (window_cuts(p, blk.lo, kpos0, KQ, wave_q0 + 31)) {
       const int out = my_q - p.window - kpos0 - rbase, sink = blk.lo + p.sinks - kpos0 - rbase;   // hidden: sink <= key <= out
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -562,7 +572,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 // and on long documents by the clock: 32768 tokens in 6, 8/1 heads of 128, 1287 us
 // (1.0 PFLOP/s, matrix cores busy 49% at 1.79 GHz); 8192 in 23, 32/8 heads, 137 us.
 template <int D, bool ROPE, bool WINDOW>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) attn_packed_dkdv_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2, D == 64 ? 4 : 2))) attn_packed_dkdv_kernel(AttnArgs<WINDOW> p) {
   constexpr int TB = QT * D * 2;
   __shared__ __attribute__((aligned(16))) uint8_t qg[kDkvStages][2][TB];   // per stage: Q tile, then dO tile
   __shared__ __attribute__((aligned(16))) float st[kDkvStages][2][QT];     // lse (base 2), delta
@@ -664,10 +674,14 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
 #pragma unroll
       for (int u = 0; u < 4; ++u) s[4 * jj + u] = fast_exp2(fmaf(s[4 * jj + u], c, -lsv[u]));
     }
-    // the tile straddles the diagonal, the document ends in it, or the first key's window does
-    if (q0 < grp_k0 + 31 || q0 + QT > blk.hi || (WINDOW && q0 + QT > grp_k0 + p.window)) {
+    bool cuts = q0 < grp_k0 + 31 || q0 + QT > blk.hi;      // the tile straddles the diagonal, or the document ends in it
+    int last = blk.hi;
+    if constexpr (WINDOW) {
+      cuts = cuts || q0 + QT > grp_k0 + p.window;
+      if (my_key >= sink_end) last = min(last, my_key + p.window);
+    }
+    if (cuts) {
       // visible query rows r (relative to the lane's first row): lo <= r <= hi
-      const int last = WINDOW && my_key >= sink_end ? min(blk.hi, my_key + p.window) : blk.hi;
       const int lo = (key_ok ? my_key - q0 : QT) - rbase, hi = last - 1 - q0 - rbase;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -828,7 +842,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
 // Four slices of 32768 rows and one head of 128: 29 us for 151 MB.  It runs wherever a
 // block may be cut, as only the GPU knows the documents: 5 us where few or none are.
 template <int D, bool ROPE, bool WINDOW>
-__global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(256) attn_packed_reduce_kernel(AttnArgs<WINDOW> p) {
   const int hk = static_cast<int>(blockIdx.y), lane = static_cast<int>(threadIdx.x) & 63, at = static_cast<int>(blockIdx.x) / 4;
   const SeqBlock blk = p.cut_rows ? block_at(p.pk, at * 128, lane) : seq_block(p.pk, at, 128, lane);
   if (blk.row0 >= blk.hi) return;
@@ -886,7 +900,7 @@ __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(PackedAttn p) {
 // kv head, a wave per first token and tensor, sixteen loads in flight (one load after another:
 // 51 us for 48 parts of four slices).
 template <int D>
-__global__ void __launch_bounds__(256) attn_sink_reduce_kernel(PackedAttn p) {
+__global__ void __launch_bounds__(256) attn_sink_reduce_kernel(WindowAttn p) {
   constexpr int N = D / 64, L = 16;      // columns per lane; loads in flight
   const int lane = static_cast<int>(threadIdx.x) & 63, hk = static_cast<int>(blockIdx.y);
   const int part0 = static_cast<int>(blockIdx.x), base = (part0 + 1) * p.far_chunk;
@@ -939,7 +953,7 @@ int packed_hpb(int heads, int kv_heads) {
 }
 
 template <int D, bool ROPE, bool WINDOW>
-hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
+hipError_t packed_launch(AttnArgs<WINDOW>& p, int part, hipStream_t stream) {
   if (part == 0 || part == 2) {
     p.hpb = packed_hpb(p.heads, p.kv_heads);
     p.n_slots = static_cast<int32_t>(packed_slots(p, 128 / p.hpb));
@@ -947,7 +961,10 @@ hipError_t packed_launch(PackedAttn& p, int part, hipStream_t stream) {
     if (part == 0) hipLaunchKernelGGL((attn_packed_fwd_kernel<D, WINDOW>), grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((attn_packed_dq_kernel<D, ROPE, WINDOW>), grid, dim3(256), 0, stream, p);
   } else if (part == 1) {
-    const unsigned blocks = static_cast<unsigned>(attn_packed_places(p)) * p.kv_heads;
+    int64_t places;
+    if constexpr (WINDOW) places = attn_window_places(p);
+    else places = attn_packed_places(p);
+    const unsigned blocks = static_cast<unsigned>(places) * p.kv_heads;
     hipLaunchKernelGGL((attn_packed_dkdv_kernel<D, ROPE, WINDOW>), dim3(blocks), dim3(512), 0, stream, p);
   } else if (part == 3) {
     if (p.n_split == 1) return hipSuccess;

@@ -273,34 +273,44 @@ struct PackedAttn {
   int32_t n_split, cut_rows;
   int32_t list_steps;       // blocks of keys that a thread of the listing workgroup counts at most
   const float2* rope;       // null, or rope_table's rows: dq and dk are turned back by them before they are rounded
-  int32_t* items;           // attn_packed_items(p) x 8 bytes (16 with a window), written by the dQ pass: its blocks of keys in order
+  int32_t* items;           // attn_packed_items(pk.tokens) x 8 bytes, written by the dQ pass: its blocks of keys in order
   float* dkv_partial;       // n_split > 1: dK [n_split][tokens][kv_heads][d_h], then dV
-  // A row sees the `window` rows up to itself and its document's first `sinks`; window 0: no
-  // window.  dK/dV, set by attn_window_plan: the queries more than far_rows behind a
-  // document's start meet its first rows in chunks of far_chunk rows of the whole array.
-  // Documents share no chunk there, and the chunk before a document's first one is no other
-  // document's and takes its first rows' own part: far_rows >= 2 far_chunk.
-  int32_t window, sinks;
-  int32_t far_rows, far_chunk, far_parts;   // far_parts: chunks, 0: no document has far rows
-  float* sink_partial;      // far_parts > 0: dK [far_parts][n_split][kv_heads][sinks][d_h], then dV
 };
 void attn_packed_plan(PackedAttn* p);                                      // from pk, heads and kv_heads
-void attn_window_plan(PackedAttn* p);            // from tokens, window and sinks, before attn_packed_plan
 int attn_packed_most_splits(int64_t tokens, int64_t heads, int64_t kv_heads);   // over every packing of the tokens
 bool attn_packed_fits(const PackedAttn& p);      // every launch within the grid limits
 int64_t attn_packed_places(const PackedAttn& p); // workgroups per kv head of the dK/dV pass: at least as many as its list is long
 hipError_t attn_packed_fwd(PackedAttn p, hipStream_t stream);
+inline int64_t attn_packed_items(int64_t tokens) { return tokens ? 1 + tokens + (tokens + 127) / 128 : 0; }
+// part 2: dQ and delta; 1: dK, dV (after part 2); 3: the sum of the slices (n_split > 1).
+hipError_t attn_packed_bwd(PackedAttn p, int part, hipStream_t stream);
+
+// A row sees the `window` rows up to itself and its document's first `sinks`.  In dK/dV the
+// queries more than far_rows behind a document's start meet its first rows in chunks of
+// far_chunk rows of the whole array.  Documents share no chunk there, and the chunk before a
+// document's first one is no other document's and takes its first rows' own part: far_rows
+// >= 2 far_chunk.  `items` has 16 bytes an entry.
+struct WindowAttn : PackedAttn {
+  int32_t window, sinks;
+  // set by attn_window_chunks from tokens, window and sinks
+  int32_t far_rows, far_chunk, far_parts;   // far_parts: chunks, 0: no document has far rows
+  float* sink_partial;      // far_parts > 0: dK [far_parts][n_split][kv_heads][sinks][d_h], then dV
+};
+void attn_window_chunks(WindowAttn* p);
+void attn_window_plan(WindowAttn* p);            // as attn_packed_plan, after the chunks
+bool attn_window_fits(const WindowAttn& p);
+int64_t attn_window_places(const WindowAttn& p);
 // Blocks of first rows times the chunks of far rows: at most that many pairs.
-__host__ __device__ inline int64_t attn_far_items(const PackedAttn& p) {
+__host__ __device__ inline int64_t attn_far_items(const WindowAttn& p) {
   return static_cast<int64_t>(p.far_parts) * ((p.sinks + 127) / 128);
 }
-__host__ __device__ inline int64_t attn_packed_items(const PackedAttn& p) {
+__host__ __device__ inline int64_t attn_window_items(const WindowAttn& p) {
   const int64_t tokens = p.pk.tokens;
   return tokens ? 1 + tokens + (tokens + 127) / 128 + attn_far_items(p) : 0;
 }
-// part 2: dQ and delta; 1: dK, dV (after part 2); 3: the sum of the slices (n_split > 1);
-// 4: the sum of the first rows' parts (far_parts > 0, after part 3).
-hipError_t attn_packed_bwd(PackedAttn p, int part, hipStream_t stream);
+hipError_t attn_window_fwd(WindowAttn p, hipStream_t stream);
+// Parts as above, and 4: the sum of the first rows' parts (far_parts > 0, after part 3).
+hipError_t attn_window_bwd(WindowAttn p, int part, hipStream_t stream);
 
 // ---------------------------------------------------------------- rotary positions
 
