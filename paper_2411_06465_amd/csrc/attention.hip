@@ -1215,38 +1215,45 @@ static int64_t window_rows(const WindowAttn& p) {
   const int64_t tokens = p.pk.tokens;
   return std::min<int64_t>(tokens, std::max(127 + p.window, p.sinks ? p.far_rows : 0));
 }
-// With a window the blocks are about equally long, so that what counts is how many rounds
-// they make, each as long as a block's tiles (0.9 us each), against the sums of the slices.
+// With a window the blocks are about equally long, so that what counts is how many rounds they
+// make, each as long as a block's tiles (0.9 us each), against the sums of the slices: fp32
+// written and read, and a launch.  All blocks in slices (few blocks), or every eighth one by
+// two, which fills a last round that is part empty.  Forward and backward without and with every
+// eighth cut, window 1024, 32/8 heads of 128: 8192 tokens in 5 documents, 1.4 rounds of blocks, 618
+// and 611 us; 6000 in 3 (1.1) 499, 476; 8192 in 3 (1.6) 627, 636: not from there on; window 2048,
+// 16/4 heads, 12000 in 2 (1.2), all in four slices 873, every eighth 819.
 // 32768 tokens in 2 documents, window 4096, 8/1 heads of 128, forward and backward in 1, 2, 4
 // slices: 2187, 2216, 2222 us; 128 tokens in 3, window 16, 4/2 heads of 64, in 1 and 2: 28.0, 31.3.
-static int window_splits(const WindowAttn& p) {
-  const int64_t tokens = p.pk.tokens, n_seqs = std::max(p.pk.n_seqs, 1), group = p.heads / p.kv_heads;
-  const int64_t at_once = p.d_h == 128 ? 256 : 512;
-  // in whole blocks: those whose window the document's end cuts are half as long on average
-  const double blocks = (tokens / 128.0 - n_seqs * std::min<double>(p.window, tokens / n_seqs) / 256) * p.kv_heads;
-  const double tiles = std::min<double>(p.window + 128, static_cast<double>(tokens) / n_seqs + QT) / QT * group;
-  int best = 1;
-  double least = 1e30;
-  for (int n = 1; n <= packed_hpb(p.heads, p.kv_heads); n *= 2) {
-    const double sums = n > 1 ? 6.0 + 16e-6 * n * tokens * p.kv_heads * p.d_h / 4.8 : 0.0;
-    const double us = std::ceil(blocks * n / at_once) * (0.9 * tiles / n + 5.0) + sums;
-    if (us < least) least = us, best = n;
-  }
-  return best;
-}
 void attn_window_plan(WindowAttn* p) {
   const int64_t tokens = p->pk.tokens, n_seqs = std::max(p->pk.n_seqs, 1), group = p->heads / p->kv_heads;
-  p->cut_rows = 0;
+  const bool few = std::min(tokens / 128 + n_seqs, tokens) * p->kv_heads < 512;
+  p->cut_rows = p->cut_mask = 0;
+  p->n_split = 1;
   p->list_steps = static_cast<int32_t>(tokens / 128 + p->pk.n_seqs / 256 + 1 + attn_far_items(*p));
-  if (std::min(tokens / 128 + n_seqs, tokens) * p->kv_heads < 512) {
-    p->n_split = window_splits(*p);
+  // in whole blocks: those whose window the document's end cuts are half as long on average
+  const double at_once = p->d_h == 128 ? 256.0 : 512.0;
+  const double blocks = (tokens / 128.0 - n_seqs * std::min<double>(p->window, tokens / n_seqs) / 256) * p->kv_heads / at_once;
+  const double tiles = std::min<double>(p->window + 128, static_cast<double>(tokens) / n_seqs + QT) / QT * group;
+  const double sums = 16e-6 * tokens * p->kv_heads * p->d_h / 4.8;      // of one slice, us
+  double least = std::ceil(blocks) * (0.9 * tiles + 5.0);
+  for (int n = 2; few && n <= packed_hpb(p->heads, p->kv_heads); n *= 2) {
+    const double us = std::ceil(blocks * n) * (0.9 * tiles / n + 5.0) + 6.0 + n * sums;
+    if (us < least) least = us, p->n_split = n;
+  }
+  if (group % 2 == 0 && blocks > 1.0 && (blocks + 0.3) * (0.9 * tiles + 5.0) + 6.0 + sums / 4 < least) {
+    p->n_split = 2;
+    p->cut_mask = 7;
+    p->cut_rows = std::max(128, (p->window + 128) / 2);
     return;
   }
-  // as attn_packed_plan: the blocks with more tiles than a CU would get on average are cut by two
+  if (few || group % 2) return;
+  // documents of other lengths: as attn_packed_plan, blocks with more tiles than a CU would get on average
   const double even = static_cast<double>(tokens) / 128 * std::min(tokens / (2.0 * n_seqs), p->window + 64.0) * p->heads / QT / 256;
   const int64_t most = static_cast<int64_t>(std::min(std::max(64.0, even), 1e9)) / group;
-  p->cut_rows = static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(most * QT + 1, 128), INT32_MAX));
-  p->n_split = group % 2 == 0 && window_rows(*p) >= p->cut_rows ? 2 : 1;
+  const int64_t rows = std::max<int64_t>(most * QT + 1, 128);
+  if (window_rows(*p) < rows) return;
+  p->cut_rows = static_cast<int32_t>(std::min<int64_t>(rows, INT32_MAX));
+  p->n_split = 2;
 }
 int64_t attn_window_places(const WindowAttn& p) {
   return attn_packed_places(p) + attn_far_items(p) * (p.cut_rows ? 1 : p.n_split);

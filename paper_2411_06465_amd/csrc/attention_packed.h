@@ -88,6 +88,16 @@ __device__ __forceinline__ SeqBlock query_block(const AttnArgs<WINDOW>& p, int i
 // WINDOW kernels: key j of a document is visible to query i >= j where i - j < window or
 // j is one of the document's first `sinks` rows.  A block of queries walks the tiles of the
 // first rows, then those from its first row's window on; the tiles between are never read.
+// Masks cost a tile at either end of the window, and one for the first rows.
+//
+// Bound as the causal kernels are, with the ends of the windows on top.  32768 tokens in 2,
+// window 4096, 4 first rows, 8/1 heads of 128: forward 482 us, dQ 672, dK/dV 1004, 1.0, 1.1 (three
+// products) and 1.0 PFLOP/s (four); 8192 in 5, window 1024, 32/8 heads: 133, 178, 255; 16384 in
+// 100, window 128, 16/4 heads of 64: 35, 47, 61, most of it the way to the first products.
+// Tried and dropped: first rows and window in one walk of keys (a tile fewer, but tiles
+// that start anywhere: forward 2% faster with heads of 128, 8% slower with 64, dQ 2% slower);
+// neighbouring blocks on one XCD where kv heads are few (traffic behind the L2s down to a
+// third, times within 4% either way).
 struct KeyTiles {
   int head, skip, n;     // tiles of the first rows; tiles left out behind them; tiles to walk
   // first key of tile t, from the document's first row on
@@ -318,10 +328,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 // windows are listed, and the pass that adds them up finds every cut block from its window.
 __host__ __device__ __forceinline__ int packed_windows(const PackedAttn& p) { return (p.pk.tokens + 127) / 128; }
 
-// Slices of a kv head's query heads that the keys of a block get whose document goes
-// on for n_rows rows from the block's first one: see attn_packed_plan.
-__device__ __forceinline__ int packed_slices(const PackedAttn& p, int n_rows) {
-  return n_rows >= p.cut_rows ? p.n_split : 1;
+// Slices of a kv head's query heads that the keys of the block from row0 on get, whose document
+// goes on for n_rows rows from there (with a window: block_rows): see attn_packed_plan.
+template <bool WINDOW>
+__device__ __forceinline__ int packed_slices(const AttnArgs<WINDOW>& p, int row0, int n_rows) {
+  bool cut = n_rows >= p.cut_rows;
+  if constexpr (WINDOW) cut = cut && (row0 >> 7 & p.cut_mask) == 0;
+  return cut ? p.n_split : 1;
 }
 
 // Workgroup 0 of the dQ pass lists the blocks of keys for the dK/dV pass, longest
@@ -358,7 +371,7 @@ __device__ __forceinline__ void packed_order(const AttnArgs<WINDOW>& p, int* bin
         visit(lo, hi, row0, q0, n_rows, static_cast<int>(__float_as_uint(work) >> 17) - (127 << 6), n);
       };
       for (int row0 = lo; row0 < hi && left > 0; row0 += 128, --left) {
-        const int n_rows = block_rows<WINDOW>(p, lo, hi, row0), slices = packed_slices(p, n_rows);
+        const int n_rows = block_rows<WINDOW>(p, lo, hi, row0), slices = packed_slices<WINDOW>(p, row0, n_rows);
         add(row0, row0, n_rows, slices, p.cut_rows ? slices : 1);
       }
       if constexpr (WINDOW)
@@ -598,7 +611,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(D == 6
   const struct { int row0, q0, hi; } blk{item.x & INT32_MAX, WINDOW ? item.y : item.x & INT32_MAX, item.z};
   const int n_rows = blk.hi - blk.q0, n_qt = (n_rows + QT - 1) / QT;
   const bool far = WINDOW && blk.q0 != blk.row0;      // rows far from first tokens: their sums go in a part
-  const int slices = far ? (p.cut_rows ? 1 : p.n_split) : packed_slices(p, n_rows);
+  const int slices = far ? (p.cut_rows ? 1 : p.n_split) : packed_slices<WINDOW>(p, blk.row0, n_rows);
   const int hps = group / slices, head0 = hk * group + split * hps;
   const int grp_k0 = blk.row0 + grp * 32;
   const int my_key = grp_k0 + (lane & 31);
@@ -846,7 +859,7 @@ __global__ void __launch_bounds__(256) attn_packed_reduce_kernel(AttnArgs<WINDOW
   const int hk = static_cast<int>(blockIdx.y), lane = static_cast<int>(threadIdx.x) & 63, at = static_cast<int>(blockIdx.x) / 4;
   const SeqBlock blk = p.cut_rows ? block_at(p.pk, at * 128, lane) : seq_block(p.pk, at, 128, lane);
   if (blk.row0 >= blk.hi) return;
-  const int n_rows = blk.hi - blk.row0, slices = packed_slices(p, block_rows<WINDOW>(p, blk.lo, blk.hi, blk.row0));
+  const int n_rows = blk.hi - blk.row0, slices = packed_slices<WINDOW>(p, blk.row0, block_rows<WINDOW>(p, blk.lo, blk.hi, blk.row0));
   if (slices == 1) return;
   const int64_t step = static_cast<int64_t>(p.pk.tokens) * p.kv_heads * D;
   constexpr int C = D / 8, R = 256 / C;                  // rows at a time
@@ -916,7 +929,7 @@ __global__ void __launch_bounds__(256) attn_sink_reduce_kernel(WindowAttn p) {
     const float* src = p.sink_partial + which * half + (static_cast<int64_t>(part0) * p.n_split * p.kv_heads + hk) * p.sinks * D +
                        static_cast<int64_t>(row) * D + lane * N;
     // the own part's slices, then those of every far part
-    const int own = packed_slices(p, block_rows<true>(p, s.lo, s.hi, s.lo + row / 128 * 128));
+    const int row0 = s.lo + row / 128 * 128, own = packed_slices<true>(p, row0, block_rows<true>(p, s.lo, s.hi, row0));
     const int n = p.cut_rows ? parts : parts * p.n_split;
     const int64_t far_step = p.cut_rows ? p.n_split * step : step;
     float v[N];

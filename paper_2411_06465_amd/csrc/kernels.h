@@ -294,6 +294,7 @@ struct WindowAttn : PackedAttn {
   int32_t window, sinks;
   // set by attn_window_chunks from tokens, window and sinks
   int32_t far_rows, far_chunk, far_parts;   // far_parts: chunks, 0: no document has far rows
+  int32_t cut_mask;         // with cut_rows: of the blocks that long only those are cut whose first row / 128 has none of these bits
   float* sink_partial;      // far_parts > 0: dK [far_parts][n_split][kv_heads][sinks][d_h], then dV
 };
 void attn_window_chunks(WindowAttn* p);

@@ -176,6 +176,19 @@ def test_long_blocks_cut_among_many_short_ones(d, window, sinks):
         compare(part, q[:, hq], k[:, hk], v[:, hk], do[:, hq], starts, window, sinks, fill=7.0)
 
 
+@pytest.mark.parametrize("sinks", [0, 200])
+def test_every_eighth_block_cut(sinks):
+    """As many blocks as fill the chip once and a part: every eighth is cut; two of the 16 kv heads are compared."""
+    starts, a, g, d = starts_of([1400, 30, 1530], 0), 32, 16, 128
+    n, win = starts[-1] + 5, L.make_window(512, sinks)
+    q, k, v, do = (t.cuda() for t in draw(n, a, g, d, 33))
+    out = run(win, q, k, v, do, packing(starts, n), fill=7.0)
+    for h in (0, 9):
+        hq, hk = slice(2 * h, 2 * h + 2), slice(h, h + 1)
+        part = {t: x[hq] if t == "lse" else x[:, hk if t in ("dk", "dv") else hq] for t, x in out.items()}
+        compare(part, q[:, hq], k[:, hk], v[:, hk], do[:, hq], starts, 512, sinks, fill=7.0)
+
+
 @pytest.mark.parametrize("window", [500, 501, 1 << 40])
 def test_a_window_of_all_rows_is_no_window(window):
     starts, n = starts_of([90, 210, 0, 150]), 500

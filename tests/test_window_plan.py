@@ -20,7 +20,8 @@ class WindowAttn(C.Structure):
                                          "dq", "dk", "dv", "dq_ld", "dk_ld", "dv_ld", "delta", "lse2")] + \
                [("n_split", C.c_int32), ("cut_rows", C.c_int32), ("list_steps", C.c_int32), ("rope", C.c_int64),
                 ("items", C.c_int64), ("dkv_partial", C.c_int64)] + \
-               [(n, C.c_int32) for n in ("window", "sinks", "far_rows", "far_chunk", "far_parts")] + [("sink_partial", C.c_int64)]
+               [(n, C.c_int32) for n in ("window", "sinks", "far_rows", "far_chunk", "far_parts", "cut_mask")] + \
+               [("sink_partial", C.c_int64)]
 
 
 def plan(starts, tokens, heads, kv, d, window, sinks):
@@ -36,8 +37,8 @@ def plan(starts, tokens, heads, kv, d, window, sinks):
     return p, places(C.byref(p))
 
 
-def slices(p, rows):
-    return p.n_split if rows >= p.cut_rows else 1
+def slices(p, row0, rows):
+    return p.n_split if rows >= p.cut_rows and not row0 >> 7 & p.cut_mask else 1
 
 
 def replay(starts, tokens, heads, kv, d, window, sinks):
@@ -50,7 +51,7 @@ def replay(starts, tokens, heads, kv, d, window, sinks):
             first = row0 - lo < sinks
             end = min(hi, lo + p.far_rows) if first else min(hi, row0 + 127 + window)
             steps[i % 256] += 1
-            cut = slices(p, end - row0)
+            cut = slices(p, row0, end - row0)
             n_items += cut if p.cut_rows else 1
             if p.cut_rows and cut > 1:
                 assert hi - row0 >= 128              # found from its 128-row window by the pass that adds the slices
@@ -102,6 +103,14 @@ def test_the_chunks_of_far_rows():
         if window < tokens:
             far += replay(starts, tokens, heads, kv, rng.choice([64, 128]), window, sinks)
     assert far > 100
+
+
+def test_every_eighth_block_is_cut_where_a_round_is_part_empty():
+    starts = [0, 2000, 4000, 6000]
+    p, _ = plan(starts, 6000, 32, 8, 128, 1024, 4)
+    assert p.cut_mask == 7 and p.n_split == 2
+    replay(starts, 6000, 32, 8, 128, 1024, 4)
+    assert plan([0, 8192], 8192, 32, 8, 128, 1024, 4)[0].n_split == 1
 
 
 def test_documents_at_the_border_of_the_far_rows():
