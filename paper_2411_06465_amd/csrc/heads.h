@@ -15,7 +15,7 @@ namespace {
 // over a head are a few exchanges within the group.  V elements are 16 bytes, in bf16 8, in
 // fp32 4 (16 heads of 128 on 4099 rows, half of each rotated, forward and backward: 80 us; with
 // units of 8 pairs, whose loads leave gaps between the lanes, 97); any other alignment takes
-// single pairs (heads of 100 in bf16 about 2.5 times the time of those of 96).
+// single pairs (heads of 100 in bf16 take 2.3 times the time of those of 96).
 template <typename T, int V, int K, bool INTER>
 struct HeadLane {
   int a[K], b[K], pair[K];     // the unit's two vectors; its first pair, -1: not rotated
