@@ -540,7 +540,7 @@ int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void
  * Also L4D_EINVAL: window < 1, sinks outside 0 .. 4096, more than 2^28 rows (with a
  * window of fewer rows).
  * The workspace is that of attn_packed_bwd, 8 bytes per row more, and fp32 sums of dk
- * and dv of the first tokens for every 512 rows (for more than 512 sinks, as many rows).
+ * and dv of the first tokens for every 128 to 512 rows (more than 512 sinks: as many rows).
  * ---------------------------------------------------------------------- */
 typedef struct {
   int64_t window;       /* rows that a row sees, itself among them */
