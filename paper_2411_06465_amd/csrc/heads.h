@@ -15,7 +15,7 @@ namespace {
 // over a head are a few exchanges within the group.  V elements are 16 bytes, in bf16 8, in
 // fp32 4 (16 heads of 128 on 4099 rows, half of each rotated, forward and backward: 80 us; with
 // units of 8 pairs, whose loads leave gaps between the lanes, 97); any other alignment takes
-// single pairs (heads of 100 in bf16 take 2.3 times the time of those of 96).
+// single pairs (heads of 100 in bf16 take 1.7 times the time of those of 96).
 template <typename T, int V, int K, bool INTER>
 struct HeadLane {
   int a[K], b[K], pair[K];     // the unit's two vectors; its first pair, -1: not rotated
@@ -83,12 +83,12 @@ __device__ __forceinline__ bool row_angles(const RopeRotate& r, int row, int lan
 
 // Bound by memory, one read and one write of the heads: 32/8 heads of 128 in bf16 on 8192 rows
 // 33 us (5.1 TB/s).
-template <typename T, int V>
-constexpr int kNormFlight = V == 1 ? 1 : 4;      // heads in flight per lane
+template <int K>
+constexpr int kNormFlight = K == 1 ? 4 : 1;      // heads in flight per lane
 
 template <typename T, int V, int K, bool INTER>
 __global__ void __launch_bounds__(256) qk_norm_fwd_kernel(QkNorm p) {
-  constexpr int F = kNormFlight<T, V>;
+  constexpr int F = kNormFlight<K>;
   __shared__ __attribute__((aligned(16))) float2 table[4][kMaxRopePairs];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = static_cast<int>(blockIdx.x) * 4 + wave;
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(256) qk_norm_fwd_kernel(QkNorm p) {
 // registers), two heads in flight per lane 74 (154 registers), 88 spilled into 128.
 template <typename T, int V, int K, bool INTER>
 __global__ void __launch_bounds__(kQkNormWaves * 64) __attribute__((amdgpu_waves_per_eu(4, 4))) qk_norm_bwd_kernel(QkNorm p) {
-  constexpr int F = sizeof(T) == 4 && V > 1 ? 2 : 1, E = 2 * V;
+  constexpr int F = V < 8 && K == 1 ? 2 : 1, E = 2 * V;
   extern __shared__ __attribute__((aligned(16))) float2 shared_lds[];       // angles of every wave, then its sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const HeadLane<T, V, K, INTER> at(p.r.d_h, p.r.rot, lane % p.group, p.group);
@@ -419,6 +419,13 @@ hipError_t norm_launch(const QkNorm& p, dim3 grid, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Single pairs: as few per lane as cover a head.
+template <typename T>
+hipError_t norm_pairs(const QkNorm& p, int units, dim3 grid, hipStream_t stream) {
+  if (units <= 64) return norm_launch<T, 1, 1>(p, grid, stream);
+  return units <= 128 ? norm_launch<T, 1, 2>(p, grid, stream) : norm_launch<T, 1, 4>(p, grid, stream);
+}
+
 template <typename T>
 hipError_t dropout_launch(const DropoutAdd& p, bool vec, dim3 grid, hipStream_t stream) {
   if (vec && p.residual) hipLaunchKernelGGL((dropout_kernel<T, true>), grid, dim3(256), 0, stream, p);
@@ -448,21 +455,20 @@ hipError_t qk_norm_rope(const QkNorm& params, hipStream_t stream) {
           (!p.backward || aligned16(p.dy[t], p.dy_ld[t], size));
   }
   p.inv_d = 1.f / static_cast<float>(p.r.d_h);
-  p.group = 64;
-  if (vec)
-    for (p.group = 1; p.group < p.r.d_h / unit;) p.group *= 2;
+  const int units = p.r.d_h / (vec ? unit : 2);
+  for (p.group = 1; p.group < std::min(units, 64);) p.group *= 2;
   p.r.parts = 1;
   dim3 grid(static_cast<unsigned>(qk_norm_parts(p.r.tokens)), static_cast<unsigned>(p.r.n_tensors));
   if (!p.backward) {
-    const int at_once = (vec ? kNormFlight<uint16_t, 8> : 1) * (64 / p.group);
+    const int at_once = (units <= 64 ? kNormFlight<1> : 1) * (64 / p.group);
     int most = p.r.t[0].heads;
     if (p.r.n_tensors > 1) most = std::max(most, p.r.t[1].heads);
     // waves per row: as rope_rotate
     while (static_cast<int64_t>(p.r.tokens) * p.r.parts * 2 <= 8192 && most > at_once * p.r.parts) p.r.parts *= 2;
     grid = dim3(static_cast<unsigned>((p.r.tokens + 3) / 4), static_cast<unsigned>(p.r.parts));
   }
-  if (p.r.f32) return vec ? norm_launch<float, 4, 1>(p, grid, stream) : norm_launch<float, 1, 4>(p, grid, stream);
-  return vec ? norm_launch<uint16_t, 8, 1>(p, grid, stream) : norm_launch<uint16_t, 1, 4>(p, grid, stream);
+  if (vec) return p.r.f32 ? norm_launch<float, 4, 1>(p, grid, stream) : norm_launch<uint16_t, 8, 1>(p, grid, stream);
+  return p.r.f32 ? norm_pairs<float>(p, units, grid, stream) : norm_pairs<uint16_t>(p, units, grid, stream);
 }
 
 hipError_t dropout_add(const DropoutAdd& params, hipStream_t stream) {
