@@ -535,8 +535,8 @@ int attn_packed_bwd(const l4d_attn* attn, const l4d_packing* packing, const void
  * attn_packed_fwd / attn_packed_bwd where row i of a document (counted from its first
  * row) sees row j <= i iff i - j < window or j < sinks: the last `window` rows up to
  * itself, and the document's first `sinks`.  Arguments, layouts, rounding and refusals are
- * those of the calls above; keys that no row of a block of queries sees are not read.  A
- * window of at least packing->tokens hides nothing, and the call then is the one above, in every bit.
+ * those of the calls above; tiles of keys that no row of a block of queries sees are not
+ * read.  A window of at least packing->tokens hides nothing, and the call then is the one above, in every bit.
  * Also L4D_EINVAL: window < 1, sinks outside 0 .. 4096, more than 2^28 rows (with a
  * window of fewer rows).
  * The workspace is that of attn_packed_bwd, 8 bytes per row more, and fp32 sums of dk

@@ -73,6 +73,9 @@ CASES = [  # rows, cols, dtype, p, first row, seed, offset
     (7, 1023, F32, 0.35, 0, 9, 9),
     (7, 1023, BF16, 0.35, 1 << 33, 9, 9),
     (64, 4, BF16, 0.5, 1, 9, 9),
+    (33, 101, F32, 0.5, 1, 9, 9),                       # units that start 1, 2 and 3 places into a counter
+    (33, 102, BF16, 0.5, 1, 9, 9),
+    (33, 103, BF16, 0.5, 1, 9, 9),
     (5, 1000, BF16, 1.0 - 2.0 ** -31, 0, 9, 9),         # all but one in 2^31 dropped
     (3, 2048, BF16, 0.25, (1 << 38) - 1, 11, 4),        # counters of more than 32 bits
 ]

@@ -129,6 +129,9 @@ NORMS = [  # lens, first, tail, heads, kv heads, d, rot, layout, dtype, pairs of
     ([60], 0, 1, 3, 1, 50, 26, "half", BF16, None),              # no whole vectors
     ([60], 0, 1, 3, 1, 510, 510, "half", F32, (100, 100, 55)),
     ([7, 9], 0, 1, 2, 1, 2, 2, "interleaved", F32, None),
+    ([40], 1, 2, 3, 1, 198, 198, "half", F32, None),             # two pairs a lane
+    ([40], 0, 2, 5, 2, 130, 66, "interleaved", BF16, None),
+    ([33], 0, 0, 7, 3, 30, 30, "half", BF16, None),              # four heads a wave
     ([5000], 10, 20, 2, 1, 64, 64, "half", BF16, None),          # more rows than waves of the backward
 ]
 
