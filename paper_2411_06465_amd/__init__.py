@@ -604,14 +604,14 @@ def qk_norm_rope_bwd(rope, q, q_gain, dq_out, dq, d_q_gain, arena, k=None, k_gai
     import torch
     dtype, tokens, d, f32 = q.dtype, q.shape[0], rope.head_dim, _float_type("q", q)
 
-    def heads(name, x, gain, dy, dx, dg):
-        shape, ld = _norm_rows(name, x, dtype, tokens, d, q)
-        dy_ld, dx_ld = _rows(f"d{name}_out", dy, dtype, shape, q), _rows(f"d{name}", dx, dtype, shape, q)
-        return NormHeadsGrad(x.data_ptr(), _norm_gain(f"{name}_gain", gain, dtype, d, q), dy.data_ptr(), dx.data_ptr(),
-                             _norm_gain(f"d_{name}_gain", dg, torch.float32, d, q), shape[1], ld, dy_ld, dx_ld)
+    def heads(names, x, gain, dy, dx, dg):
+        shape, ld = _norm_rows(names[0], x, dtype, tokens, d, q)
+        dy_ld, dx_ld = _rows(names[1], dy, dtype, shape, q), _rows(names[2], dx, dtype, shape, q)
+        return NormHeadsGrad(x.data_ptr(), _norm_gain(names[3], gain, dtype, d, q), dy.data_ptr(), dx.data_ptr(),
+                             _norm_gain(names[4], dg, torch.float32, d, q), shape[1], ld, dy_ld, dx_ld)
 
-    io = heads("q", q, q_gain, dq_out, dq, d_q_gain)
-    io_k = None if k is None else heads("k", k, k_gain, dk_out, dk, d_k_gain)
+    io = heads(("q", "dq_out", "dq", "q_gain", "d_q_gain"), q, q_gain, dq_out, dq, d_q_gain)
+    io_k = None if k is None else heads(("k", "dk_out", "dk", "k_gain", "d_k_gain"), k, k_gain, dk_out, dk, d_k_gain)
     _launch(lib().qk_norm_rope_bwd, q, stream, rope, axes, f32, tokens,
             None if packing is None else _on_one_device(packing, q), _positions(axes, positions, tokens, q), eps, io, io_k,
             arena.h)
