@@ -91,8 +91,8 @@ __device__ __forceinline__ SeqBlock query_block(const AttnArgs<WINDOW>& p, int i
 // Masks cost a tile at either end of the window, and one for the first rows.
 //
 // Bound as the causal kernels are, with the ends of the windows on top.  32768 tokens in 2,
-// window 4096, 4 first rows, 8/1 heads of 128: forward 482 us, dQ 672, dK/dV 1004, 1.0, 1.1 (three
-// products) and 1.0 PFLOP/s (four); 8192 in 5, window 1024, 32/8 heads: 133, 178, 255; 16384 in
+// window 4096, 4 first rows, 8/1 heads of 128: forward 482 us, dQ 672, dK/dV 983, 1.0, 1.1 (three
+// products) and 1.0 PFLOP/s (four); 8192 in 5, window 1024, 32/8 heads: 133, 178, 250; 16384 in
 // 100, window 128, 16/4 heads of 64: 35, 47, 55, most of it the way to the first products.
 // Tried and dropped: first rows and window in one walk of keys (a tile fewer, but tiles
 // that start anywhere: forward 2% faster with heads of 128, 8% slower with 64, dQ 2% slower);
