@@ -464,7 +464,8 @@ int rope_axes_bwd(const l4d_rope* rope, const l4d_rope_axes* axes, int dtype, in
  *   dn = A R(pos)^T dy,  r = (mean(x^2) + eps)^(-1/2),  d_gain += sum of dn x r over rows and heads,
  *   dx = r (dn g - x r^2 mean(dn g x)).
  * Everything between is fp32, outputs are rounded once; the sums of d_gain have a fixed order.
- * Squares that add up beyond fp32 (elements above 1e18) make r 0.
+ * Where a head's squares add up beyond fp32 (3.4e38), r is 0: its y and dx are 0, and it adds
+ * nothing to d_gain.  An infinity or NaN reaches its own head, and d_gain.
  *   x, y, dy, dx: up to two tensors [tokens][heads][head_dim] as in rope_fwd (k may be NULL);
  *   gain: [head_dim], of the call's dtype;  d_gain: f32 [head_dim] (+=);
  *   axes: NULL or the axes of positions, as above;  packing, positions: as in rope_fwd.  Rows

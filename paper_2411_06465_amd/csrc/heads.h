@@ -228,20 +228,26 @@ __global__ void __launch_bounds__(kQkNormWaves * 64) __attribute__((amdgpu_waves
             dn[k][at.second(i)] = y1 * cs[k][i].x - y0 * cs[k][i].y;
           }
 #pragma unroll
+          for (int i = 0; i < E; ++i) s1 = fmaf(v[k][i], v[k][i], s1);
+        }
+        // x is scaled before anything is multiplied by it: where its squares pass fp32, and rstd is 0,
+        // its products with dn would pass it too, and infinity x 0 reach dx and the gain's gradient
+        const float rstd = rsqrtf(group_sum(s1, p.group) * p.inv_d + p.eps);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
           for (int i = 0; i < E; ++i) {
-            s1 = fmaf(v[k][i], v[k][i], s1);
+            v[k][i] *= rstd;
             s2 = fmaf(dn[k][i] * g[k][i], v[k][i], s2);
           }
-        }
-        const float rstd = rsqrtf(group_sum(s1, p.group) * p.inv_d + p.eps);
-        const float c = group_sum(s2, p.group) * p.inv_d * rstd * rstd * rstd;
+        const float c = group_sum(s2, p.group) * p.inv_d * rstd;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
           float out[E];
 #pragma unroll
           for (int i = 0; i < E; ++i) {
             out[i] = rstd * g[k][i] * dn[k][i] - c * v[k][i];
-            dg[k][i] += ok ? dn[k][i] * v[k][i] * rstd : 0.f;
+            dg[k][i] += ok ? dn[k][i] * v[k][i] : 0.f;
           }
           if (ok && at.live[k]) {
             xa[f][k].set(out);
