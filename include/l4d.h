@@ -505,7 +505,7 @@ int qk_norm_rope_bwd(const l4d_rope* rope, const l4d_rope_axes* axes, int dtype,
  *   [tokens][n_kv_heads][head_dim]; row i of each starts at its pointer + i ld
  *   (elements), heads contiguous within a row (columns of a fused array are fine);
  *   lse: f32 [n_heads][tokens], natural logarithm, written by the forward, read by
- *   the backward.  Outputs must not overlap inputs or each other.
+ *   the backward.  Outputs must not overlap inputs or each other (rows of one array may alternate).
  * The backward overwrites dq, dk, dv with the gradients for d_o (dk and dv summed
  * over the query heads of their head); its sums have a fixed order.  A value that
  * is not finite in one document reaches no other document; within its own it may
@@ -513,7 +513,9 @@ int qk_norm_rope_bwd(const l4d_rope* rope, const l4d_rope_axes* axes, int dtype,
  * L4D_EINVAL: head_dim not 64 or 128, n_heads % n_kv_heads != 0, more than 2^16
  * heads, a scale that is negative or not finite, an ld that is smaller than the
  * heads' columns, no multiple of 8 or above 2^22, a NULL tensor or one not 16-byte
- * aligned (lse: 4), more blocks than a launch holds (2^24 blocks of rows and heads).  tokens == 0 or n_seqs == 0 launches nothing.
+ * aligned (lse: 4), an output that shares an element with another array of the call (lse and
+ * starts among them), more blocks than a launch holds (2^24 blocks of rows and heads).
+ * tokens == 0 or n_seqs == 0 launches nothing.
  * ---------------------------------------------------------------------- */
 typedef struct {
   int64_t n_heads, n_kv_heads, head_dim;

@@ -854,6 +854,17 @@ bool rows_meet(const RowRange& a, const RowRange& b) {
   const uint64_t off = b.p >= a.p ? (b.p - a.p) % a.ld : (a.ld - (a.p - b.p) % a.ld) % a.ld;   // b's column in a's rows
   return off < a.width || off + b.width > a.ld;
 }
+// The same, exact for different strides too.
+bool rows_share(const RowRange& a, const RowRange& b) {
+  if (a.ld == b.ld) return rows_meet(a, b);
+  const RowRange &few = a.n <= b.n ? a : b, &many = a.n <= b.n ? b : a;
+  for (uint64_t i = 0; i < few.n; ++i) {
+    const uintptr_t lo = few.p + i * few.ld;
+    const uint64_t j = lo < many.p + many.width ? 0 : (lo - many.p - many.width) / many.ld + 1;     // first row that ends behind lo
+    if (j < many.n && many.p + j * many.ld < lo + few.width) return true;
+  }
+  return false;
+}
 
 // f_j / 2 pi and the axis of every pair.
 int rope_axes(const l4d_rope* r, const l4d_rope_axes* x, RopeRotate* a) {
@@ -1097,6 +1108,31 @@ int attn_distinct(const AttnRows* t, int n, int first_out) {
   for (int i = first_out; i < n; ++i)
     for (int j = 0; j < i; ++j)
       if (t[i].p == t[j].p) return fail(L4D_EINVAL, "%s and %s are the same array", t[i].name, t[j].name);
+  return L4D_OK;
+}
+// Nothing a call writes (its tensors from first_out on; lse in the forward) may be read or written twice by it.
+int attn_apart(const AttnRows* t, int n, int first_out, const l4d_attn* at, const float* lse, const l4d_packing* pk) {
+  RowRange r[10];
+  const char* name[10];
+  const uint64_t rows = (uint64_t)pk->tokens, sums = 4ull * at->n_heads * rows, starts = 8ull * (pk->n_seqs + 1);
+  int m = 0;
+  for (int i = 0; i < n; ++i, ++m) {
+    r[m] = RowRange{reinterpret_cast<uintptr_t>(t[i].p), 2ull * t[i].heads * at->head_dim, 2ull * t[i].ld, rows};
+    name[m] = t[i].name;
+  }
+  r[m] = RowRange{reinterpret_cast<uintptr_t>(lse), sums, sums, 1};
+  name[m++] = "lse";
+  if (pk->starts) {
+    r[m] = RowRange{reinterpret_cast<uintptr_t>(pk->starts), starts, starts, 1};
+    name[m++] = "starts";
+  }
+  uintptr_t end[10];
+  for (int i = 0; i < m; ++i) end[i] = r[i].p + r[i].span();
+  const int last_out = n == 4 ? n : n - 1;
+  for (int j = first_out; j <= last_out; ++j)
+    for (int i = 0; i < m; ++i)
+      if (i != j && r[i].p < end[j] && r[j].p < end[i] && rows_share(r[i], r[j]))
+        return fail(L4D_EINVAL, "%s and %s overlap", name[i], name[j]);
   return L4D_OK;
 }
 // dQ first: it also writes delta, which dK/dV reads.
@@ -1877,6 +1913,7 @@ static int attn_forward(bool windowed, const l4d_window* w, const l4d_attn* at, 
   if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return fail(L4D_EINVAL, "lse is required, 4-byte aligned");
   p.pk = device_packing(pk);
   if (p.window ? !attn_window_fits(p) : !attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
+  if ((rc = attn_apart(t, 4, 3, at, lse, pk))) return rc;
   if (pk->tokens == 0 || pk->n_seqs == 0) return L4D_OK;
   p.q = static_cast<const uint16_t*>(q);
   p.k = static_cast<const uint16_t*>(k);
@@ -1917,6 +1954,7 @@ static int attn_backward(bool windowed, const l4d_window* w, const l4d_attn* at,
   if (!A) return fail(L4D_EINVAL, "arena is required");
   p.pk = device_packing(pk);
   if (p.window ? !attn_window_fits(p) : !attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
+  if ((rc = attn_apart(t, 8, 5, at, lse, pk))) return rc;
   if (pk->tokens == 0 || pk->n_seqs == 0) return L4D_OK;
   const PackedWs plan = plan_packed(p, pk->tokens);
   Workspace ws;
