@@ -394,7 +394,8 @@ typedef struct {
  *   y == x with y_ld == x_ld rotates in place; other overlaps of a tensor's input
  *   and output ranges are refused, and so is an output that shares an element with the
  *   other tensor's input or output (tensors with one stride may interleave as columns of
- *   one array; with different strides their ranges must not meet).
+ *   one array; with different strides their ranges must not meet), with positions or with
+ *   the packing's starts.
  * L4D_EINVAL: more than 2^25 tokens or 8192 heads, head_dim outside 2 .. 512, rot_dim odd or outside 2 .. head_dim, an
  * unknown enum value, base <= 1, factor <= 0, amplitude <= 0, original <= 0 or not
  * 0 < low < high where the scaling uses them, ld < heads head_dim, NULL or
@@ -471,7 +472,8 @@ int rope_axes_bwd(const l4d_rope* rope, const l4d_rope_axes* axes, int dtype, in
  *   axes: NULL or the axes of positions, as above;  packing, positions: as in rope_fwd.  Rows
  *   of no document add nothing to d_gain, and their outputs are left as they were.
  *   An output may be an input of its own tensor (same address and stride: y on x, dx on dy
- *   or x); other arrays that share an element with an output are refused.
+ *   or x); other arrays that share an element with an output are refused, positions and the
+ *   packing's starts among them.
  * The backward needs l4d_qk_norm_workspace_bytes of arena.
  * Also L4D_EINVAL: an odd head_dim, eps below 1e-30 or not finite, a NULL or misaligned gain.
  * ---------------------------------------------------------------------- */

@@ -856,7 +856,7 @@ bool rows_meet(const RowRange& a, const RowRange& b) {
 }
 // The same, exact for different strides too.
 bool rows_share(const RowRange& a, const RowRange& b) {
-  if (a.ld == b.ld) return rows_meet(a, b);
+  if (a.ld == b.ld || !rows_meet(a, b)) return rows_meet(a, b);
   const RowRange &few = a.n <= b.n ? a : b, &many = a.n <= b.n ? b : a;
   for (uint64_t i = 0; i < few.n; ++i) {
     const uintptr_t lo = few.p + i * few.ld;
@@ -925,6 +925,13 @@ int rope_setup(const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t 
   return L4D_OK;
 }
 
+// Whether a call over heads writes what its waves look up: the positions, or the documents' starts.
+bool on_lookups(const RowRange& out, const l4d_rope_axes* axes, int64_t tokens, const l4d_packing* pk, const int64_t* positions) {
+  const uint64_t n = 8ull * tokens * (axes ? axes->n_axes : 1), s = pk ? 8ull * (pk->n_seqs + 1) : 0;
+  return (positions && rows_share(out, RowRange{reinterpret_cast<uintptr_t>(positions), n, n, 1})) ||
+         (pk && pk->starts && rows_share(out, RowRange{reinterpret_cast<uintptr_t>(pk->starts), s, s, 1}));
+}
+
 int rope_call(const char* name, const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t tokens,
               const l4d_packing* pk, const int64_t* positions, const l4d_rope_heads* q, const l4d_rope_heads* k, int inverse,
               void* stream_ptr) {
@@ -952,6 +959,7 @@ int rope_call(const char* name, const l4d_rope* r, const l4d_rope_axes* axes, in
     // one launch turns both: what it writes of one tensor must be nothing it reads or writes of the other
     if (a.n_tensors && (rows_meet(ry, from[0]) || rows_meet(to[0], rx) || rows_meet(to[0], ry)))
       return fail(L4D_EINVAL, "rope: an output of q or k overlaps the other tensor");
+    if (on_lookups(ry, axes, tokens, pk, positions)) return fail(L4D_EINVAL, "rope: an output overlaps positions or starts");
     from[a.n_tensors] = rx, to[a.n_tensors] = ry;
     a.t[a.n_tensors++] = RopeHeads{t->x, t->y, t->x_ld, t->y_ld, (int32_t)t->heads};
   }
@@ -1018,6 +1026,7 @@ int norm_call(const char* name, const l4d_rope* r, const l4d_rope_axes* axes, in
     }
     for (int j = 0; j < i; ++j)
       if (rows_meet(outs[i].at, outs[j].at)) return fail(L4D_EINVAL, "qk_norm: two outputs overlap");
+    if (on_lookups(outs[i].at, axes, tokens, pk, positions)) return fail(L4D_EINVAL, "qk_norm: an output overlaps positions or starts");
   }
   if (backward && !A) return fail(L4D_EINVAL, "arena is required");
   if (pk && pk->n_seqs == 0) return L4D_OK;
