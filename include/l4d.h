@@ -399,7 +399,7 @@ typedef struct {
  * L4D_EINVAL: more than 2^25 tokens or 8192 heads, head_dim outside 2 .. 512, rot_dim odd or outside 2 .. head_dim, an
  * unknown enum value, base <= 1, factor <= 0, amplitude <= 0, original <= 0 or not
  * 0 < low < high where the scaling uses them, ld < heads head_dim, NULL or
- * misaligned tensors (element size).  tokens == 0 launches nothing.
+ * misaligned tensors (element size).  tokens == 0 launches nothing, and tensors and positions may then be NULL.
  * ---------------------------------------------------------------------- */
 enum { L4D_BF16 = 0, L4D_F32 = 1 };
 enum { L4D_ROPE_HALF = 0, L4D_ROPE_INTERLEAVED = 1 };
@@ -439,7 +439,7 @@ int rope_bwd(const l4d_rope* rope, int dtype, int64_t tokens, const l4d_packing*
  *            pairs[i], else to axis 0 (i + n_axes (pairs[i] - 1) < rot_dim/2 for i > 0);
  *   frequencies  L4D_AXES_SHARED: pair j turns with f_j of the whole head, whatever its axis;
  *            L4D_AXES_OWN: the m-th pair of an axis (from 0) with f_m of rot_dim = 2 pairs[i].
- *   positions: int64 [n_axes][tokens] device array of any sign, required.
+ *   positions: int64 [n_axes][tokens] device array of any sign, required where there are tokens.
  * All else, packing, scalings, in-place and refusals, as in rope_fwd.
  * ---------------------------------------------------------------------- */
 enum { L4D_AXES_SECTIONS = 0, L4D_AXES_CYCLED = 1 };
@@ -517,7 +517,7 @@ int qk_norm_rope_bwd(const l4d_rope* rope, const l4d_rope_axes* axes, int dtype,
  * heads' columns, no multiple of 8 or above 2^22, a NULL tensor or one not 16-byte
  * aligned (lse: 4), an output that shares an element with another array of the call (lse and
  * starts among them), more blocks than a launch holds (2^24 blocks of rows and heads).
- * tokens == 0 or n_seqs == 0 launches nothing.
+ * tokens == 0 (where tensors may be NULL) or n_seqs == 0 launches nothing.
  * ---------------------------------------------------------------------- */
 typedef struct {
   int64_t n_heads, n_kv_heads, head_dim;

@@ -912,7 +912,7 @@ int rope_setup(const l4d_rope* r, const l4d_rope_axes* axes, int dtype, int64_t 
   if (pk && (rc = check_packing(pk))) return rc;
   if (pk && pk->tokens != tokens) return fail(L4D_EINVAL, "rope: the packing is of another number of tokens");
   if (reinterpret_cast<uintptr_t>(positions) % 8) return fail(L4D_EINVAL, "rope: positions must be 8-byte aligned");
-  if (axes && !positions) return fail(L4D_EINVAL, "rope axes: positions are required");
+  if (axes && !positions && tokens > 0) return fail(L4D_EINVAL, "rope axes: positions are required");
   if ((rc = rope_axes(r, axes, a))) return rc;
   a->pk = pk ? device_packing(pk) : Packing{nullptr, -1, (int32_t)tokens};
   a->positions = positions;
@@ -939,6 +939,7 @@ int rope_call(const char* name, const l4d_rope* r, const l4d_rope_axes* axes, in
   RopeRotate a{};
   int rc = rope_setup(r, axes, dtype, tokens, pk, positions, &a);
   if (rc) return rc;
+  if (tokens == 0) return L4D_OK;                    // an empty array may have no address
   const int64_t size = dtype == L4D_F32 ? 4 : 2;
   const l4d_rope_heads* in[2] = {q, k};
   RowRange from[2], to[2];
@@ -963,7 +964,7 @@ int rope_call(const char* name, const l4d_rope* r, const l4d_rope_axes* axes, in
     from[a.n_tensors] = rx, to[a.n_tensors] = ry;
     a.t[a.n_tensors++] = RopeHeads{t->x, t->y, t->x_ld, t->y_ld, (int32_t)t->heads};
   }
-  if (tokens == 0 || (pk && pk->n_seqs == 0)) return L4D_OK;
+  if (pk && pk->n_seqs == 0) return L4D_OK;
   a.inverse = inverse;
   hipStream_t s = static_cast<hipStream_t>(stream_ptr);
   return launch(name, s, [&] { return rope_rotate(a, s); });
@@ -1916,6 +1917,7 @@ static int attn_forward(bool windowed, const l4d_window* w, const l4d_attn* at, 
   WindowAttn p{};
   if ((rc = attn_shape(at, &p))) return rc;
   if (windowed && (rc = attn_window(w, pk->tokens, &p))) return rc;
+  if (pk->tokens == 0) return L4D_OK;                // an empty array may have no address
   const AttnRows t[4] = {{"q", q, q_ld, at->n_heads}, {"k", k, k_ld, at->n_kv_heads}, {"v", v, v_ld, at->n_kv_heads},
                          {"o", o, o_ld, at->n_heads}};
   if ((rc = attn_rows(t, 4, at->head_dim)) || (rc = attn_distinct(t, 4, 3))) return rc;
@@ -1923,7 +1925,7 @@ static int attn_forward(bool windowed, const l4d_window* w, const l4d_attn* at, 
   p.pk = device_packing(pk);
   if (p.window ? !attn_window_fits(p) : !attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
   if ((rc = attn_apart(t, 4, 3, at, lse, pk))) return rc;
-  if (pk->tokens == 0 || pk->n_seqs == 0) return L4D_OK;
+  if (pk->n_seqs == 0) return L4D_OK;
   p.q = static_cast<const uint16_t*>(q);
   p.k = static_cast<const uint16_t*>(k);
   p.v = static_cast<const uint16_t*>(v);
@@ -1955,6 +1957,7 @@ static int attn_backward(bool windowed, const l4d_window* w, const l4d_attn* at,
   WindowAttn p{};
   if ((rc = attn_shape(at, &p))) return rc;
   if (windowed && (rc = attn_window(w, pk->tokens, &p))) return rc;
+  if (pk->tokens == 0) return L4D_OK;                // an empty array may have no address
   const int64_t a = at->n_heads, g = at->n_kv_heads;
   const AttnRows t[8] = {{"q", q, q_ld, a}, {"k", k, k_ld, g}, {"v", v, v_ld, g}, {"o", o, o_ld, a},
                          {"d_o", d_o, do_ld, a}, {"dq", dq, dq_ld, a}, {"dk", dk, dk_ld, g}, {"dv", dv, dv_ld, g}};
@@ -1964,7 +1967,7 @@ static int attn_backward(bool windowed, const l4d_window* w, const l4d_attn* at,
   p.pk = device_packing(pk);
   if (p.window ? !attn_window_fits(p) : !attn_packed_fits(p)) return fail(L4D_EINVAL, "problem too large");
   if ((rc = attn_apart(t, 8, 5, at, lse, pk))) return rc;
-  if (pk->tokens == 0 || pk->n_seqs == 0) return L4D_OK;
+  if (pk->n_seqs == 0) return L4D_OK;
   const PackedWs plan = plan_packed(p, pk->tokens);
   Workspace ws;
   if ((rc = take_ws(A, plan.total, ws))) return rc;
