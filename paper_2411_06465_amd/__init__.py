@@ -395,8 +395,10 @@ def _launch(entry, tensor, stream, *args):
     if stream is None:
         if device.type != "cuda":
             raise ValueError(f"the tensors are on {device}, not on a GPU")
-        # the handle alone: torch.cuda.current_stream builds an object around it, 1.8 us of a small call's 9
-        handle = torch._C._cuda_getCurrentRawStream(device.index)
+        # the handle alone, where torch hands it out: torch.cuda.current_stream builds an object around it, 1.8 us of
+        # a small call's 9
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        handle = torch.cuda.current_stream(device).cuda_stream if raw is None else raw(device.index)
     elif stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
     else:
