@@ -1199,9 +1199,13 @@ void attn_window_chunks(WindowAttn* p) {
   // Chunks of 256 rows: a far chunk of 512 rows is a tenth to a half of a block's tiles, and starts
   // last (16384 tokens, window 1024, 16/4 heads of 64, 512 blocks on 512 places: dK/dV 231 us
   // with chunks of 512, 198 of 256, 201 of 128; 32768 tokens, window 4096, 8/1 heads of 128: 1018,
-  // 1020, 1025, the sums of the parts 7, 9, 14).  Not more than half a short window, whose
-  // blocks would wait for the first one (window 128 of 100 documents: 94 us with 512, 67 with
-  // 128); more for many first tokens, whose parts have as many rows.
+  // 1020, 1025, the sums of the parts 7, 9, 14).  No more than half a short window, rounded up to
+  // 128 rows, where the blocks would wait for the first one (window 128 of 100 documents: 94 us with
+  // 512, 67 with 128); more for many first tokens, whose parts have as many rows.  On a long
+  // document a short window then has about as many chunks as blocks, each a workgroup of which a
+  // few first tokens use one group of keys in four: one document of 32768 rows, 8/1 heads of 128,
+  // dK/dV without and with 4 first tokens at windows of 16, 128, 512, 1024 and 4096 rows 56 and
+  // 113, 79 and 110, 169 and 222, 289 and 347, 1016 and 1048 us.
   const int blocks = (p->sinks + 127) / 128 * 128;
   const int chunk = std::min((std::max(p->window / 2, 4 * p->sinks) + 127) / 128 * 128, p->sinks > 64 ? 512 : 256);
   p->far_chunk = std::max(chunk, blocks);
@@ -1216,7 +1220,8 @@ static int64_t window_rows(const WindowAttn& p) {
   return std::min<int64_t>(tokens, std::max(127 + p.window, p.sinks ? p.far_rows : 0));
 }
 // With a window the blocks are about equally long, so that what counts is how many rounds they
-// make, each as long as a block's tiles (0.9 us each), against the sums of the slices: fp32
+// make, each as long as a block's tiles (0.9 us each; 0.96 measured with heads of 128, 1.13 with
+// heads of 64, two workgroups a CU: 32768 rows, window 4096), against the sums of the slices: fp32
 // written and read, and a launch.  All blocks in slices (few blocks), or every eighth one by
 // two, which fills a last round that is part empty.  Forward and backward without and with every
 // eighth cut, window 1024, 32/8 heads of 128: 8192 tokens in 5 documents, 1.4 rounds of blocks, 618

@@ -2,12 +2,13 @@
 // attention.hip: it stands on that file's LDS tiles, fragments and products).
 //
 //   o_i = sum_j p_ij v_j, p_i. = softmax(scale q_i . k_j), j from row i's document's
-//   first row to i; the backward recomputes p from the log-sum-exp.
+//   first row to i; the backward recomputes p from the log-sum-exp.  The WINDOW
+//   kernels take the rows j of i's window and the document's first ones alone.
 //
 // Every tile of queries and keys lies within one document (seq_block), so the
-// only mask is the causal one, as for a single sequence, and nothing a document
-// holds (an infinity or NaN in V, say, which a zero probability would not hide)
-// can reach another.
+// only masks are the causal one, as for a single sequence, and the window's, and
+// nothing a document holds (an infinity or NaN in V, say, which a zero probability
+// would not hide) can reach another.
 
 template <bool WINDOW>
 using AttnArgs = std::conditional_t<WINDOW, WindowAttn, PackedAttn>;
@@ -345,13 +346,16 @@ __device__ __forceinline__ int packed_slices(const AttnArgs<WINDOW>& p, int row0
 // started last, and short ones waited behind parts of the chip that held long ones
 // (8192 tokens in 23 documents, 32/8 heads of 128: 157 of 256 CUs busy on average).  dK/dV
 // 187 -> 152 us there, 1378 -> 1305 for 32768 tokens in 6, 8/1 heads, 90 -> 59 for 16384
-// in 160, 16/4 heads of 64.  The list hides behind the other workgroups' dQ.  Its order
-// within a step varies, the sums do not; steps of 1/16 scatter a document's neighbours,
-// which read the same rows (1305 -> 1280 us on the long documents).
+// in 160, 16/4 heads of 64.  Without a window the list hides behind the other workgroups'
+// dQ.  Its order within a step varies, the sums do not; steps of 1/16 scatter a document's
+// neighbours, which read the same rows (1305 -> 1280 us on the long documents).
 //
 // With a window the entries are {first row, sign bit: second slice; first query row; row
 // behind the last one; row behind the first tokens, sign bit: sums in parts}, and behind the
-// blocks of a document's first tokens come the chunks of the rows far from them.
+// blocks of a document's first tokens come the chunks of the rows far from them.  A document
+// is one thread's, at about 0.4 us a block or chunk: where few documents are long and the
+// window is short, the list is what dQ takes (32768 rows, 8/1 heads of 64, window 128: dQ in
+// 256 documents 36 us, in one 94, with 4 first tokens, whose 254 chunks are listed too, 202).
 constexpr int kOrderBins = 2048;
 template <bool WINDOW>
 __device__ __forceinline__ void packed_order(const AttnArgs<WINDOW>& p, int* bin) {
@@ -361,7 +365,7 @@ __device__ __forceinline__ void packed_order(const AttnArgs<WINDOW>& p, int* bin
   const int group = p.heads / p.kv_heads;
   for (int i = tid; i < kOrderBins; i += 256) bin[i] = 0;
   __syncthreads();
-  // a document per thread: a document of n blocks takes the pass n^2 tiles, this loop n steps
+  // a document per thread: one of n blocks takes the pass n^2 tiles (with a window n times a window's), this loop n steps
   const auto each = [&](auto visit) __attribute__((always_inline)) {
     int left = p.list_steps;             // no more blocks than that, whatever starts holds
     for (int i = tid; i < p.pk.n_seqs; i += 256) {
@@ -577,8 +581,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 // (32768 tokens in 6 documents, 8/1 heads of 128), and 2.2 times (8192 tokens in 23,
 // 32/8 heads).
 //
-// Tiles of 32 queries, from the block's own first row to the document's end, of
-// each head in turn, stream through a ring of four stages.  Heads of 64 take 128
+// Tiles of 32 queries, from the block's own first row to the document's end (with a
+// window of w rows to the last row that sees a key of the block), of each head in turn,
+// stream through a ring of four stages.  All four groups take every tile, also those that
+// the window or the diagonal hides from a group: of (127 + w)/32 tiles, rounded up, a group's
+// keys are seen from (31 + w)/32 (8 and 5 at w = 128, 36 and 33 at 1024).  Heads of 64 take 128
 // registers and 65 KB: two workgroups per CU (103 -> 90 us for 16384 tokens in 160
 // documents, 16/4 heads).
 //
